@@ -73,7 +73,10 @@ const char *sbvr_status_string(int status);
 /* Library ABI version (major * 100 + minor); 1.01 adds sbvr_decompress,
  * 1.02 sbvr_gemv_a8, 1.03 the coefficient-cache format entry points,
  * 1.04 sbvr_encode and sbvr_decompress_indexed, 1.05 sbvr_gemm_prefill,
- * 1.06 sbvr_gemv_grouped and sbvr_gemv_grouped_a8, 1.07 sbvr_encode_cached. */
+ * 1.06 sbvr_gemv_grouped and sbvr_gemv_grouped_a8, 1.07 sbvr_encode_cached,
+ * 1.08 the operators between the products of a step: sbvr_batch_plan,
+ * sbvr_cache_write, sbvr_tree_attention, sbvr_residual_norm,
+ * sbvr_adjust_logits. */
 int sbvr_version(void);
 
 /*
@@ -343,6 +346,210 @@ int sbvr_encode(int O, int I, int k, const float *W, int n_ratio1, int n_ratio2,
 int sbvr_encode_cached(int O, int I, int k, const float *W, int n_ratio1, int n_ratio2, int n_scale, int n_bias,
                        int normalise, int cache_slots, uint32_t *planes_canon, uint16_t *coeffs_canon,
                        double *mse, uint8_t *hits, hipStream_t stream);
+
+/*
+ * OPERATORS BETWEEN THE PRODUCTS OF A STEP.  A step takes R requests; request
+ * r has context_lens[r] tokens in a paged key/value cache and brings
+ * new_lens[r] more: one (plain decoding), a tree of drafted tokens to verify,
+ * or a prompt chunk.  The step's tokens are numbered request by request;
+ * token t of request r is its j-th new token, j = t - query_start[r], and its
+ * key and value have position context_lens[r] + j of the request.
+ *
+ * Pages: position p of request r lies in page page_table[r][p / page_size] at
+ * offset p % page_size; its slot number is page * page_size + offset.
+ *   page_size  a power of two, 16 .. SBVR_PAGE_MAX.
+ *
+ * Trees: a tree has at most SBVR_TREE_MAX tokens; parents[t] is the index j
+ * of token t's parent within its request (smaller than its own; anything else
+ * makes it a root), and tree_mask[t] has bit j set where token t sees the
+ * request's j-th new token.
+ *
+ * The conventions above hold for these entry points too, with these alignments:
+ * keys, values, queries, attention outputs and the cache 16 bytes, int64 /
+ * uint64 arrays 8, int32 / uint32 / binary32 arrays 4, 16-bit arrays 2.
+ * Zero tokens is a valid step: nothing is enqueued and no pointer is read.
+ */
+enum sbvr_dtype {
+    SBVR_F16 = 0,  /* IEEE binary16 */
+    SBVR_BF16 = 1, /* bfloat16 */
+    SBVR_F32 = 2   /* IEEE binary32 */
+};
+
+#define SBVR_REQUESTS_MAX 4096
+#define SBVR_TREE_MAX 64
+#define SBVR_PAGE_MAX 4096
+
+/*
+ * The plan of a step: pages for the new tokens, and what the other operators
+ * need per token.
+ *   R, T          1 <= R <= SBVR_REQUESTS_MAX requests; room for T >= 0 tokens
+ *                 in the outputs per token.
+ *   context_lens, new_lens   int32 [R] (a negative length counts as 0).
+ *   free_pages    int32 [n_free]: unused pages, taken in order.
+ *   parents       int32 [T] (above), or NULL: each token's parent is the one
+ *                 before it.  Requests of more than SBVR_TREE_MAX new tokens are
+ *                 such chains in any case, and have tree_mask 0.
+ *   page_table    int32 [R][table_stride], max_pages used (in and out).  The
+ *                 ceil(context_lens[r] / page_size) entries of the cached tokens
+ *                 are read; the entries of the pages that the new tokens need
+ *                 beyond them are written: request by request, then by position,
+ *                 from free_pages in order, -1 once that is used up.  A request
+ *                 takes no pages beyond max_pages.  No other entry is touched.
+ *   query_start   int32 [R + 1] (output): tokens before request r, at most T;
+ *                 the last one is the number of tokens.
+ *   token_request int32 [T] (output): the token's request; -1 past the last token.
+ *   positions     int32 [T] (output): context_lens[r] + the number of the
+ *                 token's proper ancestors; 0 past the last token.
+ *   slots         int64 [T] (output): the token's slot; -1 where it has no page
+ *                 and past the last token.
+ *   tree_mask     uint64 [T] (output): the token's ancestors, itself included;
+ *                 0 past the last token.
+ *   used          int32 [2] (output): pages taken (more than n_free: the free
+ *                 pages did not suffice), and new tokens (more than T: the last
+ *                 ones were left out).
+ * Inputs and outputs must not overlap.
+ */
+int sbvr_batch_plan(int R, int T, int page_size, const int32_t *context_lens, const int32_t *new_lens,
+                    const int32_t *free_pages, int n_free, const int32_t *parents, int32_t *page_table,
+                    int max_pages, int64_t table_stride, int32_t *query_start, int32_t *token_request,
+                    int32_t *positions, int64_t *slots, uint64_t *tree_mask, int32_t *used, hipStream_t stream);
+
+/*
+ * A paged key/value cache: element (page, offset, head, d) of the keys is at
+ * k + page * k_page_stride + offset * k_token_stride + head * k_head_stride + d
+ * (strides in elements, multiples of 8, not negative), values likewise.
+ *   dtype     SBVR_F16 or SBVR_BF16.
+ *   head_dim  a multiple of 8, 8 .. 128 (larger: SBVR_E_UNSUPPORTED).
+ * The struct is read during the call only.
+ */
+typedef struct sbvr_kv_cache {
+    void *k, *v;
+    int64_t k_page_stride, k_token_stride, k_head_stride;
+    int64_t v_page_stride, v_token_stride, v_head_stride;
+    int32_t n_pages, page_size, kv_heads, head_dim, dtype;
+} sbvr_kv_cache;
+
+/*
+ * Write a step's keys and values into the cache: token t's at slots[t]; a
+ * token whose slot is negative or past the cache is skipped.  Two tokens must
+ * not share a slot.
+ *   k, v   [T][kv_heads][head_dim] of the cache's dtype, with the given token
+ *          and head strides (elements, multiples of 8, not negative).
+ *   slots  int64 [T].
+ */
+int sbvr_cache_write(const sbvr_kv_cache *cache, int T, const void *k, int64_t k_token_stride,
+                     int64_t k_head_stride, const void *v, int64_t v_token_stride, int64_t v_head_stride,
+                     const int64_t *slots, hipStream_t stream);
+
+/*
+ * Attention of a step's tokens over the cache, which already holds their own
+ * keys and values (sbvr_cache_write).  Token t of request r sees all
+ * context_lens[r] cached tokens, and of its request's new tokens those whose
+ * bit is set in tree_mask[t]; head h reads key/value head
+ * h / (heads / kv_heads).
+ *     out[t][h] = sum_p w_p v_p / sum_p w_p,  w_p = exp(scale q[t][h] . k_p - max)
+ * over the positions p that t sees; a token that sees none gets 0.  Scores,
+ * exponentials' sums and products are accumulated in binary32; the weights
+ * are rounded to the cache's type for the product with the values; the output
+ * is rounded once.  What lies in a slot that a token does not see has no
+ * effect on it, NaN and infinities included.
+ *   q            [T][heads][head_dim] of the cache's dtype, with strides as
+ *                sbvr_cache_write's inputs; heads a multiple of kv_heads.
+ *   page_table   int32 [R][table_stride], max_pages used.  A request is cut to
+ *                max_pages * page_size tokens; the positions of a page outside
+ *                0 .. n_pages - 1 are not seen.
+ *   context_lens int32 [R]; query_start int32 [R + 1] ascending, at most T;
+ *   tree_mask    uint64 [T].  1 <= R <= SBVR_REQUESTS_MAX.
+ *   max_new      1 .. SBVR_TREE_MAX: no request brings more new tokens than
+ *                this (the rest of a longer one is left out).
+ *   out          [T][heads][head_dim] contiguous; rows past query_start[R] are
+ *                left as they are.  Must not overlap the inputs.
+ *   workspace    sbvr_tree_attention_workspace_bytes, 16-byte aligned; its
+ *                content needs no preparation and is not kept.
+ */
+size_t sbvr_tree_attention_workspace_bytes(int R, int max_new, int heads, int kv_heads, int head_dim);
+int sbvr_tree_attention(const sbvr_kv_cache *cache, int R, int T, int heads, const void *q, int64_t q_token_stride,
+                        int64_t q_head_stride, const int32_t *page_table, int max_pages, int64_t table_stride,
+                        const int32_t *context_lens, const int32_t *query_start, const uint64_t *tree_mask,
+                        int max_new, float scale, void *out, void *workspace, size_t ws_bytes, hipStream_t stream);
+
+#define SBVR_NORM_MAX_WIDTH 32768
+
+/*
+ * The norms around a block, with its gate and residual scale, in one pass:
+ *     z = y * rsqrt(mean(y^2) + eps) * post_weight     (post_weight NULL: z = y)
+ *     x' = x + scale * gate * z                        (gate NULL: 1; y NULL: x' = x)
+ *     h = x' * rsqrt(mean(x'^2) + eps) * pre_weight
+ * per token, in binary32, each output rounded once (h from the unrounded x').
+ *   T, H     T >= 0 tokens of 1 <= H <= SBVR_NORM_MAX_WIDTH elements (more:
+ *            SBVR_E_UNSUPPORTED).
+ *   dtype    of y, gate, the weights and h: SBVR_F16 or SBVR_BF16.
+ *   x_dtype  of x and x_out (the residual stream): dtype or SBVR_F32.
+ *   x, y, gate, x_out, h_out   [T][H] with the given row strides in elements;
+ *            gate_stride 0 is one gate for all tokens, [H]; output rows must not
+ *            overlap.
+ *   x_out    may be x itself (same stride), or NULL: not wanted.
+ *   h_out    NULL: not wanted (and pre_weight is not read; else it must be given).
+ * Apart from x_out = x, inputs and outputs must not overlap.
+ */
+int sbvr_residual_norm(int T, int H, int dtype, int x_dtype, const void *x, int64_t x_stride, const void *y,
+                       int64_t y_stride, const void *post_weight, const void *gate, int64_t gate_stride, float scale,
+                       const void *pre_weight, float eps, void *x_out, int64_t x_out_stride, void *h_out,
+                       int64_t h_stride, hipStream_t stream);
+
+/*
+ * Adjustment of logits before sampling.  Row t belongs to request r =
+ * token_request[t] (NULL: r = t); for token v of the vocabulary, with c the
+ * number of times v occurs among the request's generated tokens and on t's
+ * drafted path, and "seen" where c > 0 or v occurs in the request's prompt:
+ *     l = logits[t][v]
+ *     seen:   l = l > 0 ? l / repetition[r] : l * repetition[r]
+ *     l = l - frequency[r] * c - presence[r] * (c > 0)
+ *     l = l + bias(r, v)
+ *     l = l / temperature[r]            (temperature <= 0: unchanged)
+ *     grammar bit v of the row is 0:  l = -infinity
+ * in binary32, rounded once to the output type.
+ *   logits  [T][V] of dtype, row stride logits_stride elements; out [T][V] of
+ *           out_dtype (dtype or SBVR_F32), row stride out_stride; out may be
+ *           logits itself where the types and strides agree.  Rows whose request
+ *           is outside 0 .. R - 1 are converted, not adjusted.
+ *   history int32, request r's tokens at history_start[r] .. history_start[r + 1]
+ *           (int32 [R + 1], ascending), the first prompt_lens[r] (int32 [R], NULL:
+ *           0) of them its prompt, the others generated; NULL: none.
+ *   repetition, frequency, presence, temperature  binary32 [R], or NULL: 1, 0, 0, 1.
+ *   bias_tokens, bias_values  int32 and binary32, request r's at bias_start[r] ..
+ *           bias_start[r + 1] (int32 [R + 1]); of several entries for a token the
+ *           last one counts; NULL: none.
+ *   grammar uint32 [grammar_count][grammar_stride]: bit v % 32 of word v / 32 is 1
+ *           where v is allowed; grammar_rows int32 [T] names each row's mask
+ *           (outside 0 .. grammar_count - 1: unconstrained; NULL: row t has mask t);
+ *           grammar NULL: none.
+ *   draft_tokens int32 [T], tree_mask uint64 [T], query_start int32 [R + 1]: token
+ *           t's drafted path is the tokens of its tree_mask, numbered within the
+ *           request from query_start[r]; all three or none (NULL).
+ * Token ids outside 0 .. V - 1 are ignored.  At most 65535 rows and 2^30 tokens
+ * in the vocabulary (more: SBVR_E_UNSUPPORTED).  The struct is read during the call.
+ */
+typedef struct sbvr_logits_args {
+    int32_t R, T, V, dtype, out_dtype;
+    const void *logits;
+    int64_t logits_stride;
+    void *out;
+    int64_t out_stride;
+    const int32_t *token_request;
+    const int32_t *history, *history_start, *prompt_lens;
+    const float *repetition, *frequency, *presence, *temperature;
+    const int32_t *bias_tokens, *bias_start;
+    const float *bias_values;
+    const uint32_t *grammar;
+    int64_t grammar_stride;
+    const int32_t *grammar_rows;
+    int32_t grammar_count;
+    const int32_t *draft_tokens, *query_start;
+    const uint64_t *tree_mask;
+} sbvr_logits_args;
+
+int sbvr_adjust_logits(const sbvr_logits_args *args, hipStream_t stream);
 
 #ifdef __cplusplus
 }

@@ -32,8 +32,36 @@ EXPORTED = (
     "sbvr_decompress", "sbvr_gemv_a8", "sbvr_packed_index_bytes", "sbvr_packed_table_bytes",
     "sbvr_pack_indexed", "sbvr_unpack_indexed", "sbvr_gemv_indexed", "sbvr_gemv_indexed_a8", "sbvr_encode",
     "sbvr_decompress_indexed", "sbvr_gemm_prefill", "sbvr_gemv_grouped", "sbvr_gemv_grouped_a8",
-    "sbvr_encode_cached",
+    "sbvr_encode_cached", "sbvr_batch_plan", "sbvr_cache_write", "sbvr_tree_attention_workspace_bytes",
+    "sbvr_tree_attention", "sbvr_residual_norm", "sbvr_adjust_logits",
 )
+
+# enum sbvr_dtype and the limits of the operators between the products
+SBVR_F16, SBVR_BF16, SBVR_F32 = 0, 1, 2
+REQUESTS_MAX = 4096
+TREE_MAX = 64
+PAGE_MAX = 4096
+NORM_MAX_WIDTH = 32768
+
+
+class CacheStruct(C.Structure):
+    """sbvr_kv_cache"""
+    _fields_ = ([(n, C.c_void_p) for n in ("k", "v")]
+                + [(n, C.c_int64) for n in ("k_page_stride", "k_token_stride", "k_head_stride",
+                                            "v_page_stride", "v_token_stride", "v_head_stride")]
+                + [(n, C.c_int32) for n in ("n_pages", "page_size", "kv_heads", "head_dim", "dtype")])
+
+
+class LogitsStruct(C.Structure):
+    """sbvr_logits_args"""
+    _fields_ = ([(n, C.c_int32) for n in ("R", "T", "V", "dtype", "out_dtype")]
+                + [("logits", C.c_void_p), ("logits_stride", C.c_int64), ("out", C.c_void_p),
+                   ("out_stride", C.c_int64)]
+                + [(n, C.c_void_p) for n in ("token_request", "history", "history_start", "prompt_lens", "repetition",
+                                             "frequency", "presence", "temperature", "bias_tokens", "bias_start",
+                                             "bias_values", "grammar")]
+                + [("grammar_stride", C.c_int64), ("grammar_rows", C.c_void_p), ("grammar_count", C.c_int32)]
+                + [(n, C.c_void_p) for n in ("draft_tokens", "query_start", "tree_mask")])
 
 
 class SBVRError(RuntimeError):
@@ -56,7 +84,7 @@ def _load():
         raise ImportError(
             f"SBVR HIP library not built ({path}); run `python -c 'import __graft_entry__ as g; g.build()'`")
     lib = C.CDLL(path)
-    vp, sz, i32 = C.c_void_p, C.c_size_t, C.c_int
+    vp, sz, i32, i64, f32 = C.c_void_p, C.c_size_t, C.c_int, C.c_int64, C.c_float
     sig = {
         "sbvr_status_string": (C.c_char_p, [i32]),
         "sbvr_version": (i32, []),
@@ -81,6 +109,14 @@ def _load():
         "sbvr_gemm_prefill": (i32, [i32, i32, i32, vp, vp, vp, vp, i32, vp]),
         "sbvr_gemv_grouped": (i32, [i32, vp, i32, i32, vp, vp, vp, vp, vp, sz, vp]),
         "sbvr_gemv_grouped_a8": (i32, [i32, vp, i32, i32, vp, vp, vp, vp, vp, sz, vp]),
+        "sbvr_batch_plan": (i32, [i32, i32, i32, vp, vp, vp, i32, vp, vp, i32, i64, vp, vp, vp, vp, vp, vp, vp]),
+        "sbvr_cache_write": (i32, [vp, i32, vp, i64, i64, vp, i64, i64, vp, vp]),
+        "sbvr_tree_attention_workspace_bytes": (sz, [i32, i32, i32, i32, i32]),
+        "sbvr_tree_attention": (i32, [vp, i32, i32, i32, vp, i64, i64, vp, i32, i64, vp, vp, vp, i32, f32, vp, vp, sz,
+                                      vp]),
+        "sbvr_residual_norm": (i32, [i32, i32, i32, i32, vp, i64, vp, i64, vp, vp, i64, f32, vp, f32, vp, i64, vp, i64,
+                                     vp]),
+        "sbvr_adjust_logits": (i32, [vp, vp]),
     }
     for name, (res, args) in sig.items():
         f = getattr(lib, name)
@@ -218,6 +254,44 @@ def sbvr_decompress_indexed(O, I, k, n_sets, planes_dev, index_dev, table_dev, W
 
 def sbvr_gemm_prefill(O, I, k, planes_dev, coeffs_dev, X, Y, T, stream=0) -> int:
     return _lib.sbvr_gemm_prefill(O, I, k, planes_dev, coeffs_dev, X, Y, T, stream)
+
+
+def sbvr_batch_plan(R, T, page_size, context_lens, new_lens, free_pages, n_free, parents, page_table, max_pages,
+                    table_stride, query_start, token_request, positions, slots, tree_mask, used, stream=0) -> int:
+    return _lib.sbvr_batch_plan(R, T, page_size, context_lens, new_lens, free_pages, n_free, parents, page_table,
+                                max_pages, table_stride, query_start, token_request, positions, slots, tree_mask,
+                                used, stream)
+
+
+def sbvr_cache_write(cache, T, k, k_token_stride, k_head_stride, v, v_token_stride, v_head_stride, slots,
+                     stream=0) -> int:
+    """cache: a CacheStruct (or None)."""
+    return _lib.sbvr_cache_write(None if cache is None else C.addressof(cache), T, k, k_token_stride, k_head_stride, v,
+                                 v_token_stride, v_head_stride, slots, stream)
+
+
+def sbvr_tree_attention_workspace_bytes(R, max_new, heads, kv_heads, head_dim) -> int:
+    return _lib.sbvr_tree_attention_workspace_bytes(R, max_new, heads, kv_heads, head_dim)
+
+
+def sbvr_tree_attention(cache, R, T, heads, q, q_token_stride, q_head_stride, page_table, max_pages, table_stride,
+                        context_lens, query_start, tree_mask, max_new, scale, out, workspace=None, ws_bytes=0,
+                        stream=0) -> int:
+    """cache: a CacheStruct (or None)."""
+    return _lib.sbvr_tree_attention(None if cache is None else C.addressof(cache), R, T, heads, q, q_token_stride,
+                                    q_head_stride, page_table, max_pages, table_stride, context_lens, query_start,
+                                    tree_mask, max_new, scale, out, workspace, ws_bytes, stream)
+
+
+def sbvr_residual_norm(T, H, dtype, x_dtype, x, x_stride, y, y_stride, post_weight, gate, gate_stride, scale,
+                       pre_weight, eps, x_out, x_out_stride, h_out, h_stride, stream=0) -> int:
+    return _lib.sbvr_residual_norm(T, H, dtype, x_dtype, x, x_stride, y, y_stride, post_weight, gate, gate_stride,
+                                   scale, pre_weight, eps, x_out, x_out_stride, h_out, h_stride, stream)
+
+
+def sbvr_adjust_logits(args, stream=0) -> int:
+    """args: a LogitsStruct (or None)."""
+    return _lib.sbvr_adjust_logits(None if args is None else C.addressof(args), stream)
 
 
 # --------------------------------------------------------------------------
@@ -503,3 +577,8 @@ def algorithmic_bytes(O: int, I: int, k: int, B: int = 1) -> int:
     """Bytes the method must move per call: planes k*O*I/8, fp16 coefficients
     2*k*O*I/128, activations 2*I*B and outputs 2*O*B."""
     return k * O * I // 8 + 2 * k * O * I // GROUP + 2 * I * B + 2 * O * B
+
+
+# the operators between the products of a step
+from .step import (BatchPlan, KVCache, adjust_logits, batch_plan, cache_write, residual_norm,  # noqa: E402,F401
+                   tree_attention)

@@ -1,0 +1,120 @@
+// Shared by the operators between the products of a step (plan, cache write,
+// attention, norms, logits): element types, launch parameters, and the scan
+// over the requests that several kernels repeat in every workgroup.
+#pragma once
+
+#include <hip/hip_fp16.h>
+#include <hip/hip_runtime.h>
+
+#include <type_traits>
+
+#include "launch.h"
+#include "sbvr.h"
+
+namespace sbvr {
+
+typedef __bf16 bf16_t;
+typedef _Float16 f16_t;
+
+// a 16-byte or 8-byte piece of a row of 16-bit elements
+template <int N>
+struct alignas(2 * N) Halves {
+    uint32_t w[N / 2];
+};
+
+struct PlanArgs {
+    int R, T, page_shift, n_free, max_pages;
+    const int32_t *context_lens, *new_lens, *free_pages, *parents;
+    int32_t *page_table;
+    int64_t table_stride;
+    int32_t *query_start, *token_request, *positions;
+    int64_t *slots;
+    uint64_t *tree_mask;
+    int32_t *used;
+};
+
+struct AttnArgs {
+    sbvr_kv_cache kv;
+    int R, T, heads, max_pages, max_new;
+    const void *q;
+    int64_t q_token_stride, q_head_stride;
+    const int32_t *page_table;
+    int64_t table_stride;
+    const int32_t *context_lens, *query_start;
+    const uint64_t *tree_mask;
+    float scale;
+    void *out;
+    void *workspace;
+};
+
+struct NormArgs {
+    int T, H;
+    const void *x, *y, *post, *gate, *pre;
+    void *x_out, *h_out;
+    int64_t x_stride, y_stride, gate_stride, x_out_stride, h_stride;
+    float scale, eps;
+};
+
+int launch_plan(const PlanArgs &a, hipStream_t stream);
+int launch_cache_write(const sbvr_kv_cache &c, int T, const void *k, int64_t k_token_stride, int64_t k_head_stride,
+                       const void *v, int64_t v_token_stride, int64_t v_head_stride, const int64_t *slots,
+                       hipStream_t stream);
+size_t attn_workspace_bytes(int R, int max_new, int heads, int kv_heads, int head_dim);
+int launch_attn(const AttnArgs &a, hipStream_t stream);
+int launch_norm(const NormArgs &a, int dtype, int x_dtype, hipStream_t stream);
+int launch_logits(const sbvr_logits_args &a, hipStream_t stream);
+
+// The last index i of the ascending start[0 .. n] with start[i] <= v, for
+// start[0] <= v < start[n]: the owner of item v, empty owners skipped.
+template <typename I>
+__device__ __forceinline__ int owner_of(const I *start, int n, I v)
+{
+    int lo = 0, hi = n;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (start[mid] <= v)
+            lo = mid;
+        else
+            hi = mid;
+    }
+    return lo;
+}
+
+// Exclusive prefix sums of two values per thread over a workgroup of THREADS
+// threads (a multiple of 64); `total` gets the sums.  scratch: 2 * THREADS / 64
+// entries of LDS.  Ends with a barrier passed by every thread.
+template <int THREADS>
+__device__ __forceinline__ void scan_pair(long long &a, long long &b, long long &total_a, long long &total_b,
+                                          long long *scratch)
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    long long ia = a, ib = b;
+#pragma unroll
+    for (int s = 1; s < 64; s <<= 1) {
+        const long long pa = __shfl_up(ia, s), pb = __shfl_up(ib, s);
+        if (lane >= s) {
+            ia += pa;
+            ib += pb;
+        }
+    }
+    if (lane == 63) {
+        scratch[2 * wave] = ia;
+        scratch[2 * wave + 1] = ib;
+    }
+    __syncthreads();
+    long long ba = 0, bb = 0;
+    total_a = total_b = 0;
+#pragma unroll
+    for (int w = 0; w < THREADS / 64; ++w) {
+        if (w == wave) {
+            ba = total_a;
+            bb = total_b;
+        }
+        total_a += scratch[2 * w];
+        total_b += scratch[2 * w + 1];
+    }
+    a = ba + ia - a;
+    b = bb + ib - b;
+}
+
+}  // namespace sbvr

@@ -1,0 +1,247 @@
+"""The operators between the products of a step, on torch tensors: the plan of
+a batch, the paged key/value cache, attention for trees of drafted tokens, the
+norms around a block and the adjustment of logits (include/sbvr.h says what
+each computes).  Marshalling only, as the package's other helpers: shapes are
+checked here, outputs come from torch, and a non-zero status raises
+``SBVRError``.
+
+A step in order: ``batch_plan`` (pages, slots, masks), per layer
+``residual_norm`` -> products -> ``cache_write`` -> ``tree_attention`` ->
+products, and ``adjust_logits`` on the last product.
+"""
+from __future__ import annotations
+
+import torch
+
+from . import (SBVR_BF16, SBVR_F16, SBVR_F32, CacheStruct, LogitsStruct, _check, _stream, sbvr_adjust_logits,
+               sbvr_batch_plan, sbvr_cache_write, sbvr_residual_norm, sbvr_tree_attention,
+               sbvr_tree_attention_workspace_bytes)
+
+_DTYPE = {torch.float16: SBVR_F16, torch.bfloat16: SBVR_BF16, torch.float32: SBVR_F32}
+
+
+def _dense(t, dtype, shape, device, what):
+    """The pointer of an optional contiguous tensor of one dtype and shape
+    (None in a shape: any size)."""
+    if t is None:
+        return None
+    assert t.dtype == dtype and t.is_contiguous() and t.device == device and len(t.shape) == len(shape) \
+        and all(n is None or n == m for n, m in zip(shape, t.shape)), \
+        f"{what} must be a contiguous {dtype} tensor of shape {shape} on {device}"
+    return t.data_ptr()
+
+
+def _rows(t, dtype, shape, device, what):
+    """The pointer and row stride of a 2-D tensor with contiguous rows."""
+    assert t.dtype == dtype and tuple(t.shape) == tuple(shape) and t.device == device \
+        and (t.stride(1) == 1 or shape[1] == 1), f"{what} must be a {dtype} tensor {tuple(shape)} of contiguous rows"
+    return t.data_ptr(), t.stride(0)
+
+
+def _table(page_table, R, device):
+    assert page_table.dtype == torch.int32 and page_table.dim() == 2 and page_table.shape[0] == R \
+        and page_table.device == device and (page_table.stride(1) == 1 or page_table.shape[1] == 1), \
+        "page_table must be an int32 tensor [requests][max_pages] of contiguous rows on the batch's device"
+    # a single row's stride means nothing, and torch may report a smaller one
+    return page_table.data_ptr(), page_table.shape[1], max(page_table.stride(0), page_table.shape[1])
+
+
+class BatchPlan:
+    """What ``batch_plan`` returns: device tensors query_start int32 [R + 1],
+    token_request and positions int32 [T], slots int64 [T], tree_mask int64
+    [T] (bits of a uint64), used int32 [2] (pages taken, new tokens)."""
+
+    def __init__(self, R: int, T: int, device):
+        i32, i64 = torch.int32, torch.int64
+        self.query_start = torch.empty(R + 1, dtype=i32, device=device)
+        self.token_request = torch.empty(T, dtype=i32, device=device)
+        self.positions = torch.empty(T, dtype=i32, device=device)
+        self.slots = torch.empty(T, dtype=i64, device=device)
+        self.tree_mask = torch.empty(T, dtype=i64, device=device)
+        self.used = torch.empty(2, dtype=i32, device=device)
+
+
+def batch_plan(context_lens, new_lens, free_pages, page_table, page_size: int, n_tokens: int, parents=None, out=None,
+               stream=None) -> BatchPlan:
+    """Pages for a step's new tokens (entered into page_table, in place) and
+    what the other operators need per token.  context_lens, new_lens int32
+    [R]; free_pages int32 [n]; page_table int32 [R][max_pages]; parents int32
+    [n_tokens] within each request (None: chains); n_tokens: room for the
+    step's tokens.  out: a BatchPlan of the same sizes to fill."""
+    device = context_lens.device
+    assert context_lens.is_cuda and context_lens.dim() == 1
+    R, T = context_lens.shape[0], int(n_tokens)
+    i32 = torch.int32
+    table, max_pages, stride = _table(page_table, R, device)
+    if out is None:
+        p = BatchPlan(R, T, device)
+    else:
+        p = out
+        for name, dtype, n in (("query_start", i32, R + 1), ("token_request", i32, T), ("positions", i32, T),
+                               ("slots", torch.int64, T), ("tree_mask", torch.int64, T), ("used", i32, 2)):
+            _dense(getattr(p, name), dtype, (n,), device, name)
+    _check(sbvr_batch_plan(R, T, page_size, _dense(context_lens, i32, (R,), device, "context_lens"),
+                           _dense(new_lens, i32, (R,), device, "new_lens"),
+                           _dense(free_pages, i32, (None,), device, "free_pages"), free_pages.shape[0],
+                           _dense(parents, i32, (T,), device, "parents"), table, max_pages, stride,
+                           p.query_start.data_ptr(), p.token_request.data_ptr(), p.positions.data_ptr(),
+                           p.slots.data_ptr(), p.tree_mask.data_ptr(), p.used.data_ptr(), _stream(stream)),
+           "sbvr_batch_plan")
+    return p
+
+
+class KVCache:
+    """A paged key/value cache: two fp16 or bf16 tensors [pages][page_size]
+    [kv_heads][head_dim], of any strides with contiguous heads (a head-major
+    page is a transposed view)."""
+
+    def __init__(self, k, v):
+        assert k.dim() == 4 and k.shape == v.shape and k.dtype == v.dtype and k.dtype in _DTYPE \
+            and k.is_cuda and k.device == v.device, "k and v must be alike, [pages][page_size][kv_heads][head_dim]"
+        assert k.stride(3) == 1 and v.stride(3) == 1, "a head's elements must be contiguous"
+        self.k, self.v = k, v
+        n_pages, page_size, heads, dim = k.shape
+        self.struct = CacheStruct(k.data_ptr(), v.data_ptr(), *k.stride()[:3], *v.stride()[:3], n_pages, page_size,
+                                  heads, dim, _DTYPE[k.dtype])
+
+    @staticmethod
+    def alloc(n_pages: int, page_size: int, kv_heads: int, head_dim: int, dtype=torch.float16, device="cuda"):
+        shape = (n_pages, page_size, kv_heads, head_dim)
+        return KVCache(torch.empty(shape, dtype=dtype, device=device), torch.empty(shape, dtype=dtype, device=device))
+
+
+def _heads(t, heads, dim, cache, what):
+    """The pointer and the token and head strides of a [T][heads][dim] tensor
+    that goes with a cache."""
+    assert t.dim() == 3 and t.shape[1] == heads and t.shape[2] == dim and t.dtype == cache.k.dtype \
+        and t.device == cache.k.device and t.stride(2) == 1, \
+        f"{what} must be a {cache.k.dtype} tensor [tokens][{heads}][{dim}] with contiguous heads on the cache's device"
+    return t.data_ptr(), t.stride(0), t.stride(1)
+
+
+def cache_write(cache: KVCache, k, v, slots, stream=None):
+    """Write a step's keys and values [T][kv_heads][head_dim] (views with
+    contiguous heads) to the slots (int64 [T]; negative: skipped)."""
+    heads, dim = cache.k.shape[2:]
+    T = k.shape[0]
+    assert v.shape[0] == T
+    _check(sbvr_cache_write(cache.struct, T, *_heads(k, heads, dim, cache, "k"), *_heads(v, heads, dim, cache, "v"),
+                            _dense(slots, torch.int64, (T,), k.device, "slots"), _stream(stream)), "sbvr_cache_write")
+
+
+def tree_attention(q, cache: KVCache, page_table, context_lens, query_start, tree_mask, max_new: int, scale=None,
+                   out=None, workspace=None, stream=None):
+    """Attention of a step's tokens q [T][heads][head_dim] over the cache,
+    which already holds their keys and values; max_new: the most new tokens of
+    a request; scale: 1 / sqrt(head_dim) by default.  Returns [T][heads]
+    [head_dim].  workspace: a uint8 tensor of
+    sbvr_tree_attention_workspace_bytes, by default a new one."""
+    T, H, D = q.shape
+    R, device = context_lens.shape[0], q.device
+    kv_heads = cache.k.shape[2]
+    qp, q_token, q_head = _heads(q, H, cache.k.shape[3], cache, "q")
+    table, max_pages, stride = _table(page_table, R, device)
+    if out is None:
+        out = torch.empty((T, H, D), dtype=q.dtype, device=device)
+    need = sbvr_tree_attention_workspace_bytes(R, max_new, H, kv_heads, D)
+    if workspace is None and need:
+        workspace = torch.empty(need, dtype=torch.uint8, device=device)
+        if stream is not None:
+            workspace.record_stream(stream)
+    _check(sbvr_tree_attention(cache.struct, R, T, H, qp, q_token, q_head, table, max_pages, stride,
+                               _dense(context_lens, torch.int32, (R,), device, "context_lens"),
+                               _dense(query_start, torch.int32, (R + 1,), device, "query_start"),
+                               _dense(tree_mask, torch.int64, (T,), device, "tree_mask"), max_new,
+                               float(D ** -0.5 if scale is None else scale),
+                               _dense(out, q.dtype, (T, H, D), device, "out"),
+                               _dense(workspace, torch.uint8, (None,), device, "workspace"),
+                               0 if workspace is None else workspace.numel(), _stream(stream)),
+           "sbvr_tree_attention")
+    return out
+
+
+def residual_norm(x, y=None, post_weight=None, gate=None, scale: float = 1.0, pre_weight=None, eps: float = 1e-5,
+                  x_out=None, h_out=None, stream=None):
+    """x' = x + scale * gate * rms(y) * post_weight and h = rms(x') *
+    pre_weight for tokens x [T][H] (fp16, bf16 or fp32 stream), y [T][H] and
+    gate [T][H] or [H] (fp16 or bf16); returns (x', h).  Without pre_weight h
+    is None; without y x' is x itself.  x_out may be x."""
+    assert x.dim() == 2 and x.is_cuda and x.dtype in _DTYPE
+    T, H = x.shape
+    device = x.device
+    given = [t for t in (y, post_weight, gate, pre_weight, h_out) if t is not None]
+    dtype = given[0].dtype if given else x.dtype
+    assert dtype in _DTYPE, "y, gate, weights and h must be fp16 or bf16"
+    assert y is not None or (post_weight is None and gate is None), "a post_weight or a gate needs a y"
+    assert y is not None or x_out is None, "without a y there is no x' to write"
+    assert pre_weight is not None or h_out is None, "an h needs a pre_weight"
+    assert y is not None or pre_weight is not None, "nothing to compute: neither y nor pre_weight"
+    xp, x_stride = _rows(x, x.dtype, (T, H), device, "x")
+    yp, y_stride = (None, 0) if y is None else _rows(y, dtype, (T, H), device, "y")
+    if gate is None or gate.dim() == 1:
+        gp, g_stride = _dense(gate, dtype, (H,), device, "gate"), 0
+    else:
+        gp, g_stride = _rows(gate, dtype, (T, H), device, "gate")
+    op, o_stride, hp, h_stride = None, 0, None, 0
+    if y is not None:
+        x_out = torch.empty((T, H), dtype=x.dtype, device=device) if x_out is None else x_out
+        op, o_stride = _rows(x_out, x.dtype, (T, H), device, "x_out")
+    if pre_weight is not None:
+        h_out = torch.empty((T, H), dtype=dtype, device=device) if h_out is None else h_out
+        hp, h_stride = _rows(h_out, dtype, (T, H), device, "h_out")
+    _check(sbvr_residual_norm(T, H, _DTYPE[dtype], _DTYPE[x.dtype], xp, x_stride, yp, y_stride,
+                              _dense(post_weight, dtype, (H,), device, "post_weight"), gp, g_stride, float(scale),
+                              _dense(pre_weight, dtype, (H,), device, "pre_weight"), float(eps), op, o_stride, hp,
+                              h_stride, _stream(stream)), "sbvr_residual_norm")
+    return (x if y is None else x_out), h_out
+
+
+def adjust_logits(logits, history=None, history_start=None, prompt_lens=None, repetition=None, frequency=None,
+                  presence=None, temperature=None, bias_tokens=None, bias_values=None, bias_start=None, grammar=None,
+                  grammar_rows=None, token_request=None, query_start=None, tree_mask=None, draft_tokens=None,
+                  n_requests=None, out=None, out_dtype=None, stream=None):
+    """The logits [T][V] (fp16, bf16 or fp32) with the penalties, biases,
+    temperatures and grammar masks of their requests applied (every part
+    optional); out may be logits.  The number of requests R comes from
+    history_start, bias_start or the parameters per request, or n_requests;
+    without token_request row t is request t."""
+    assert logits.dim() == 2 and logits.is_cuda and logits.dtype in _DTYPE
+    T, V = logits.shape
+    device = logits.device
+    i32, f32 = torch.int32, torch.float32
+    R = n_requests
+    if R is None:
+        R = next((t.shape[0] - less for t, less in ((history_start, 1), (bias_start, 1), (query_start, 1),
+                                                    (prompt_lens, 0), (repetition, 0), (frequency, 0), (presence, 0),
+                                                    (temperature, 0)) if t is not None), T)
+    if out is None:
+        out = torch.empty((T, V), dtype=out_dtype or logits.dtype, device=device)
+    assert out.dtype in _DTYPE and (out_dtype is None or out.dtype == out_dtype)
+    assert (history is None) == (history_start is None), "history and history_start go together"
+    assert (bias_tokens is None) == (bias_start is None) == (bias_values is None), "the three bias tensors go together"
+    lp, l_stride = _rows(logits, logits.dtype, (T, V), device, "logits")
+    op, o_stride = _rows(out, out.dtype, (T, V), device, "out")
+    n_bias = None if bias_tokens is None else bias_tokens.shape[0]
+    gp, g_stride, g_count = None, 0, 0
+    if grammar is not None:
+        g_count = grammar.shape[0]
+        gp, g_stride = _rows(grammar, i32, (g_count, (V + 31) // 32), device, "grammar")
+        g_stride = max(g_stride, grammar.shape[1])
+    args = LogitsStruct(R, T, V, _DTYPE[logits.dtype], _DTYPE[out.dtype], lp, l_stride, op, o_stride,
+                        _dense(token_request, i32, (T,), device, "token_request"),
+                        _dense(history, i32, (None,), device, "history"),
+                        _dense(history_start, i32, (R + 1,), device, "history_start"),
+                        _dense(prompt_lens, i32, (R,), device, "prompt_lens"),
+                        _dense(repetition, f32, (R,), device, "repetition"),
+                        _dense(frequency, f32, (R,), device, "frequency"),
+                        _dense(presence, f32, (R,), device, "presence"),
+                        _dense(temperature, f32, (R,), device, "temperature"),
+                        _dense(bias_tokens, i32, (n_bias,), device, "bias_tokens"),
+                        _dense(bias_start, i32, (R + 1,), device, "bias_start"),
+                        _dense(bias_values, f32, (n_bias,), device, "bias_values"), gp, g_stride,
+                        _dense(grammar_rows, i32, (T,), device, "grammar_rows"), g_count,
+                        _dense(draft_tokens, i32, (T,), device, "draft_tokens"),
+                        _dense(query_start, i32, (R + 1,), device, "query_start"),
+                        _dense(tree_mask, torch.int64, (T,), device, "tree_mask"))
+    _check(sbvr_adjust_logits(args, _stream(stream)), "sbvr_adjust_logits")
+    return out
