@@ -420,6 +420,7 @@ int sbvr_batch_plan(int R, int T, int page_size, const int32_t *context_lens, co
  * (strides in elements, multiples of 8, not negative), values likewise.
  *   dtype     SBVR_F16 or SBVR_BF16.
  *   head_dim  a multiple of 8, 8 .. 128 (larger: SBVR_E_UNSUPPORTED).
+ * Token strides are at most 2^30 / page_size (else SBVR_E_UNSUPPORTED).
  * The struct is read during the call only.
  */
 typedef struct sbvr_kv_cache {

@@ -39,6 +39,9 @@ int check_cache(const sbvr_kv_cache *c)
         return SBVR_E_INVALID_ARG;
     if (c->head_dim > 128 || c->kv_heads > 4096)
         return SBVR_E_UNSUPPORTED;
+    // the kernels' byte offsets within a page are 32-bit
+    if ((c->k_token_stride | c->v_token_stride) > (1ll << 30) / c->page_size)
+        return SBVR_E_UNSUPPORTED;
     if (!aligned(c->k, 16) || !aligned(c->v, 16))
         return SBVR_E_ALIGNMENT;
     return SBVR_OK;
