@@ -135,7 +135,7 @@ int sbvr_tree_attention(const sbvr_kv_cache *cache, int R, int T, int heads, con
         !aligned(tree_mask, 8) || !aligned(out, 16) || (need && !aligned(workspace, 16)))
         return SBVR_E_ALIGNMENT;
     const AttnArgs a{*cache, R, T, heads, max_pages, max_new, q, q_token_stride, q_head_stride, page_table,
-                     table_stride, context_lens, query_start, tree_mask, scale, out, workspace};
+                     table_stride, context_lens, query_start, tree_mask, scale, out, workspace, 0};
     return launch_attn(a, stream);
 }
 

@@ -26,7 +26,8 @@
 //     reads are free of bank conflicts.
 //
 // Work: the cached positions of all items, in units of one step of a
-// workgroup, are one line that is cut into (up to) SPLITS equal ranges,
+// workgroup, are one line that is cut into (up to) SPLITS (as many workgroups as the chip
+// holds) equal ranges,
 // whatever the requests' lengths; a workgroup runs the segments of items in
 // its range.  An item within one range is finished there; of an item that a
 // cut divides, every workgroup leaves its unnormalised sums, and a second
@@ -54,7 +55,7 @@ typedef uint32_t v4u __attribute__((ext_vector_type(4)));
 
 constexpr int ATTN_WAVES = 4, ATTN_THREADS = 64 * ATTN_WAVES;
 constexpr int TILE = 32;              // positions of one score / product step
-constexpr int SPLITS = 512;           // ranges: two workgroups a CU
+constexpr int CUS = 256;
 constexpr float NO_SCORE = -1.0e30f;  // running maximum before any score
 constexpr float GAP = 8.f;            // binary exponent by which weights may exceed 1
 constexpr float LOG2E = 1.4426950408889634f;
@@ -96,12 +97,32 @@ __device__ __forceinline__ float unpack(uint32_t w, int hi)
         return (float)__builtin_bit_cast(f16_t, (uint16_t)h);
 }
 
+// Sixteen lanes' 8-byte pieces of LDS as four rows of sixteen 16-bit elements
+// (lane i: row i / 4, elements 4 (i % 4) ..), read by columns: lane i gets
+// element i of the four rows.
+typedef uint32_t v2u __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ v2u read_transposed(const char *p)
+{
+    typedef short v4s __attribute__((ext_vector_type(4)));
+    typedef __attribute__((address_space(3))) v4s lds_v4s;
+    return __builtin_bit_cast(v2u, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s *)p));
+}
+
 // true where one of the two 16-bit values is an infinity or NaN
 template <bool BF>
 __device__ __forceinline__ bool not_finite(uint32_t w)
 {
     constexpr uint32_t E = BF ? 0x7f80u : 0x7c00u;
-    return (w & E) == E || (w & (E << 16)) == (E << 16);
+    return ((w & E) == E) | ((w & (E << 16)) == (E << 16));
+}
+
+// A value that is the same in every lane and that no kernel of this file
+// writes, read on the scalar side: a vector load would have its wait among
+// those of the tiles.
+template <typename T>
+__device__ __forceinline__ T uniform_load(const T *p)
+{
+    return *(const __attribute__((address_space(4))) T *)p;
 }
 
 __device__ __forceinline__ float max4(float v)  // over the four lane groups
@@ -132,12 +153,12 @@ __device__ __forceinline__ Request request_of(const AttnArgs &a, int r)
 }
 
 // Where the items lie on the line of units: request r's kv_heads * row blocks
-// items one after the other, each of the request's units.
+// items one after the other, each of the request's units.  The line has fewer
+// than 2^31 units (checked by the launcher).
 struct Item {
     int r, kvh, block;
     Request rq;
-    long long start;  // first unit
-    int units;
+    int start, units;  // first unit, number of units
 };
 
 template <int ROWS>
@@ -146,106 +167,99 @@ __device__ __forceinline__ int row_blocks(const AttnArgs &a, const Request &q)
     return (q.n * (a.heads / a.kv.kv_heads) + ROWS - 1) / ROWS;
 }
 
+// Inclusive prefix sum over a wavefront's lanes.
+__device__ __forceinline__ int wave_scan(int v)
+{
+    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);  // row_shr 1, 2, 4, 8
+    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);  // row_bcast 15, 31
+    v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);
+    return v;
+}
+
 // Up to 64 requests: a lane each, in every wavefront by itself.  More: each
-// thread sums up a run of them, the workgroup scans the runs.
+// lane has a run of requests, in every wavefront again.
 template <int ROWS, int UNIT>
 struct Line {
-    long long total;
     const AttnArgs &a;
-    const long long *runs;  // LDS [ATTN_THREADS + 1]; unused up to 64 requests
-    int per;
-    Request mine;
-    long long before;
+    int total, per, before;
+    Request mine;  // per == 1: the lane's request
 
-    __device__ static long long units_of(const AttnArgs &a, const Request &q)
+    __device__ static int units_of(const AttnArgs &a, const Request &q)
     {
-        return (long long)((q.ctx + q.n + UNIT - 1) / UNIT) * row_blocks<ROWS>(a, q) * a.kv.kv_heads;
+        return (q.ctx + q.n + UNIT - 1) / UNIT * row_blocks<ROWS>(a, q) * a.kv.kv_heads;
     }
 
-    __device__ Line(const AttnArgs &a_, long long *lds, long long *scratch) : a(a_), runs(lds)
+    __device__ explicit Line(const AttnArgs &a_) : a(a_)
     {
-        if (a.R <= 64) {
-            const int lane = threadIdx.x & 63;
-            mine = request_of(a, min(lane, a.R - 1));
-            const long long own = lane < a.R ? units_of(a, mine) : 0;
-            long long sum = own;
-#pragma unroll
-            for (int s = 1; s < 64; s <<= 1) {
-                const long long p = __shfl_up(sum, s);
-                if (lane >= s)
-                    sum += p;
-            }
-            before = sum - own;
-            total = __shfl(sum, 63);
-            return;
-        }
-        per = (a.R + ATTN_THREADS - 1) / ATTN_THREADS;
-        long long units = 0, none = 0, zero;
-        const int r0 = threadIdx.x * per, r1 = min(r0 + per, a.R);
-        for (int r = r0; r < r1; ++r)
-            units += units_of(a, request_of(a, r));
-        scan_pair<ATTN_THREADS>(units, none, total, zero, scratch);
-        lds[threadIdx.x] = units;
-        if (threadIdx.x == 0)
-            lds[ATTN_THREADS] = total;
-        __syncthreads();
+        const int lane = threadIdx.x & 63;
+        per = (a.R + 63) / 64;
+        const int r0 = lane * per, r1 = min(r0 + per, a.R);
+        mine = request_of(a, min(r0, a.R - 1));
+        int own = r0 < a.R ? units_of(a, mine) : 0;
+        for (int r = r0 + 1; r < r1; ++r)
+            own += units_of(a, request_of(a, r));
+        const int sum = wave_scan(own);
+        before = sum - own;
+        total = __builtin_amdgcn_readlane(sum, 63);
     }
 
     // the item that holds unit u (the same in every lane)
-    __device__ Item item_at(long long u) const
+    __device__ Item item_at(int u) const
     {
         Item it;
-        long long base;
-        if (a.R <= 64) {
-            it.r = 63 - __builtin_clzll(__ballot((threadIdx.x & 63) < (unsigned)a.R && before <= u));
-            it.rq.ctx = __builtin_amdgcn_readlane(mine.ctx, it.r);
-            it.rq.n = __builtin_amdgcn_readlane(mine.n, it.r);
-            it.rq.first = __builtin_amdgcn_readlane(mine.first, it.r);
-            base = (long long)(((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(before >> 32), it.r) << 32) |
-                               (uint32_t)__builtin_amdgcn_readlane((int)before, it.r));
-        } else {
-            const int i = owner_of(runs, ATTN_THREADS, u);
-            base = runs[i];
-            for (it.r = i * per;; ++it.r) {
-                it.rq = request_of(a, it.r);
-                const long long all = units_of(a, it.rq);
-                if (u < base + all || it.r + 1 >= a.R)
-                    break;
-                base += all;
-            }
-            it.r = __builtin_amdgcn_readfirstlane(it.r);
-            it.rq.ctx = __builtin_amdgcn_readfirstlane(it.rq.ctx);
-            it.rq.n = __builtin_amdgcn_readfirstlane(it.rq.n);
-            it.rq.first = __builtin_amdgcn_readfirstlane(it.rq.first);
+        const int lane = threadIdx.x & 63;
+        const int run = 63 - __builtin_clzll(__ballot(lane * per < a.R && before <= u));
+        int base = __builtin_amdgcn_readlane(before, run), at = run;
+        it.r = run;
+        Request q = mine;
+        if (per > 1) {
+            // the run's requests, a lane each
+            it.r = run * per;
+            const int n = min(per, a.R - it.r);
+            q = request_of(a, it.r + min(lane, n - 1));
+            const int own = lane < n ? units_of(a, q) : 0, sum = wave_scan(own);
+            at = 63 - __builtin_clzll(__ballot(lane < n && base + sum - own <= u));
+            base += __builtin_amdgcn_readlane(sum - own, at);
+            it.r += at;
         }
+        it.rq.ctx = __builtin_amdgcn_readlane(q.ctx, at);
+        it.rq.n = __builtin_amdgcn_readlane(q.n, at);
+        it.rq.first = __builtin_amdgcn_readlane(q.first, at);
         it.units = (it.rq.ctx + it.rq.n + UNIT - 1) / UNIT;
-        const int blocks = row_blocks<ROWS>(a, it.rq);
-        const uint32_t k = __builtin_amdgcn_readfirstlane((uint32_t)((uint64_t)(u - base) / (uint32_t)it.units));
-        it.start = base + (long long)k * it.units;
-        it.kvh = k / blocks;
-        it.block = k % blocks;
+        const uint32_t blocks = row_blocks<ROWS>(a, it.rq);
+        const uint32_t k = __builtin_amdgcn_readfirstlane((uint32_t)(u - base) / (uint32_t)it.units);
+        it.start = base + (int)k * it.units;
+        it.kvh = __builtin_amdgcn_readfirstlane(k / blocks);
+        it.block = (int)k - it.kvh * (int)blocks;
         return it;
     }
 };
 
 // The line's ranges, none empty: their number, where range i starts, and the
-// range that holds unit u.
-__device__ __forceinline__ int ranges(long long total) { return (int)min(total, (long long)SPLITS); }
-__device__ __forceinline__ long long cut(long long total, int i)
-{
-    return total <= SPLITS ? i : total * i / SPLITS;
-}
-__device__ __forceinline__ int range_of(long long total, long long u)
-{
-    return total <= SPLITS ? (int)u : (int)(((u + 1) * SPLITS - 1) / total);
-}
+// range that holds unit u.  The first `more` ranges have one unit more.
+template <int SPLITS>
+struct Cuts {
+    uint32_t total, each, more;
+    __device__ explicit Cuts(int t) : total(t), each((uint32_t)t / SPLITS), more((uint32_t)t % SPLITS) {}
+    __device__ __forceinline__ int ranges() const { return min((int)total, SPLITS); }
+    __device__ __forceinline__ int start(uint32_t i) const { return (int)(each * i + min(i, more)); }
+    __device__ __forceinline__ int holder(uint32_t u) const
+    {
+        const uint32_t longer = more * (each + 1);
+        return (int)(u < longer ? u / (each + 1) : more + (u - longer) / each);
+    }
+};
 
-// The workspace: what the join of cut i has to do (parts 0: nothing; the first
-// cut that divides an item does it), then the parts -- the range's own part
-// 2 i for its first segment, 2 i + 1 for another (only its last can be divided
-// too).
+// The workspace: the joins of divided items, then the parts -- range i's own
+// part 2 i for its first segment, 2 i + 1 for another (only its last can be
+// divided too).  A join is written by the range in which its item begins: as
+// entry i by range i (at most one divided item begins in a range), or, where the
+// call has few items (a.by_item), as the item's entry, by number.
 struct Join {
-    int parts, range, second;  // parts of the item, the first one's range and whether it is its second
+    int parts, range, second;  // parts (0: nothing to do), the first one's range and whether it is its second
     int rows, row0, first, kvh;
     int unused;
 };
@@ -256,34 +270,37 @@ struct Part {
     float m[ROWS], l[ROWS];
 };
 
-template <int ROWS, int DP>
+template <int ROWS, int DP, int SPLITS>
 struct Workspace {
     Join join[SPLITS];
     Part<ROWS, DP> part[2 * SPLITS];
 };
 
-// Start of a workgroup's segment: its item, its positions, and, at the range's
-// start, the join that its cut asks for.
-template <int ROWS, int UNIT>
-__device__ __forceinline__ Item open_segment(const Line<ROWS, UNIT> &line, long long u, long long u0, Join *join,
-                                             const AttnArgs &a)
+template <int ROWS>
+__device__ __forceinline__ int most_blocks(const AttnArgs &a)
 {
-    const Item it = line.item_at(u);
-    if (u == u0 && threadIdx.x == 0) {
-        Join j = {};
-        const int i = blockIdx.x;
-        if (i > 0 && u > it.start && cut(line.total, i - 1) <= it.start) {
-            j.range = range_of(line.total, it.start);
-            j.parts = range_of(line.total, it.start + it.units - 1) - j.range + 1;
-            j.second = cut(line.total, j.range) < it.start;
-            j.row0 = it.block * ROWS;
-            j.rows = min(it.rq.n * (a.heads / a.kv.kv_heads) - j.row0, ROWS);
-            j.first = it.rq.first;
-            j.kvh = it.kvh;
-        }
-        join[i] = j;
+    return (a.max_new * (a.heads / a.kv.kv_heads) + ROWS - 1) / ROWS;
+}
+
+// End of a workgroup's segment [u, stop) of an item (called by one thread).
+template <int ROWS, int SPLITS>
+__device__ __forceinline__ void note_join(const AttnArgs &a, const Cuts<SPLITS> &cuts, const Item &it, int u, int stop,
+                                          int u0, int u1, Join *join)
+{
+    const bool begins = u == it.start, divided = begins && stop < it.start + it.units;
+    if (a.by_item ? !begins : stop < u1)
+        return;
+    Join j = {};
+    if (divided) {
+        j.range = blockIdx.x;
+        j.parts = cuts.holder(it.start + it.units - 1) - j.range + 1;
+        j.second = u != u0;
+        j.row0 = it.block * ROWS;
+        j.rows = min(it.rq.n * (a.heads / a.kv.kv_heads) - j.row0, ROWS);
+        j.first = it.rq.first;
+        j.kvh = it.kvh;
     }
-    return it;
+    join[a.by_item ? (it.r * a.kv.kv_heads + it.kvh) * most_blocks<ROWS>(a) + it.block : blockIdx.x] = j;
 }
 
 __device__ __forceinline__ uint16_t *out_row(const AttnArgs &a, int first, int kvh, int row, int group)
@@ -301,19 +318,39 @@ __device__ __forceinline__ float inverse(float total)  // 0 for a row that saw n
 // one tile
 // ---------------------------------------------------------------------------
 
-// A wavefront's 16 NT rows, c of each sixteen in lanes (c, *).
-template <int DP, int DS, int NT, bool BF>
+// A wavefront's 16 NT rows, c of each sixteen in lanes (c, *).  Output element
+// i of operand row 4 g + i of product q is element d(q, i) of the head: DV (4 g
+// + i) + q, or, where the values came transposed out of LDS, 16 q + 4 g + i.
+template <int DP, int DS, int NT, bool BF, bool TRANSPOSED>
 struct Rows {
     static constexpr int DV = DP / 16;
     v4u q[NT][DS];
     uint64_t mask[NT];
-    v4f acc[NT][DV];
-    float m[NT], l[NT];
+    v4f acc[NT][DV], sum[NT];  // sum: every element is the lane's row's sum of weights
+    float m[NT];
     float scale2;
 
-    // rows row0 .. row0 + rows - 1 of the item; the scale's sign goes into Q,
-    // and a scale of zero too, so that masked scores stay -infinity
-    __device__ __forceinline__ void open(const AttnArgs &a, const Item &it, int row0, int rows, int group)
+    // Rows row0 .. row0 + rows - 1 of the item: begin() sends the loads off,
+    // without a branch (past the end, a piece that is there is read), and
+    // finish() drops what is past the end.
+    __device__ __forceinline__ void begin(const AttnArgs &a, const Item &it, int row0, int rows, int group)
+    {
+        const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4, pieces = a.kv.head_dim / 8;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            const int row = 16 * nt + c < rows ? row0 + 16 * nt + c : row0;
+            const int tok = it.rq.first + row / group, head = it.kvh * group + row % group;
+            const uint16_t *p = (const uint16_t *)a.q + tok * a.q_token_stride + head * a.q_head_stride;
+            mask[nt] = a.tree_mask[tok];
+#pragma unroll
+            for (int s = 0; s < DS; ++s)
+                q[nt][s] = *(const v4u *)(p + 8 * (4 * s + g < pieces ? 4 * s + g : 0));
+        }
+    }
+
+    // The scale's sign goes into Q, and a scale of zero too, so that masked
+    // scores stay -infinity.
+    __device__ __forceinline__ void finish(const AttnArgs &a, int rows)
     {
         const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4, pieces = a.kv.head_dim / 8;
         const uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u, keep = a.scale == 0.f ? 0u : ~0u;
@@ -321,19 +358,12 @@ struct Rows {
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
             const bool ok = 16 * nt + c < rows;
-            const int row = ok ? row0 + 16 * nt + c : row0;
-            const int tok = it.rq.first + row / group, head = it.kvh * group + row % group;
-            const uint16_t *p = (const uint16_t *)a.q + tok * a.q_token_stride + head * a.q_head_stride;
-            mask[nt] = ok ? a.tree_mask[tok] : 0;
+            mask[nt] = ok ? mask[nt] : 0;
 #pragma unroll
-            for (int s = 0; s < DS; ++s) {
-                const int piece = 4 * s + g;
-                q[nt][s] = v4u{0, 0, 0, 0};
-                if (ok && piece < pieces)
-                    q[nt][s] = (*(const v4u *)(p + 8 * piece) ^ flip) & keep;
-            }
+            for (int s = 0; s < DS; ++s)
+                q[nt][s] = (q[nt][s] ^ flip) & (ok && 4 * s + g < pieces ? keep : 0u);
             m[nt] = NO_SCORE;
-            l[nt] = 0.f;
+            sum[nt] = v4f{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int i = 0; i < DV; ++i)
                 acc[nt][i] = v4f{0.f, 0.f, 0.f, 0.f};
@@ -353,62 +383,86 @@ struct Rows {
             }
     }
 
-    // Masks the tile at p0: scores of what a row does not see, and the values
-    // of positions that are not there.  True where values of the step's own
-    // tokens are not finite (the same in every lane).
-    __device__ __forceinline__ bool hide(int p0, bool ok0, bool ok1, const Request &rq, v4f (&s)[NT][2],
-                                         uint32_t (&v)[8][DV / 2])
+    // hides the scores of the tile at p0 that a row does not see
+    __device__ __forceinline__ void hide(int p0, bool ok0, bool ok1, const Request &rq, v4f (&s)[NT][2])
     {
         const int g = (threadIdx.x & 63) >> 4;
-        bool odd_values = false;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            const int p = p0 + 16 * (e / 4) + 4 * g + e % 4, j = p - rq.ctx;
-            const bool there = j < rq.n && (e / 4 ? ok1 : ok0);
-            bool odd = false;
-#pragma unroll
-            for (int i = 0; i < DV / 2; ++i) {
-                if (!there)
-                    v[e][i] = 0;
-                odd |= not_finite<BF>(v[e][i]);
-            }
-            odd_values |= odd && j >= 0;
+            const int j = p0 + 16 * (e / 4) + 4 * g + e % 4 - rq.ctx;
+            const bool there = (j < rq.n) & (e / 4 ? ok1 : ok0);
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
-                const bool seen = there && (j < 0 || ((mask[nt] >> (j & 63)) & 1));
-                if (!seen)
-                    s[nt][e / 4][e % 4] = -INFINITY;
+                const bool seen = there & ((j < 0) | (((mask[nt] >> (j & 63)) & 1) != 0));
+                s[nt][e / 4][e % 4] = seen ? s[nt][e / 4][e % 4] : -INFINITY;
             }
         }
-        return __ballot(odd_values) != 0;
     }
 
-    // weights of the tile, as the products' operand
+    __device__ __forceinline__ void form(const v4f (&s)[2], float top, v4u &pf)
+    {
+        float x[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            x[e] = fast_exp2(fmaf(s[e / 4][e % 4], scale2, -top));
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            pf[i] = pack2<BF>(x[2 * i], x[2 * i + 1]);
+    }
+
+    // Weights of the tile, as the products' operand.  They are formed with the
+    // maximum so far; only where one exceeds 2^GAP (compared as integers, two at
+    // a time: they are not negative) is the maximum moved and the tile done again.
     __device__ __forceinline__ void weights(const v4f (&s)[NT][2], v4u (&pf)[NT])
     {
+        typedef uint16_t v2s __attribute__((ext_vector_type(2)));
+        constexpr uint32_t LIMIT = BF ? 0x43804380u : 0x5c005c00u;  // 2^GAP, twice
+        const v2s limit = __builtin_bit_cast(v2s, LIMIT);
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-            float top = fmaxf(fmaxf(fmaxf(s[nt][0][0], s[nt][0][1]), fmaxf(s[nt][0][2], s[nt][0][3])),
-                              fmaxf(fmaxf(s[nt][1][0], s[nt][1][1]), fmaxf(s[nt][1][2], s[nt][1][3])));
-            top *= scale2;
-            if (__ballot(top > m[nt] + GAP)) {
-                top = fmaxf(max4(top), m[nt]);
+            form(s[nt], m[nt], pf[nt]);
+            v2s most = limit;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                most = __builtin_elementwise_max(most, __builtin_bit_cast(v2s, (uint32_t)pf[nt][i]));
+            if (__ballot(__builtin_bit_cast(uint32_t, most) != LIMIT)) {
+                float top = fmaxf(fmaxf(fmaxf(s[nt][0][0], s[nt][0][1]), fmaxf(s[nt][0][2], s[nt][0][3])),
+                                  fmaxf(fmaxf(s[nt][1][0], s[nt][1][1]), fmaxf(s[nt][1][2], s[nt][1][3])));
+                top = fmaxf(max4(top * scale2), m[nt]);
                 const float keep = fast_exp2(m[nt] - top);
                 m[nt] = top;
-                l[nt] *= keep;
+                sum[nt] *= keep;
 #pragma unroll
                 for (int i = 0; i < DV; ++i)
                     acc[nt][i] *= keep;
+                form(s[nt], top, pf[nt]);
             }
-            float x[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                x[e] = fast_exp2(fmaf(s[nt][e / 4][e % 4], scale2, -m[nt]));
-            l[nt] += ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                pf[nt][i] = pack2<BF>(x[2 * i], x[2 * i + 1]);
         }
+    }
+
+    // The values of positions that are not there become 0.  True where values
+    // of the step's own tokens are not finite (the same in every lane).
+    __device__ __forceinline__ bool hide_values(int p0, bool ok0, bool ok1, const Request &rq, v4u (&v)[DV])
+    {
+        const int g = (threadIdx.x & 63) >> 4;
+        bool odd = false;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            uint32_t there = 0, own = 0;
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const int e = 2 * w + k, j = p0 + 16 * (e / 4) + 4 * g + e % 4 - rq.ctx;
+                const uint32_t half = k ? 0xffff0000u : 0xffffu;
+                there |= (j < rq.n) & (e / 4 ? ok1 : ok0) ? half : 0;
+                own |= j >= 0 ? half : 0;
+            }
+#pragma unroll
+            for (int i = 0; i < DV; ++i) {
+                v[i][w] &= there;
+                odd |= not_finite<BF>(v[i][w] & own);
+            }
+        }
+        return __ballot(odd) != 0;
     }
 
     // Values of the step's own tokens that are not finite: their products are
@@ -416,7 +470,7 @@ struct Rows {
     // in the operand.  value(p): position p's values.
     template <typename F>
     __device__ __forceinline__ void odd_products(int p0, bool ok0, bool ok1, const AttnArgs &a, const Request &rq,
-                                                 const v4u (&pf)[NT], uint32_t (&v)[8][DV / 2], F value)
+                                                 const v4u (&pf)[NT], v4u (&v)[DV], F value)
     {
         const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
 #pragma unroll 1
@@ -435,17 +489,28 @@ struct Rows {
                                                     : pf[nt][3];
                     const float weight = unpack<BF>(__shfl(w, 16 * gg + c), e & 1);
                     const bool seen = (mask[nt] >> j) & 1;
+                    auto term = [&](uint32_t bits) {
+                        return seen & not_finite<BF>(bits) ? weight * unpack<BF>(bits, 0) : 0.f;
+                    };
+                    if constexpr (TRANSPOSED) {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int d = DV * (4 * g + i);
-                        if (d >= a.kv.head_dim)
-                            continue;
-                        const Halves<DV> piece = *(const Halves<DV> *)(row + d);
+                        for (int i = 0; i < DV; ++i) {
+                            if (16 * i + 4 * g >= a.kv.head_dim)
+                                continue;
+                            const Halves<4> piece = *(const Halves<4> *)(row + 16 * i + 4 * g);
 #pragma unroll
-                        for (int q = 0; q < DV; ++q) {
-                            const uint32_t bits = q & 1 ? piece.w[q / 2] >> 16 : piece.w[q / 2] & 0xffffu;
-                            if (seen && not_finite<BF>(bits))
-                                acc[nt][q][i] += weight * unpack<BF>(bits, 0);
+                            for (int k = 0; k < 4; ++k)
+                                acc[nt][i][k] += term(k & 1 ? piece.w[k / 2] >> 16 : piece.w[k / 2] & 0xffffu);
+                        }
+                    } else {
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            if (DV * (4 * g + k) >= a.kv.head_dim)
+                                continue;
+                            const Halves<DV> piece = *(const Halves<DV> *)(row + DV * (4 * g + k));
+#pragma unroll
+                            for (int i = 0; i < DV; ++i)
+                                acc[nt][i][k] += term(i & 1 ? piece.w[i / 2] >> 16 : piece.w[i / 2] & 0xffffu);
                         }
                     }
                 }
@@ -454,34 +519,25 @@ struct Rows {
         for (int e = 0; e < 8; ++e) {
             if (p0 + 16 * (e / 4) + 4 * g + e % 4 < rq.ctx)
                 continue;
+            const uint32_t half = e & 1 ? 0xffff0000u : 0xffffu;
 #pragma unroll
-            for (int i = 0; i < DV / 2; ++i) {
-                if (not_finite<BF>(v[e][i] & 0xffffu))
-                    v[e][i] &= 0xffff0000u;
-                if (not_finite<BF>(v[e][i] >> 16))
-                    v[e][i] &= 0xffffu;
-            }
+            for (int i = 0; i < DV; ++i)
+                if (not_finite<BF>(v[i][e / 2] & half))
+                    v[i][e / 2] &= ~half;
         }
     }
 
-    __device__ __forceinline__ void products(const v4u (&pf)[NT], const uint32_t (&v)[8][DV / 2])
+    __device__ __forceinline__ void products(const v4u (&pf)[NT], const v4u (&v)[DV])
     {
+        constexpr uint32_t ONE = BF ? 0x3f803f80u : 0x3c003c00u;
 #pragma unroll
-        for (int i = 0; i < DV; ++i) {
-            v4u vf;
+        for (int nt = 0; nt < NT; ++nt)
+            sum[nt] = mfma<BF>(v4u{ONE, ONE, ONE, ONE}, pf[nt], sum[nt]);
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                vf[e] = __builtin_amdgcn_perm(v[2 * e + 1][i / 2], v[2 * e][i / 2], i & 1 ? 0x07060302u : 0x05040100u);
+        for (int i = 0; i < DV; ++i)
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
-                acc[nt][i] = mfma<BF>(vf, pf[nt], acc[nt][i]);
-        }
-    }
-
-    __device__ __forceinline__ float row_sum(int nt) const
-    {
-        float t = l[nt] + __shfl_xor(l[nt], 16);
-        return t + __shfl_xor(t, 32);
+                acc[nt][i] = mfma<BF>(v[i], pf[nt], acc[nt][i]);
     }
 };
 
@@ -499,8 +555,8 @@ __device__ __forceinline__ const char *at_page(const void *base, int page, int p
 __device__ __forceinline__ int page_at(const AttnArgs &a, const int32_t *table, int p, int end, int page_shift)
 {
     p = __builtin_amdgcn_readfirstlane(p);
-    const int id = p < end ? table[p >> page_shift] : -1;
-    return __builtin_amdgcn_readfirstlane(id < a.kv.n_pages ? max(id, -1) : -1);
+    const int id = uniform_load(table + (min(p, end - 1) >> page_shift));
+    return p < end && id < a.kv.n_pages ? max(id, -1) : -1;
 }
 
 // ---------------------------------------------------------------------------
@@ -508,38 +564,38 @@ __device__ __forceinline__ int page_at(const AttnArgs &a, const int32_t *table, 
 // ---------------------------------------------------------------------------
 
 // DP: padded head size, DS: 32-element steps of it that hold elements, NT:
-// 16-row tiles per item, BF: bfloat16.
-template <int DP, int DS, int NT, bool BF>
-__global__ void __launch_bounds__(ATTN_THREADS, 2) attn_rows_kernel(AttnArgs a)
+// 16-row tiles per item, BF: bfloat16, WGS: workgroups a CU.
+template <int DP, int DS, int NT, bool BF, int WGS>
+__global__ void __launch_bounds__(ATTN_THREADS, WGS) attn_rows_kernel(AttnArgs a)
 {
-    constexpr int DV = DP / 16, ROWS = 16 * NT, UNIT = ATTN_WAVES * TILE;
+    constexpr int DV = DP / 16, ROWS = 16 * NT, UNIT = ATTN_WAVES * TILE, SPLITS = WGS * CUS;
     __shared__ float lds_o[ATTN_WAVES][ROWS][DP + 4];
     __shared__ float lds_m[ATTN_WAVES][ROWS], lds_l[ATTN_WAVES][ROWS];
-    __shared__ long long runs[ATTN_THREADS + 1], scratch[2 * ATTN_WAVES];
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int c = lane & 15, g = lane >> 4;
     const int group = a.heads / a.kv.kv_heads;
     const int D = a.kv.head_dim, pieces = D / 8;
     const int page_shift = __builtin_ctz(a.kv.page_size);
-    Workspace<ROWS, DP> &ws = *(Workspace<ROWS, DP> *)a.workspace;
-    const Line<ROWS, UNIT> line(a, runs, scratch);
-    if ((int)blockIdx.x >= ranges(line.total)) {
-        if (threadIdx.x == 0)
+    Workspace<ROWS, DP, SPLITS> &ws = *(Workspace<ROWS, DP, SPLITS> *)a.workspace;
+    const Line<ROWS, UNIT> line(a);
+    const Cuts<SPLITS> cuts(line.total);
+    if ((int)blockIdx.x >= cuts.ranges()) {
+        if (!a.by_item && threadIdx.x == 0)
             ws.join[blockIdx.x].parts = 0;
         return;
     }
-    const long long u0 = cut(line.total, blockIdx.x), u1 = cut(line.total, blockIdx.x + 1);
+    const int u0 = cuts.start(blockIdx.x), u1 = cuts.start(blockIdx.x + 1);
     const uint32_t k_step = 2 * (uint32_t)a.kv.k_token_stride, v_step = 2 * (uint32_t)a.kv.v_token_stride;
     const uint32_t k_lane = c * k_step, v_lane = 4 * g * v_step + 2 * (DV * c < D ? DV * c : 0);
 
-    for (long long u = u0; u < u1;) {
-        const Item it = open_segment(line, u, u0, ws.join, a);
+    for (int u = u0; u < u1;) {
+        const Item it = line.item_at(u);
         const Request &rq = it.rq;
         const int row0 = it.block * ROWS, rows = min(rq.n * group - row0, ROWS), end = rq.ctx + rq.n;
-        const long long stop = min(u1, it.start + it.units);
+        const int stop = min(u1, it.start + it.units);
         const bool whole = u == it.start && stop == it.start + it.units;
-        const int first = (int)(u - it.start) * UNIT + wave * TILE, last = min((int)(stop - it.start) * UNIT, end);
+        const int first = (u - it.start) * UNIT + wave * TILE, last = min((stop - it.start) * UNIT, end);
         const int32_t *table = a.page_table + it.r * a.table_stride;
         const uint16_t *kb = (const uint16_t *)a.kv.k + it.kvh * a.kv.k_head_stride;
         const uint16_t *vb = (const uint16_t *)a.kv.v + it.kvh * a.kv.v_head_stride;
@@ -570,51 +626,61 @@ __global__ void __launch_bounds__(ATTN_THREADS, 2) attn_rows_kernel(AttnArgs a)
                 }
             }
         };
-        int page[2], next[2];
+        int page[2], next[2], after[2];
         auto pages_of = [&](int p0, int *id) {
             id[0] = page_at(a, table, p0, end, page_shift);
             id[1] = page_at(a, table, p0 + 16, end, page_shift);
         };
-        if (first < last) {
-            pages_of(first, page);
-            load_k(first, page);
-            load_v(first, page);
-        }
-        Rows<DP, DS, NT, BF> row;
-        row.open(a, it, row0, rows, group);
+        // a tile past the segment's end is the one before it once more
+        auto next_tile = [&](int p0) { return p0 + UNIT < last ? p0 + UNIT : p0; };
+        Rows<DP, DS, NT, BF, false> row;
+        row.begin(a, it, row0, rows, group);
+        // (a wavefront without a tile loads one too)
+        const int start = min(first, (last - 1) & ~(TILE - 1));
+        pages_of(start, page);
+        pages_of(next_tile(start), next);
+        load_k(start, page);
+        load_v(start, page);
+        row.finish(a, rows);
         for (int p0 = first; p0 < last; p0 += UNIT) {
-            const bool more = p0 + UNIT < last;
-            if (more)
-                pages_of(p0 + UNIT, next);
+            // no branch around the loads, so that their counters stay exact: the
+            // last tile is loaded once more, from L2, and not used
+            const int pn = next_tile(p0);
+            pages_of(next_tile(pn), after);
             v4f s[NT][2];
             row.scores(kf, s);
-            if (more)
-                load_k(p0 + UNIT, next);
-            bool odd = false;
-            if (p0 + TILE > rq.ctx || (page[0] | page[1]) < 0)
-                odd = row.hide(p0, page[0] >= 0, page[1] >= 0, rq, s, vr);
-            v4u pf[NT];
+            load_k(pn, next);
+            const bool masked = p0 + TILE > rq.ctx || (page[0] | page[1]) < 0;
+            if (masked)
+                row.hide(p0, page[0] >= 0, page[1] >= 0, rq, s);
+            v4u pf[NT], vf[DV];
             row.weights(s, pf);
-            if (odd)
-                row.odd_products(p0, page[0] >= 0, page[1] >= 0, a, rq, pf, vr, [&](int p) {
+#pragma unroll
+            for (int i = 0; i < DV; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    vf[i][e] = __builtin_amdgcn_perm(vr[2 * e + 1][i / 2], vr[2 * e][i / 2],
+                                                     i & 1 ? 0x07060302u : 0x05040100u);
+            if (__builtin_expect(masked && row.hide_values(p0, page[0] >= 0, page[1] >= 0, rq, vf), 0))
+                row.odd_products(p0, page[0] >= 0, page[1] >= 0, a, rq, pf, vf, [&](int p) {
                     const int id = p - p0 < 16 ? page[0] : page[1];
                     return (const uint16_t *)at_page(vb, id, p, a.kv.page_size, a.kv.v_page_stride, v_step);
                 });
-            row.products(pf, vr);
-            if (more) {
-                load_v(p0 + UNIT, next);
-                page[0] = next[0];
-                page[1] = next[1];
+            row.products(pf, vf);
+            load_v(pn, next);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                page[h] = next[h];
+                next[h] = after[h];
             }
         }
 
         // the wavefronts' parts meet in LDS
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-            const float l = row.row_sum(nt);
             if (g == 0) {
                 lds_m[wave][16 * nt + c] = row.m[nt];
-                lds_l[wave][16 * nt + c] = l;
+                lds_l[wave][16 * nt + c] = row.sum[nt][0];
             }
 #pragma unroll
             for (int i = 0; i < 4; ++i)
@@ -623,6 +689,8 @@ __global__ void __launch_bounds__(ATTN_THREADS, 2) attn_rows_kernel(AttnArgs a)
                     lds_o[wave][16 * nt + c][DV * (4 * g + i) + q] = row.acc[nt][q][i];
         }
         __syncthreads();
+        if (threadIdx.x == 0)
+            note_join<ROWS>(a, cuts, it, u, stop, u0, u1, ws.join);
         Part<ROWS, DP> &part = ws.part[2 * blockIdx.x + (u != u0)];
         for (int i = wave; i < rows; i += ATTN_WAVES) {
             float top = NO_SCORE;
@@ -663,29 +731,29 @@ __global__ void __launch_bounds__(ATTN_THREADS, 2) attn_rows_kernel(AttnArgs a)
 // items of many rows
 // ---------------------------------------------------------------------------
 
-template <int DP, int DS, int NT, bool BF>
-__global__ void __launch_bounds__(ATTN_THREADS, 2) attn_block_kernel(AttnArgs a)
+template <int DP, int DS, int NT, bool BF, int WGS>
+__global__ void __launch_bounds__(ATTN_THREADS, WGS) attn_block_kernel(AttnArgs a)
 {
-    constexpr int DV = DP / 16, WROWS = 16 * NT, ROWS = WROWS * ATTN_WAVES, UNIT = 64;
+    constexpr int DV = DP / 16, WROWS = 16 * NT, ROWS = WROWS * ATTN_WAVES, UNIT = 64, SPLITS = WGS * CUS;
     constexpr int PIECES = DP / 8;         // 16-byte pieces of a stored row
     constexpr int LOADS = UNIT * PIECES / ATTN_THREADS;  // per thread, of keys and of values
     constexpr int LOAD_ROWS = 64 / PIECES; // rows that one load of a wavefront covers
     __shared__ v4u tile[2][2][UNIT][PIECES];  // [buffer][keys, values][position][piece, permuted]
-    __shared__ long long runs[ATTN_THREADS + 1], scratch[2 * ATTN_WAVES];
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int c = lane & 15, g = lane >> 4;
     const int group = a.heads / a.kv.kv_heads;
     const int D = a.kv.head_dim, pieces = D / 8;
     const int page_shift = __builtin_ctz(a.kv.page_size);
-    Workspace<ROWS, DP> &ws = *(Workspace<ROWS, DP> *)a.workspace;
-    const Line<ROWS, UNIT> line(a, runs, scratch);
-    if ((int)blockIdx.x >= ranges(line.total)) {
-        if (threadIdx.x == 0)
+    Workspace<ROWS, DP, SPLITS> &ws = *(Workspace<ROWS, DP, SPLITS> *)a.workspace;
+    const Line<ROWS, UNIT> line(a);
+    const Cuts<SPLITS> cuts(line.total);
+    if ((int)blockIdx.x >= cuts.ranges()) {
+        if (!a.by_item && threadIdx.x == 0)
             ws.join[blockIdx.x].parts = 0;
         return;
     }
-    const long long u0 = cut(line.total, blockIdx.x), u1 = cut(line.total, blockIdx.x + 1);
+    const int u0 = cuts.start(blockIdx.x), u1 = cuts.start(blockIdx.x + 1);
     const uint32_t k_step = 2 * (uint32_t)a.kv.k_token_stride, v_step = 2 * (uint32_t)a.kv.v_token_stride;
 
     // Piece j of stored row r lies at j ^ swap(r): sixteen lanes that read one
@@ -698,14 +766,23 @@ __global__ void __launch_bounds__(ATTN_THREADS, 2) attn_block_kernel(AttnArgs a)
     const int from = load_piece < pieces ? load_piece : 0;
     const uint32_t k_lane = load_row * k_step + 16 * from, v_lane = load_row * v_step + 16 * from;
 
-    for (long long u = u0; u < u1;) {
-        const Item it = open_segment(line, u, u0, ws.join, a);
+    // Where lane (c, g) reads its operands in a stored tile: keys, piece 4 s + g
+    // of row c (and 16 + c); values, transposed, elements 16 i + 4 (c % 4) .. of
+    // row 4 g + c / 4 (and 16 + that) -- row and swap are the same for both
+    // halves, and s and i only move the piece.
+    constexpr int ROW_BYTES = 16 * PIECES;
+    const int v_row = 4 * g + c / 4;
+    const uint32_t k_read = c * ROW_BYTES + 16 * (g ^ swap(c));
+    const uint32_t v_read = v_row * ROW_BYTES + 16 * (((c & 3) >> 1) ^ swap(v_row)) + 8 * (c & 1);
+
+    for (int u = u0; u < u1;) {
+        const Item it = line.item_at(u);
         const Request &rq = it.rq;
         const int row0 = it.block * ROWS + wave * WROWS, rows = min(max(rq.n * group - row0, 0), WROWS);
         const int end = rq.ctx + rq.n;
-        const long long stop = min(u1, it.start + it.units);
+        const int stop = min(u1, it.start + it.units);
         const bool whole = u == it.start && stop == it.start + it.units;
-        const int first = (int)(u - it.start) * UNIT, last = min((int)(stop - it.start) * UNIT, end);
+        const int first = (u - it.start) * UNIT, last = min((stop - it.start) * UNIT, end);
         const int32_t *table = a.page_table + it.r * a.table_stride;
         const uint16_t *kb = (const uint16_t *)a.kv.k + it.kvh * a.kv.k_head_stride;
         const uint16_t *vb = (const uint16_t *)a.kv.v + it.kvh * a.kv.v_head_stride;
@@ -738,9 +815,10 @@ __global__ void __launch_bounds__(ATTN_THREADS, 2) attn_block_kernel(AttnArgs a)
             }
         };
 
+        Rows<DP, DS, NT, BF, true> row;
+        row.begin(a, it, rows ? row0 : it.block * ROWS, rows, group);
         int there = load(first), coming = 0;
-        Rows<DP, DS, NT, BF> row;
-        row.open(a, it, rows ? row0 : it.block * ROWS, rows, group);
+        row.finish(a, rows);
         store(0);
         if (first + UNIT < last)
             coming = load(first + UNIT);
@@ -752,38 +830,34 @@ __global__ void __launch_bounds__(ATTN_THREADS, 2) attn_block_kernel(AttnArgs a)
                 const int pt = p0 + t * TILE;
                 if (pt >= end || rows == 0)
                     continue;
+                const char *keys = (const char *)tile[buffer][0][t * TILE], *values = (const char *)tile[buffer][1][t * TILE];
                 v4u kf[2][DS];
 #pragma unroll
                 for (int h = 0; h < 2; ++h)
 #pragma unroll
-                    for (int s = 0; s < DS; ++s) {
-                        const int r = t * TILE + 16 * h + c;
-                        kf[h][s] = tile[buffer][0][r][(4 * s + g) ^ swap(r)];
-                    }
+                    for (int s = 0; s < DS; ++s)
+                        kf[h][s] = *(const v4u *)(keys + 16 * h * ROW_BYTES + (k_read ^ (64 * s)));
                 v4f s[NT][2];
                 row.scores(kf, s);
-                uint32_t vr[8][DV / 2];
+                v4u vf[DV];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const int r = t * TILE + 16 * (e / 4) + 4 * g + e % 4;
-                    const char *p = (const char *)tile[buffer][1][r];
-                    const Halves<DV> v = *(const Halves<DV> *)(p + 16 * ((DV * c / 8) ^ swap(r)) + 2 * (DV * c % 8));
-#pragma unroll
-                    for (int i = 0; i < DV / 2; ++i)
-                        vr[e][i] = v.w[i];
+                for (int i = 0; i < DV; ++i) {
+                    const v2u lo = read_transposed(values + (v_read ^ (32 * i)));
+                    const v2u hi = read_transposed(values + 16 * ROW_BYTES + (v_read ^ (32 * i)));
+                    vf[i] = v4u{lo[0], lo[1], hi[0], hi[1]};
                 }
                 const bool ok0 = (there >> (2 * t)) & 1, ok1 = (there >> (2 * t + 1)) & 1;
-                bool odd = false;
-                if (pt + TILE > rq.ctx || !ok0 || !ok1)
-                    odd = row.hide(pt, ok0, ok1, rq, s, vr);
+                const bool masked = pt + TILE > rq.ctx || !ok0 || !ok1;
+                if (masked)
+                    row.hide(pt, ok0, ok1, rq, s);
                 v4u pf[NT];
                 row.weights(s, pf);
-                if (odd)
-                    row.odd_products(pt, ok0, ok1, a, rq, pf, vr, [&](int p) {
+                if (__builtin_expect(masked && row.hide_values(pt, ok0, ok1, rq, vf), 0))
+                    row.odd_products(pt, ok0, ok1, a, rq, pf, vf, [&](int p) {
                         return (const uint16_t *)at_page(vb, table[p >> page_shift], p, a.kv.page_size,
                                                          a.kv.v_page_stride, v_step);
                     });
-                row.products(pf, vr);
+                row.products(pf, vf);
             }
             if (p0 + UNIT < last) {
                 // the other buffer was last read before the barrier at the end
@@ -797,10 +871,12 @@ __global__ void __launch_bounds__(ATTN_THREADS, 2) attn_block_kernel(AttnArgs a)
             __syncthreads();
         }
 
+        if (threadIdx.x == 0)
+            note_join<ROWS>(a, cuts, it, u, stop, u0, u1, ws.join);
         Part<ROWS, DP> &part = ws.part[2 * blockIdx.x + (u != u0)];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-            const float total = row.row_sum(nt), inv = inverse(total);
+            const float total = row.sum[nt][0], inv = inverse(total);
             const int i = 16 * nt + c;
             if (i >= rows)
                 continue;
@@ -810,22 +886,16 @@ __global__ void __launch_bounds__(ATTN_THREADS, 2) attn_block_kernel(AttnArgs a)
             }
             uint16_t *out = out_row(a, rq.first, it.kvh, row0 + i, group);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int d = DV * (4 * g + j);
+            for (int q = 0; q < DV; ++q) {
+                const int d = 16 * q + 4 * g;
                 if (d >= D)
                     continue;
-                if (whole) {
-                    Halves<DV> o;
-#pragma unroll
-                    for (int q = 0; q < DV; q += 2)
-                        o.w[q / 2] = pack2<BF>(row.acc[nt][q][j] * inv, row.acc[nt][q + 1][j] * inv);
-                    *(Halves<DV> *)(out + d) = o;
-                } else {
-#pragma unroll
-                    for (int q = 0; q < DV; q += 4)
-                        *(v4f *)&part.o[wave * WROWS + i][d + q] = v4f{row.acc[nt][q][j], row.acc[nt][q + 1][j],
-                                                                       row.acc[nt][q + 2][j], row.acc[nt][q + 3][j]};
-                }
+                const v4f o = row.acc[nt][q];
+                if (whole)
+                    *(Halves<4> *)(out + d) = Halves<4>{pack2<BF>(o[0] * inv, o[1] * inv),
+                                                        pack2<BF>(o[2] * inv, o[3] * inv)};
+                else
+                    *(v4f *)&part.o[wave * WROWS + i][d] = o;
             }
         }
         u = stop;
@@ -836,79 +906,120 @@ __global__ void __launch_bounds__(ATTN_THREADS, 2) attn_block_kernel(AttnArgs a)
 // the join
 // ---------------------------------------------------------------------------
 
-constexpr int JOIN_ROWS = 4, JOIN_WAVES = 4, JOIN_THREADS = 64 * JOIN_WAVES, JOIN_GROUPS = 8;
+constexpr int JOIN_WAVES = 4, JOIN_THREADS = 64 * JOIN_WAVES, JOIN_AHEAD = 4;
 
-// Joins the parts of a divided item: workgroup (i, y) takes rows JOIN_ROWS y ..
-// (and on, JOIN_GROUPS apart) of the item that cut i + 1 divides first.
-// Wavefront w first works out the factors of row w's parts, a part a lane;
-// then the wavefronts share the parts of all rows among them, so that many
-// loads are in flight, and meet in LDS.
-template <int DP, int ROWS, bool BF>
+// Joins the parts of a divided item: workgroup (i, y) takes JR rows of join i.
+// Its wavefronts share the parts and meet in LDS.  The first parts' sums are
+// loaded together with the maxima, so that one latency covers both; a CU brings
+// in no more than some ten bytes a cycle from other XCDs' results, so the rows
+// are spread over as many workgroups as is useful.
+template <int DP, int ROWS, bool BF, int SPLITS, int JR>
 __global__ void __launch_bounds__(JOIN_THREADS) attn_join_kernel(AttnArgs a)
 {
-    static_assert(JOIN_ROWS == JOIN_WAVES && ROWS % JOIN_ROWS == 0, "a row's factors per wavefront");
-    __shared__ float factor[SPLITS][JOIN_ROWS], total[JOIN_ROWS];
-    __shared__ float2 sum[JOIN_WAVES][JOIN_ROWS][64];
-    const Workspace<ROWS, DP> &ws = *(const Workspace<ROWS, DP> *)a.workspace;
-    const Join j = ws.join[blockIdx.x + 1];
-    if (j.parts == 0)
+    static_assert(ROWS % JR == 0 && (JR == 1 || JR == 4), "whole row groups");
+    typedef float vrows __attribute__((ext_vector_type(JR)));
+    __shared__ float2 meet[JOIN_WAVES][JR][64];
+    const Workspace<ROWS, DP, SPLITS> &ws = *(const Workspace<ROWS, DP, SPLITS> *)a.workspace;
+    const Join j = ws.join[blockIdx.x];
+    if (a.by_item) {
+        // no range begins an item that has no units
+        const int blocks = most_blocks<ROWS>(a);
+        const Request q = request_of(a, blockIdx.x / blocks / a.kv.kv_heads);
+        if ((int)(blockIdx.x % blocks) >= row_blocks<ROWS>(a, q))
+            return;
+    }
+    const int i0 = blockIdx.y * JR, n = j.parts;
+    if (n == 0 || i0 >= j.rows)
         return;
-    const int group = a.heads / a.kv.kv_heads, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = j.parts;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const Part<ROWS, DP> *parts = ws.part + 2 * j.range;
     auto part = [&](int k) -> const Part<ROWS, DP> & { return parts[k ? 2 * k : j.second]; };
     const int D = a.kv.head_dim, d = 2 * lane < D ? 2 * lane : 0;
 
-    for (int i0 = blockIdx.y * JOIN_ROWS; i0 < j.rows; i0 += JOIN_GROUPS * JOIN_ROWS) {
-        const int rows = min(j.rows - i0, JOIN_ROWS);
-        if (wave < rows) {
-            float top = NO_SCORE, t = 0.f;
-            for (int k = lane; k < n; k += 64)
-                top = fmaxf(top, part(k).m[i0 + wave]);
+    // (rows past the item's are in the workspace too, and not used)
+    float2 ahead[JOIN_AHEAD][JR];
 #pragma unroll
-            for (int s = 32; s; s >>= 1)
-                top = fmaxf(top, __shfl_xor(top, s));
-            for (int k = lane; k < n; k += 64) {
-                const float f = fast_exp2(part(k).m[i0 + wave] - top);
-                factor[k][wave] = f;
-                t += f * part(k).l[i0 + wave];
+    for (int k = 0; k < JOIN_AHEAD; ++k)
+#pragma unroll
+        for (int r = 0; r < JR; ++r)
+            ahead[k][r] = wave + k * JOIN_WAVES < n
+                              ? *(const float2 *)&part(wave + k * JOIN_WAVES).o[i0 + r][d]
+                              : make_float2(0.f, 0.f);
+    vrows top = NO_SCORE;
+    for (int k = lane; k < n; k += 64) {
+        const vrows m = *(const vrows *)&part(k).m[i0];
+#pragma unroll
+        for (int r = 0; r < JR; ++r)
+            top[r] = fmaxf(top[r], m[r]);
+    }
+#pragma unroll
+    for (int s = 32; s; s >>= 1)
+#pragma unroll
+        for (int r = 0; r < JR; ++r)
+            top[r] = fmaxf(top[r], __shfl_xor(top[r], s));
+    vrows total = 0.f;
+    float2 o[JR] = {};
+    for (int k0 = 0; k0 < n; k0 += 64) {
+        // factors of 64 parts, a part a lane
+        vrows f = 0.f;
+        if (k0 + lane < n) {
+            const vrows m = *(const vrows *)&part(k0 + lane).m[i0], l = *(const vrows *)&part(k0 + lane).l[i0];
+#pragma unroll
+            for (int r = 0; r < JR; ++r) {
+                f[r] = fast_exp2(m[r] - top[r]);
+                total[r] += f[r] * l[r];
             }
-#pragma unroll
-            for (int s = 32; s; s >>= 1)
-                t += __shfl_xor(t, s);
-            if (lane == 0)
-                total[wave] = t;
         }
-        __syncthreads();
-
-        float2 o[JOIN_ROWS] = {};
+        auto factor = [&](int r, int k) {
+            return __builtin_bit_cast(float,
+                                      __builtin_amdgcn_readlane(__builtin_bit_cast(int, (float)f[r]), k - k0));
+        };
+        const int k1 = min(n, k0 + 64);
+        int k = k0 + wave;
+        if (k0 == 0) {
+#pragma unroll
+            for (int i = 0; i < JOIN_AHEAD; ++i, k += JOIN_WAVES)
+                if (k < k1)
+#pragma unroll
+                    for (int r = 0; r < JR; ++r) {
+                        const float w = factor(r, k);
+                        o[r].x += w * ahead[i][r].x;
+                        o[r].y += w * ahead[i][r].y;
+                    }
+        }
 #pragma unroll 4
-        for (int k = wave; k < n; k += JOIN_WAVES) {
-            const Part<ROWS, DP> &p = part(k);
+        for (; k < k1; k += JOIN_WAVES)
 #pragma unroll
-            for (int r = 0; r < JOIN_ROWS; ++r) {
-                const int rr = min(r, rows - 1);
-                const float2 v = *(const float2 *)&p.o[i0 + rr][d];
-                o[r].x += factor[k][rr] * v.x;
-                o[r].y += factor[k][rr] * v.y;
+            for (int r = 0; r < JR; ++r) {
+                const float w = factor(r, k);
+                const float2 v = *(const float2 *)&part(k).o[i0 + r][d];
+                o[r].x += w * v.x;
+                o[r].y += w * v.y;
             }
-        }
+    }
 #pragma unroll
-        for (int r = 0; r < JOIN_ROWS; ++r)
-            sum[wave][r][lane] = o[r];
-        __syncthreads();
-        if (wave < rows && 2 * lane < D) {
+    for (int s = 32; s; s >>= 1)
+#pragma unroll
+        for (int r = 0; r < JR; ++r)
+            total[r] += __shfl_xor(total[r], s);
+#pragma unroll
+    for (int r = 0; r < JR; ++r)
+        meet[wave][r][lane] = o[r];
+    __syncthreads();
+    const int group = a.heads / a.kv.kv_heads;
+#pragma unroll
+    for (int r = 0; r < JR; ++r)
+        if (r % JOIN_WAVES == wave && i0 + r < j.rows && 2 * lane < D) {
             float2 v = make_float2(0.f, 0.f);
 #pragma unroll
             for (int w = 0; w < JOIN_WAVES; ++w) {
-                v.x += sum[w][wave][lane].x;
-                v.y += sum[w][wave][lane].y;
+                v.x += meet[w][r][lane].x;
+                v.y += meet[w][r][lane].y;
             }
-            const float inv = inverse(total[wave]);
-            *(uint32_t *)(out_row(a, j.first, j.kvh, j.row0 + i0 + wave, group) + 2 * lane) =
+            const float inv = inverse(total[r]);
+            *(uint32_t *)(out_row(a, j.first, j.kvh, j.row0 + i0 + r, group) + 2 * lane) =
                 pack2<BF>(v.x * inv, v.y * inv);
         }
-        __syncthreads();
-    }
 }
 
 // ---------------------------------------------------------------------------
@@ -925,18 +1036,29 @@ Shape shape_of(int max_new, int heads, int kv_heads)
     return rows <= 16 ? ROWS16 : rows <= 32 ? ROWS32 : rows <= 64 ? ROWS64 : ROWS128;
 }
 
-int item_rows(Shape s) { return 16 << (int)s; }
+constexpr int WGS = 2;          // workgroups a CU, by registers
+constexpr int JOIN_MOST = 4096;         // workgroups beyond which a join takes four rows each
 
 template <int DP, int ROWS, bool BF>
 int run_attn(const void *kernel, const AttnArgs &a, hipStream_t stream)
 {
+    constexpr int SPLITS = WGS * CUS;
     AttnArgs args = a;
+    const int rows = a.max_new * (a.heads / a.kv.kv_heads), blocks = (rows + ROWS - 1) / ROWS;
+    const long long items = (long long)a.R * a.kv.kv_heads * blocks;
+    // units of 64 positions at least, on a line numbered in 32 bits
+    if (((long long)a.max_pages * a.kv.page_size / 64 + 2) * items >= (1ll << 31))
+        return SBVR_E_UNSUPPORTED;
+    args.by_item = items < SPLITS;
     void *argv[] = {&args};
     const int st = launch_kernel(kernel, dim3(SPLITS), dim3(ATTN_THREADS), 0, stream, argv);
     if (st != SBVR_OK)
         return st;
-    const int groups = (min(a.max_new * (a.heads / a.kv.kv_heads), ROWS) + JOIN_ROWS - 1) / JOIN_ROWS;
-    return launch_kernel((const void *)attn_join_kernel<DP, ROWS, BF>, dim3(SPLITS - 1, min(groups, JOIN_GROUPS)),
+    const int joins = args.by_item ? (int)items : SPLITS - 1, most = min(rows, ROWS);  // the last range divides nothing
+    if ((long long)joins * most <= JOIN_MOST)
+        return launch_kernel((const void *)attn_join_kernel<DP, ROWS, BF, SPLITS, 1>, dim3(joins, most),
+                             dim3(JOIN_THREADS), 0, stream, argv);
+    return launch_kernel((const void *)attn_join_kernel<DP, ROWS, BF, SPLITS, 4>, dim3(joins, (most + 3) / 4),
                          dim3(JOIN_THREADS), 0, stream, argv);
 }
 
@@ -944,10 +1066,10 @@ template <int DP, int DS, bool BF>
 int by_shape(const AttnArgs &a, hipStream_t stream)
 {
     switch (shape_of(a.max_new, a.heads, a.kv.kv_heads)) {
-    case ROWS16: return run_attn<DP, 16, BF>((const void *)attn_rows_kernel<DP, DS, 1, BF>, a, stream);
-    case ROWS32: return run_attn<DP, 32, BF>((const void *)attn_rows_kernel<DP, DS, 2, BF>, a, stream);
-    case ROWS64: return run_attn<DP, 64, BF>((const void *)attn_block_kernel<DP, DS, 1, BF>, a, stream);
-    default: return run_attn<DP, 128, BF>((const void *)attn_block_kernel<DP, DS, 2, BF>, a, stream);
+    case ROWS16: return run_attn<DP, 16, BF>((const void *)attn_rows_kernel<DP, DS, 1, BF, WGS>, a, stream);
+    case ROWS32: return run_attn<DP, 32, BF>((const void *)attn_rows_kernel<DP, DS, 2, BF, WGS>, a, stream);
+    case ROWS64: return run_attn<DP, 64, BF>((const void *)attn_block_kernel<DP, DS, 1, BF, WGS>, a, stream);
+    default: return run_attn<DP, 128, BF>((const void *)attn_block_kernel<DP, DS, 2, BF, WGS>, a, stream);
     }
 }
 
@@ -957,11 +1079,21 @@ int by_type(const AttnArgs &a, hipStream_t stream)
     return a.kv.dtype == SBVR_BF16 ? by_shape<DP, DS, true>(a, stream) : by_shape<DP, DS, false>(a, stream);
 }
 
+template <int DP>
+size_t workspace_of(Shape s)
+{
+    switch (s) {
+    case ROWS16: return sizeof(Workspace<16, DP, WGS * CUS>);
+    case ROWS32: return sizeof(Workspace<32, DP, WGS * CUS>);
+    case ROWS64: return sizeof(Workspace<64, DP, WGS * CUS>);
+    default: return sizeof(Workspace<128, DP, WGS * CUS>);
+    }
+}
+
 size_t attn_workspace_bytes(int, int max_new, int heads, int kv_heads, int head_dim)
 {
-    const size_t rows = item_rows(shape_of(max_new, heads, kv_heads)), dp = head_dim <= 64 ? 64 : 128;
-    static_assert(sizeof(Workspace<16, 64>) == SPLITS * (sizeof(Join) + 2 * 4 * 16 * (64 + 2)), "no padding");
-    return SPLITS * (sizeof(Join) + 2 * 4 * rows * (dp + 2));
+    const Shape s = shape_of(max_new, heads, kv_heads);
+    return head_dim <= 64 ? workspace_of<64>(s) : workspace_of<128>(s);
 }
 
 int launch_attn(const AttnArgs &a, hipStream_t stream)

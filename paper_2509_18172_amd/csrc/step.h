@@ -45,6 +45,7 @@ struct AttnArgs {
     float scale;
     void *out;
     void *workspace;
+    int by_item;  // set by the launcher: joins are numbered by item
 };
 
 struct NormArgs {
