@@ -8,6 +8,8 @@
 
 namespace sbvr {
 
+typedef uint32_t v4u __attribute__((ext_vector_type(4)));
+
 constexpr int WRITE_THREADS = 256, WRITE_UNROLL = 4;
 
 struct WriteArgs {
@@ -33,19 +35,19 @@ __global__ void __launch_bounds__(WRITE_THREADS) cache_write_kernel(WriteArgs a)
         uint16_t *dst = (uint16_t *)(is_v ? a.c.v : a.c.k) + off + head * (is_v ? a.c.v_head_stride : a.c.k_head_stride);
         const int64_t page_stride = is_v ? a.c.v_page_stride : a.c.k_page_stride;
         const int64_t token_stride = is_v ? a.c.v_token_stride : a.c.k_token_stride;
-        uint4 val[WRITE_UNROLL];
+        v4u val[WRITE_UNROLL];
         long long slot[WRITE_UNROLL];
 #pragma unroll
         for (int u = 0; u < WRITE_UNROLL; ++u) {
             const long long t = t0 + u * Y;
-            slot[u] = t < a.T ? a.slots[t] : -1;
-            if (t < a.T)
-                val[u] = *(const uint4 *)(src + t * src_stride);
+            const long long at = min(t, (long long)a.T - 1);  // no branch around the loads
+            slot[u] = t < a.T ? a.slots[at] : -1;
+            val[u] = *(const v4u *)(src + at * src_stride);
         }
 #pragma unroll
         for (int u = 0; u < WRITE_UNROLL; ++u)
             if (slot[u] >= 0 && slot[u] < n_slots)
-                *(uint4 *)(dst + (slot[u] >> a.page_shift) * page_stride + (slot[u] & in_page) * token_stride) = val[u];
+                *(v4u *)(dst + (slot[u] >> a.page_shift) * page_stride + (slot[u] & in_page) * token_stride) = val[u];
     }
 }
 

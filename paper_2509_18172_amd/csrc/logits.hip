@@ -11,119 +11,188 @@
 
 namespace sbvr {
 
-constexpr int LOGITS_THREADS = 256;
 constexpr uint32_t IN_PROMPT = 1u << 31;  // beside the count of generated tokens
 
-// 8 elements, at any alignment of T
-template <typename T>
-struct __attribute__((packed, aligned(sizeof(T)))) Loose8 {
-    T e[8];
+// N elements, at any alignment of T
+template <typename T, int N>
+struct __attribute__((packed, aligned(sizeof(T)))) Loose {
+    T e[N];
 };
 
-template <typename T, typename O, int TILE>
-__global__ void __launch_bounds__(LOGITS_THREADS) logits_kernel(sbvr_logits_args a)
+// f(i, ids[i]) for i0 <= i < i1 over a workgroup, AHEAD pieces of four a thread
+// at a time; past the end f gets the id -1.
+template <int THREADS, int AHEAD, typename F>
+__device__ __forceinline__ void each_id(const int32_t *ids, int i0, int i1, F f)
 {
-    __shared__ uint32_t count[TILE];
-    __shared__ uint32_t bias_at[TILE];  // 1 + index of the last bias of the token, 0: none
+    constexpr int STEP = 4 * THREADS;
+    for (int base = i0; base < i1; base += AHEAD * STEP) {
+        Loose<int32_t, 4> p[AHEAD];
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) {
+            const int i = base + k * STEP + 4 * (int)threadIdx.x;
+            if (i + 4 <= i1)
+                p[k] = *(const Loose<int32_t, 4> *)(ids + i);
+            else
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    p[k].e[e] = i + e < i1 ? ids[i + e] : -1;
+        }
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                f(base + k * STEP + 4 * (int)threadIdx.x + e, p[k].e[e]);
+    }
+}
+
+template <typename T, typename O, int TILE, int THREADS>
+__global__ void __launch_bounds__(THREADS) logits_kernel(sbvr_logits_args a)
+{
+    constexpr int PIECES = TILE / (8 * THREADS);
+    __shared__ __attribute__((aligned(16))) uint32_t count[TILE];
+    __shared__ __attribute__((aligned(16))) uint32_t bias_at[TILE];  // 1 + index of the token's last bias, 0: none
     const long long t = blockIdx.y;
     const int v0 = blockIdx.x * TILE, n = min(TILE, a.V - v0);
+    const T *in = (const T *)a.logits + t * a.logits_stride + v0;
+    O *out = (O *)a.out + t * a.out_stride + v0;
     const int r = a.token_request ? a.token_request[t] : (int)t;
+    Loose<T, 8> l[PIECES];
+#pragma unroll
+    for (int k = 0; k < PIECES; ++k) {
+        const int i = (k * THREADS + (int)threadIdx.x) * 8;
+        if (i + 8 <= n)
+            l[k] = *(const Loose<T, 8> *)(in + i);
+        else
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                l[k].e[e] = i + e < n ? in[i + e] : (T)0.f;
+    }
+
+    // everything of the row that a later load depends on is asked for now
     const bool adjust = r >= 0 && r < a.R;
     const bool counted = adjust && (a.history || a.draft_tokens), biased = adjust && a.bias_tokens;
+    const int row = adjust ? r : 0;
+    const int h0 = a.history ? a.history_start[row] : 0, h1 = a.history ? a.history_start[row + 1] : 0;
+    const int b0 = a.bias_tokens ? a.bias_start[row] : 0, b1 = a.bias_tokens ? a.bias_start[row + 1] : 0;
+    const int prompt = a.prompt_lens ? a.prompt_lens[row] : 0;
+    const uint64_t path = a.draft_tokens ? a.tree_mask[t] : 0;
+    const long long node = a.draft_tokens ? (long long)a.query_start[row] + threadIdx.x : 0;
+    const int g = a.grammar && a.grammar_rows ? a.grammar_rows[t] : (int)t;
+    const float rep = adjust && a.repetition ? a.repetition[row] : 1.f;
+    const float freq = adjust && a.frequency ? a.frequency[row] : 0.f;
+    const float pres = adjust && a.presence ? a.presence[row] : 0.f;
+    const float temp = adjust && a.temperature ? a.temperature[row] : 1.f;
+    uint32_t allowed[PIECES];
+    const bool constrained = adjust && a.grammar && g >= 0 && g < a.grammar_count;
+    const uint8_t *grammar = (const uint8_t *)(a.grammar + (constrained ? g : 0) * a.grammar_stride) + v0 / 8;
+#pragma unroll
+    for (int k = 0; k < PIECES; ++k) {
+        const int i = (k * THREADS + (int)threadIdx.x) * 8;
+        allowed[k] = constrained && i < n ? grammar[i / 8] : 0xffu;
+    }
 
     if (counted || biased) {
-        for (int i = threadIdx.x; i < TILE; i += LOGITS_THREADS) {
-            count[i] = 0;
-            bias_at[i] = 0;
+#pragma unroll
+        for (int k = 0; k < TILE / 4 / THREADS; ++k) {
+            const int i = 4 * (k * THREADS + (int)threadIdx.x);
+            *(uint4 *)&count[i] = uint4{0, 0, 0, 0};
+            *(uint4 *)&bias_at[i] = uint4{0, 0, 0, 0};
         }
         __syncthreads();
-        if (counted && a.history) {
-            const int h0 = a.history_start[r], h1 = a.history_start[r + 1];
-            const int prompt = a.prompt_lens ? a.prompt_lens[r] : 0;
-            for (int i = h0 + threadIdx.x; i < h1; i += LOGITS_THREADS) {
-                const uint32_t d = (uint32_t)(a.history[i] - v0);
+        // An id below v0 or negative is a large d (v0 is at most 2^30), as is the
+        // -1 past the end.
+        if (counted) {
+            each_id<THREADS, 4>(a.history, h0, h1, [&](int i, int id) {
+                const uint32_t d = (uint32_t)(id - v0);
                 if (d < (uint32_t)n) {
                     if (i - h0 < prompt)
                         atomicOr(&count[d], IN_PROMPT);
                     else
                         atomicAdd(&count[d], 1u);
                 }
-            }
-        }
-        if (counted && a.draft_tokens && threadIdx.x < SBVR_TREE_MAX && ((a.tree_mask[t] >> threadIdx.x) & 1)) {
-            const long long node = (long long)a.query_start[r] + threadIdx.x;
-            if (node >= 0 && node < a.T) {
+            });
+            if (threadIdx.x < SBVR_TREE_MAX && ((path >> threadIdx.x) & 1) && node >= 0 && node < a.T) {
                 const uint32_t d = (uint32_t)(a.draft_tokens[node] - v0);
                 if (d < (uint32_t)n)
                     atomicAdd(&count[d], 1u);
             }
         }
-        if (biased) {
-            const int b0 = a.bias_start[r], b1 = a.bias_start[r + 1];
-            for (int i = b0 + threadIdx.x; i < b1; i += LOGITS_THREADS) {
-                const uint32_t d = (uint32_t)(a.bias_tokens[i] - v0);
+        if (biased)
+            each_id<THREADS, 1>(a.bias_tokens, b0, b1, [&](int i, int id) {
+                const uint32_t d = (uint32_t)(id - v0);
                 if (d < (uint32_t)n)
                     atomicMax(&bias_at[d], (uint32_t)(i - b0) + 1u);
-            }
-        }
+            });
         __syncthreads();
     }
 
-    const float rep = adjust && a.repetition ? a.repetition[r] : 1.f;
-    const float freq = adjust && a.frequency ? a.frequency[r] : 0.f;
-    const float pres = adjust && a.presence ? a.presence[r] : 0.f;
-    const float temp = adjust && a.temperature ? a.temperature[r] : 1.f;
-    const float inv_temp = temp > 0.f ? 1.f / temp : 1.f;
-    const float *bias = biased ? a.bias_values + a.bias_start[r] : nullptr;
-    const uint8_t *grammar = nullptr;
-    if (adjust && a.grammar) {
-        const int g = a.grammar_rows ? a.grammar_rows[t] : (int)t;
-        if (g >= 0 && g < a.grammar_count)
-            grammar = (const uint8_t *)(a.grammar + g * a.grammar_stride) + v0 / 8;
-    }
-    const T *in = (const T *)a.logits + t * a.logits_stride + v0;
-    O *out = (O *)a.out + t * a.out_stride + v0;
-
-    auto one = [&](float l, int i) {
+    const float inv_rep = 1.f / rep, inv_temp = temp > 0.f ? 1.f / temp : 1.f;
+#pragma unroll
+    for (int k = 0; k < PIECES; ++k) {
+        const int i = (k * THREADS + (int)threadIdx.x) * 8;
+        if (i >= n)
+            continue;
+        uint32_t c[8] = {}, b[8] = {}, any_c = 0, any_b = 0;
         if (counted) {
-            const uint32_t c = count[i];
-            if (c) {
-                l = l > 0.f ? l / rep : l * rep;
-                const uint32_t times = c & ~IN_PROMPT;
-                l -= freq * (float)times + (times ? pres : 0.f);
-            }
+            *(uint4 *)&c[0] = *(const uint4 *)&count[i];
+            *(uint4 *)&c[4] = *(const uint4 *)&count[i + 4];
         }
         if (biased) {
-            const uint32_t b = bias_at[i];
-            if (b)
-                l += bias[b - 1];
+            *(uint4 *)&b[0] = *(const uint4 *)&bias_at[i];
+            *(uint4 *)&b[4] = *(const uint4 *)&bias_at[i + 4];
         }
-        return l * inv_temp;
-    };
-    for (int i = threadIdx.x * 8; i < n; i += LOGITS_THREADS * 8) {
-        const uint32_t allowed = grammar ? grammar[i / 8] : 0xffu;
-        if (i + 8 <= n) {
-            const Loose8<T> l = *(const Loose8<T> *)(in + i);
-            Loose8<O> o;
+        float x[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            x[e] = (float)l[k].e[e];
+            any_c |= c[e];
+            any_b |= b[e];
+        }
+        if (any_c) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const uint32_t times = c[e] & ~IN_PROMPT;
+                const float y = x[e] * (x[e] > 0.f ? inv_rep : rep) - (freq * (float)times + (times ? pres : 0.f));
+                x[e] = c[e] ? y : x[e];
+            }
+        }
+        if (any_b) {
 #pragma unroll
             for (int e = 0; e < 8; ++e)
-                o.e[e] = (O)((allowed >> e) & 1 ? one((float)l.e[e], i + e) : -INFINITY);
-            *(Loose8<O> *)(out + i) = o;
-        } else {
-            for (int e = 0; e < n - i; ++e)
-                out[i + e] = (O)((allowed >> e) & 1 ? one((float)in[i + e], i + e) : -INFINITY);
+                if (b[e])
+                    x[e] += a.bias_values[b0 + (int)b[e] - 1];
         }
+        Loose<O, 8> o;
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            o.e[e] = (O)((allowed[k] >> e) & 1 ? x[e] * inv_temp : -INFINITY);
+        if (i + 8 <= n)
+            *(Loose<O, 8> *)(out + i) = o;
+        else
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (i + e < n)
+                    out[i + e] = o.e[e];
     }
+}
+
+template <typename T, typename O, int TILE, int THREADS>
+int run_logits(const sbvr_logits_args &a, hipStream_t stream)
+{
+    sbvr_logits_args args = a;
+    void *argv[] = {&args};
+    return launch_kernel((const void *)logits_kernel<T, O, TILE, THREADS>, dim3((a.V + TILE - 1) / TILE, a.T),
+                         dim3(THREADS), 0, stream, argv);
 }
 
 template <typename T, typename O>
 int go_logits(const sbvr_logits_args &a, hipStream_t stream)
 {
-    sbvr_logits_args args = a;
-    void *argv[] = {&args};
-    constexpr int TILE = 4096;
-    return launch_kernel((const void *)logits_kernel<T, O, TILE>, dim3((a.V + TILE - 1) / TILE, a.T),
-                         dim3(LOGITS_THREADS), 0, stream, argv);
+    // large tiles read the history less often; small ones where those would not
+    // fill the chip twice
+    if ((long long)a.T * ((a.V + 8191) / 8192) >= 512)
+        return run_logits<T, O, 8192, 512>(a, stream);
+    return run_logits<T, O, 2048, 256>(a, stream);
 }
 
 int launch_logits(const sbvr_logits_args &a, hipStream_t stream)

@@ -1,6 +1,5 @@
 // Shared by the operators between the products of a step (plan, cache write,
-// attention, norms, logits): element types, launch parameters, and the scan
-// over the requests that several kernels repeat in every workgroup.
+// attention, norms, logits): element types, launch parameters and a search.
 #pragma once
 
 #include <hip/hip_fp16.h>
@@ -79,43 +78,6 @@ __device__ __forceinline__ int owner_of(const I *start, int n, I v)
             hi = mid;
     }
     return lo;
-}
-
-// Exclusive prefix sums of two values per thread over a workgroup of THREADS
-// threads (a multiple of 64); `total` gets the sums.  scratch: 2 * THREADS / 64
-// entries of LDS.  Ends with a barrier passed by every thread.
-template <int THREADS>
-__device__ __forceinline__ void scan_pair(long long &a, long long &b, long long &total_a, long long &total_b,
-                                          long long *scratch)
-{
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    long long ia = a, ib = b;
-#pragma unroll
-    for (int s = 1; s < 64; s <<= 1) {
-        const long long pa = __shfl_up(ia, s), pb = __shfl_up(ib, s);
-        if (lane >= s) {
-            ia += pa;
-            ib += pb;
-        }
-    }
-    if (lane == 63) {
-        scratch[2 * wave] = ia;
-        scratch[2 * wave + 1] = ib;
-    }
-    __syncthreads();
-    long long ba = 0, bb = 0;
-    total_a = total_b = 0;
-#pragma unroll
-    for (int w = 0; w < THREADS / 64; ++w) {
-        if (w == wave) {
-            ba = total_a;
-            bb = total_b;
-        }
-        total_a += scratch[2 * w];
-        total_b += scratch[2 * w + 1];
-    }
-    a = ba + ia - a;
-    b = bb + ib - b;
 }
 
 }  // namespace sbvr

@@ -11,39 +11,62 @@ products, and ``adjust_logits`` on the last product.
 """
 from __future__ import annotations
 
+import ctypes as C
+import functools
+
 import torch
 
-from . import (SBVR_BF16, SBVR_F16, SBVR_F32, CacheStruct, LogitsStruct, _check, _stream, sbvr_adjust_logits,
-               sbvr_batch_plan, sbvr_cache_write, sbvr_residual_norm, sbvr_tree_attention,
+from . import (SBVR_BF16, SBVR_F16, SBVR_F32, CacheStruct, LogitsStruct, SBVRError, _lib, _stream,
                sbvr_tree_attention_workspace_bytes)
+
+# These calls are short, and one step makes hundreds of them: the library's
+# functions are called without the wrappers of the same names.
+_workspace_bytes = functools.lru_cache(maxsize=256)(sbvr_tree_attention_workspace_bytes)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
+def _on(stream, device) -> int:
+    """The handle of `stream`, by default the current stream of `device`."""
+    return _stream(stream) if stream is not None or _raw_stream is None else _raw_stream(device.index)
+
+
+def _check(status: int, what: str):
+    if status:
+        raise SBVRError(status, what)
+
 
 _DTYPE = {torch.float16: SBVR_F16, torch.bfloat16: SBVR_BF16, torch.float32: SBVR_F32}
 
 
 def _dense(t, dtype, shape, device, what):
-    """The pointer of an optional contiguous tensor of one dtype and shape
-    (None in a shape: any size)."""
+    """The pointer of an optional contiguous tensor of one dtype and shape."""
     if t is None:
         return None
-    assert t.dtype == dtype and t.is_contiguous() and t.device == device and len(t.shape) == len(shape) \
-        and all(n is None or n == m for n, m in zip(shape, t.shape)), \
-        f"{what} must be a contiguous {dtype} tensor of shape {shape} on {device}"
+    if t.dtype != dtype or t.shape != shape or not t.is_contiguous() or t.device != device:
+        raise AssertionError(f"{what} must be a contiguous {dtype} tensor of shape {tuple(shape)} on {device}")
     return t.data_ptr()
+
+
+def _list(t, dtype, device, what):
+    """The pointer and length of an optional contiguous 1-D tensor."""
+    if t is None:
+        return None, 0
+    n, = t.shape
+    return _dense(t, dtype, (n,), device, what), n
 
 
 def _rows(t, dtype, shape, device, what):
     """The pointer and row stride of a 2-D tensor with contiguous rows."""
-    assert t.dtype == dtype and tuple(t.shape) == tuple(shape) and t.device == device \
-        and (t.stride(1) == 1 or shape[1] == 1), f"{what} must be a {dtype} tensor {tuple(shape)} of contiguous rows"
+    if t.dtype != dtype or t.shape != shape or t.device != device or (t.stride(1) != 1 and shape[1] != 1):
+        raise AssertionError(f"{what} must be a {dtype} tensor {tuple(shape)} of contiguous rows on {device}")
     return t.data_ptr(), t.stride(0)
 
 
 def _table(page_table, R, device):
-    assert page_table.dtype == torch.int32 and page_table.dim() == 2 and page_table.shape[0] == R \
-        and page_table.device == device and (page_table.stride(1) == 1 or page_table.shape[1] == 1), \
-        "page_table must be an int32 tensor [requests][max_pages] of contiguous rows on the batch's device"
+    rows, pages = page_table.shape
+    pointer, stride = _rows(page_table, torch.int32, (R, pages), device, "page_table")
     # a single row's stride means nothing, and torch may report a smaller one
-    return page_table.data_ptr(), page_table.shape[1], max(page_table.stride(0), page_table.shape[1])
+    return pointer, pages, max(stride, pages)
 
 
 class BatchPlan:
@@ -52,13 +75,9 @@ class BatchPlan:
     [T] (bits of a uint64), used int32 [2] (pages taken, new tokens)."""
 
     def __init__(self, R: int, T: int, device):
-        i32, i64 = torch.int32, torch.int64
-        self.query_start = torch.empty(R + 1, dtype=i32, device=device)
-        self.token_request = torch.empty(T, dtype=i32, device=device)
-        self.positions = torch.empty(T, dtype=i32, device=device)
-        self.slots = torch.empty(T, dtype=i64, device=device)
-        self.tree_mask = torch.empty(T, dtype=i64, device=device)
-        self.used = torch.empty(2, dtype=i32, device=device)
+        self.query_start, self.token_request, self.positions, self.used = torch.empty(
+            R + 2 * T + 3, dtype=torch.int32, device=device).split((R + 1, T, T, 2))
+        self.slots, self.tree_mask = torch.empty((2, T), dtype=torch.int64, device=device).unbind(0)
 
 
 def batch_plan(context_lens, new_lens, free_pages, page_table, page_size: int, n_tokens: int, parents=None, out=None,
@@ -80,12 +99,12 @@ def batch_plan(context_lens, new_lens, free_pages, page_table, page_size: int, n
         for name, dtype, n in (("query_start", i32, R + 1), ("token_request", i32, T), ("positions", i32, T),
                                ("slots", torch.int64, T), ("tree_mask", torch.int64, T), ("used", i32, 2)):
             _dense(getattr(p, name), dtype, (n,), device, name)
-    _check(sbvr_batch_plan(R, T, page_size, _dense(context_lens, i32, (R,), device, "context_lens"),
+    _check(_lib.sbvr_batch_plan(R, T, page_size, _dense(context_lens, i32, (R,), device, "context_lens"),
                            _dense(new_lens, i32, (R,), device, "new_lens"),
-                           _dense(free_pages, i32, (None,), device, "free_pages"), free_pages.shape[0],
+                           *_list(free_pages, i32, device, "free_pages"),
                            _dense(parents, i32, (T,), device, "parents"), table, max_pages, stride,
                            p.query_start.data_ptr(), p.token_request.data_ptr(), p.positions.data_ptr(),
-                           p.slots.data_ptr(), p.tree_mask.data_ptr(), p.used.data_ptr(), _stream(stream)),
+                           p.slots.data_ptr(), p.tree_mask.data_ptr(), p.used.data_ptr(), _on(stream, device)),
            "sbvr_batch_plan")
     return p
 
@@ -96,13 +115,17 @@ class KVCache:
     page is a transposed view)."""
 
     def __init__(self, k, v):
-        assert k.dim() == 4 and k.shape == v.shape and k.dtype == v.dtype and k.dtype in _DTYPE \
-            and k.is_cuda and k.device == v.device, "k and v must be alike, [pages][page_size][kv_heads][head_dim]"
-        assert k.stride(3) == 1 and v.stride(3) == 1, "a head's elements must be contiguous"
-        self.k, self.v = k, v
         n_pages, page_size, heads, dim = k.shape
-        self.struct = CacheStruct(k.data_ptr(), v.data_ptr(), *k.stride()[:3], *v.stride()[:3], n_pages, page_size,
-                                  heads, dim, _DTYPE[k.dtype])
+        ks, vs = k.stride(), v.stride()
+        assert k.shape == v.shape and k.dtype == v.dtype and k.dtype in _DTYPE and k.is_cuda and k.device == v.device, \
+            "k and v must be alike, [pages][page_size][kv_heads][head_dim]"
+        assert ks[3] == 1 and vs[3] == 1, "a head's elements must be contiguous"
+        self.k, self.v = k, v
+        self.dtype, self.device, self.kv_heads, self.head_dim = k.dtype, k.device, heads, dim
+        # (the struct is kept with its address, which the library reads it at)
+        self.struct = CacheStruct(k.data_ptr(), v.data_ptr(), *ks[:3], *vs[:3], n_pages, page_size, heads, dim,
+                                  _DTYPE[k.dtype])
+        self.address = C.addressof(self.struct)
 
     @staticmethod
     def alloc(n_pages: int, page_size: int, kv_heads: int, head_dim: int, dtype=torch.float16, device="cuda"):
@@ -113,20 +136,22 @@ class KVCache:
 def _heads(t, heads, dim, cache, what):
     """The pointer and the token and head strides of a [T][heads][dim] tensor
     that goes with a cache."""
-    assert t.dim() == 3 and t.shape[1] == heads and t.shape[2] == dim and t.dtype == cache.k.dtype \
-        and t.device == cache.k.device and t.stride(2) == 1, \
-        f"{what} must be a {cache.k.dtype} tensor [tokens][{heads}][{dim}] with contiguous heads on the cache's device"
-    return t.data_ptr(), t.stride(0), t.stride(1)
+    token, head, one = t.stride()
+    if t.shape != (t.shape[0], heads, dim) or one != 1 or t.dtype != cache.dtype or t.device != cache.device:
+        raise AssertionError(f"{what} must be a {cache.dtype} tensor [tokens][{heads}][{dim}] with contiguous heads on "
+                             "the cache's device")
+    return t.data_ptr(), token, head
 
 
 def cache_write(cache: KVCache, k, v, slots, stream=None):
     """Write a step's keys and values [T][kv_heads][head_dim] (views with
     contiguous heads) to the slots (int64 [T]; negative: skipped)."""
-    heads, dim = cache.k.shape[2:]
+    heads, dim = cache.kv_heads, cache.head_dim
     T = k.shape[0]
-    assert v.shape[0] == T
-    _check(sbvr_cache_write(cache.struct, T, *_heads(k, heads, dim, cache, "k"), *_heads(v, heads, dim, cache, "v"),
-                            _dense(slots, torch.int64, (T,), k.device, "slots"), _stream(stream)), "sbvr_cache_write")
+    assert v.shape[0] == T, "k and v must have the same tokens"
+    _check(_lib.sbvr_cache_write(cache.address, T, *_heads(k, heads, dim, cache, "k"), *_heads(v, heads, dim, cache, "v"),
+                            _dense(slots, torch.int64, (T,), cache.device, "slots"), _on(stream, cache.device)),
+           "sbvr_cache_write")
 
 
 def tree_attention(q, cache: KVCache, page_table, context_lens, query_start, tree_mask, max_new: int, scale=None,
@@ -137,25 +162,23 @@ def tree_attention(q, cache: KVCache, page_table, context_lens, query_start, tre
     [head_dim].  workspace: a uint8 tensor of
     sbvr_tree_attention_workspace_bytes, by default a new one."""
     T, H, D = q.shape
-    R, device = context_lens.shape[0], q.device
-    kv_heads = cache.k.shape[2]
-    qp, q_token, q_head = _heads(q, H, cache.k.shape[3], cache, "q")
+    R, device = context_lens.shape[0], cache.device
+    qp, q_token, q_head = _heads(q, H, cache.head_dim, cache, "q")
     table, max_pages, stride = _table(page_table, R, device)
     if out is None:
         out = torch.empty((T, H, D), dtype=q.dtype, device=device)
-    need = sbvr_tree_attention_workspace_bytes(R, max_new, H, kv_heads, D)
+    need = _workspace_bytes(R, max_new, H, cache.kv_heads, D)
     if workspace is None and need:
         workspace = torch.empty(need, dtype=torch.uint8, device=device)
         if stream is not None:
             workspace.record_stream(stream)
-    _check(sbvr_tree_attention(cache.struct, R, T, H, qp, q_token, q_head, table, max_pages, stride,
+    _check(_lib.sbvr_tree_attention(cache.address, R, T, H, qp, q_token, q_head, table, max_pages, stride,
                                _dense(context_lens, torch.int32, (R,), device, "context_lens"),
                                _dense(query_start, torch.int32, (R + 1,), device, "query_start"),
                                _dense(tree_mask, torch.int64, (T,), device, "tree_mask"), max_new,
                                float(D ** -0.5 if scale is None else scale),
                                _dense(out, q.dtype, (T, H, D), device, "out"),
-                               _dense(workspace, torch.uint8, (None,), device, "workspace"),
-                               0 if workspace is None else workspace.numel(), _stream(stream)),
+                               *_list(workspace, torch.uint8, device, "workspace"), _on(stream, device)),
            "sbvr_tree_attention")
     return out
 
@@ -189,10 +212,10 @@ def residual_norm(x, y=None, post_weight=None, gate=None, scale: float = 1.0, pr
     if pre_weight is not None:
         h_out = torch.empty((T, H), dtype=dtype, device=device) if h_out is None else h_out
         hp, h_stride = _rows(h_out, dtype, (T, H), device, "h_out")
-    _check(sbvr_residual_norm(T, H, _DTYPE[dtype], _DTYPE[x.dtype], xp, x_stride, yp, y_stride,
+    _check(_lib.sbvr_residual_norm(T, H, _DTYPE[dtype], _DTYPE[x.dtype], xp, x_stride, yp, y_stride,
                               _dense(post_weight, dtype, (H,), device, "post_weight"), gp, g_stride, float(scale),
                               _dense(pre_weight, dtype, (H,), device, "pre_weight"), float(eps), op, o_stride, hp,
-                              h_stride, _stream(stream)), "sbvr_residual_norm")
+                              h_stride, _on(stream, device)), "sbvr_residual_norm")
     return (x if y is None else x_out), h_out
 
 
@@ -221,7 +244,7 @@ def adjust_logits(logits, history=None, history_start=None, prompt_lens=None, re
     assert (bias_tokens is None) == (bias_start is None) == (bias_values is None), "the three bias tensors go together"
     lp, l_stride = _rows(logits, logits.dtype, (T, V), device, "logits")
     op, o_stride = _rows(out, out.dtype, (T, V), device, "out")
-    n_bias = None if bias_tokens is None else bias_tokens.shape[0]
+    n_bias = 0 if bias_tokens is None else bias_tokens.shape[0]
     gp, g_stride, g_count = None, 0, 0
     if grammar is not None:
         g_count = grammar.shape[0]
@@ -229,7 +252,7 @@ def adjust_logits(logits, history=None, history_start=None, prompt_lens=None, re
         g_stride = max(g_stride, grammar.shape[1])
     args = LogitsStruct(R, T, V, _DTYPE[logits.dtype], _DTYPE[out.dtype], lp, l_stride, op, o_stride,
                         _dense(token_request, i32, (T,), device, "token_request"),
-                        _dense(history, i32, (None,), device, "history"),
+                        _list(history, i32, device, "history")[0],
                         _dense(history_start, i32, (R + 1,), device, "history_start"),
                         _dense(prompt_lens, i32, (R,), device, "prompt_lens"),
                         _dense(repetition, f32, (R,), device, "repetition"),
@@ -243,5 +266,5 @@ def adjust_logits(logits, history=None, history_start=None, prompt_lens=None, re
                         _dense(draft_tokens, i32, (T,), device, "draft_tokens"),
                         _dense(query_start, i32, (R + 1,), device, "query_start"),
                         _dense(tree_mask, torch.int64, (T,), device, "tree_mask"))
-    _check(sbvr_adjust_logits(args, _stream(stream)), "sbvr_adjust_logits")
+    _check(_lib.sbvr_adjust_logits(C.addressof(args), _on(stream, device)), "sbvr_adjust_logits")
     return out
