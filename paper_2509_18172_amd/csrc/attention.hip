@@ -116,15 +116,6 @@ __device__ __forceinline__ bool not_finite(uint32_t w)
     return ((w & E) == E) | ((w & (E << 16)) == (E << 16));
 }
 
-// A value that is the same in every lane and that no kernel of this file
-// writes, read on the scalar side: a vector load would have its wait among
-// those of the tiles.
-template <typename T>
-__device__ __forceinline__ T uniform_load(const T *p)
-{
-    return *(const __attribute__((address_space(4))) T *)p;
-}
-
 __device__ __forceinline__ float max4(float v)  // over the four lane groups
 {
     v = fmaxf(v, __shfl_xor(v, 16));

@@ -1,27 +1,73 @@
 // The norms around a block with its gate and residual scale: z = rms(y) * w,
 // x' = x + scale * gate * z, h = rms(x') * w', one pass over the rows.
 //
-// A row is held in registers by the threads of one workgroup (a piece of VEC
-// elements each, CH times), so x, y and the gate are read once and x' and h
-// written once; the two means are sums over the workgroup in a fixed order.
-// Memory-bound for many tokens, bound by its two reductions' latency for few.
+// A row is held in registers by THREADS threads, CH pieces of eight elements
+// each, so x, y and the gate are read once and x' and h written once; the two
+// means are sums in a fixed order.  Every load is sent off at the start, without
+// a branch, so that one latency covers them; the first reduction and the second
+// follow.  Up to 512 elements a wavefront has a row of its own, four to a
+// workgroup, and no barrier.  Memory-bound for many tokens.
+//
+// Rows need no alignment beyond their elements'.  A piece that would pass the
+// row's end is moved back to end with it: of its elements the first ones belong
+// to the piece before and are neither summed nor stored.
 #include "step.h"
 
 namespace sbvr {
 
-template <typename T, int N>
-struct alignas(sizeof(T) * N) Vec {
-    T e[N];
+enum Tail { EVEN, ODD, SHORT };  // H a multiple of 8; any other from 8 on; below 8
+
+// where a thread's piece lies: from `at`, its own elements from `own` on (8: none)
+struct Piece {
+    int at, own;
 };
 
-template <typename T>
-__device__ __forceinline__ float widen(T v)
+template <Tail TAIL>
+__device__ __forceinline__ Piece piece_at(int i, int H)
 {
-    return (float)v;
+    if constexpr (TAIL == SHORT)
+        return {0, i == 0 ? 0 : 8};
+    const int at = min(i, H - 8);
+    return {at, min(i - at, 8)};
+}
+
+template <Tail TAIL, typename T>
+__device__ __forceinline__ Loose<T, 8> load8(const T *row, Piece p, int H)
+{
+    if constexpr (TAIL != SHORT)
+        return from_words<T>(load_words(row + p.at));
+    Loose<T, 8> r;
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        r.e[e] = row[min(e, H - 1)];
+    return r;
+}
+
+// whether element e of the piece is the thread's own
+template <Tail TAIL>
+__device__ __forceinline__ bool owns(Piece p, int e, int H)
+{
+    return TAIL == EVEN ? p.own == 0 : TAIL == ODD ? e >= p.own : e >= p.own && e < H;
+}
+
+template <Tail TAIL, typename T>
+__device__ __forceinline__ void store8(T *row, Piece p, int H, const float (&v)[8])
+{
+    Loose<T, 8> r;
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        r.e[e] = (T)v[e];
+    if (TAIL != SHORT && p.own == 0)
+        store_words(row + p.at, to_words(r));
+    else if (TAIL != EVEN)
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (owns<TAIL>(p, e, H))
+                row[p.at + e] = r.e[e];
 }
 
 template <int THREADS>
-__device__ __forceinline__ float block_sum(float v, float *scratch)
+__device__ __forceinline__ float row_sum(float v, float *scratch)
 {
 #pragma unroll
     for (int s = 32; s; s >>= 1)
@@ -38,120 +84,107 @@ __device__ __forceinline__ float block_sum(float v, float *scratch)
     return t;
 }
 
+constexpr int rows_of(int threads) { return threads == 64 ? 4 : 1; }  // rows of a workgroup
+
 // A: type of y, gate, weights, h; X: type of the residual stream.
-template <typename A, typename X, int VEC, int CH, int THREADS>
-__global__ void __launch_bounds__(THREADS) norm_kernel(NormArgs a)
+template <typename A, typename X, int CH, int THREADS, Tail TAIL>
+__global__ void __launch_bounds__(THREADS *rows_of(THREADS)) norm_kernel(NormArgs a)
 {
     __shared__ float scratch[2][THREADS / 64];
-    const long long t = blockIdx.x;
-    const A *y = (const A *)a.y + t * a.y_stride;
-    const A *gate = (const A *)a.gate + t * a.gate_stride;
+    const int lane = threadIdx.x % THREADS;
+    const long long t = (long long)blockIdx.x * rows_of(THREADS) + threadIdx.x / THREADS;
+    if (t >= a.T)  // only where a wavefront has a row of its own
+        return;
+    // an operand that is not given is read from x's row all the same (x is no
+    // shorter) and not used
     const X *x = (const X *)a.x + t * a.x_stride;
-    const A *post = (const A *)a.post, *pre = (const A *)a.pre;
+    const A *y = a.y ? (const A *)a.y + t * a.y_stride : (const A *)x;
+    const A *gate = a.gate ? (const A *)a.gate + t * a.gate_stride : (const A *)x;
+    const A *post = a.post ? (const A *)a.post : (const A *)x, *pre = a.h_out ? (const A *)a.pre : (const A *)x;
 
-    float xv[CH][VEC], yv[CH][VEC];
-    float sum = 0.f;
+    Piece p[CH];
+    Loose<X, 8> xr[CH];
+    Loose<A, 8> yr[CH], postr[CH], gater[CH], prer[CH];
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
-        const int i = (c * THREADS + (int)threadIdx.x) * VEC;
-        Vec<X, VEC> xr = {};
-        Vec<A, VEC> yr = {};
-        if (i < a.H) {
-            xr = *(const Vec<X, VEC> *)(x + i);
-            if (a.y)
-                yr = *(const Vec<A, VEC> *)(y + i);
-        }
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) {
-            xv[c][e] = widen(xr.e[e]);
-            yv[c][e] = widen(yr.e[e]);
-            sum += yv[c][e] * yv[c][e];
-        }
+        p[c] = piece_at<TAIL>((c * THREADS + lane) * 8, a.H);
+        xr[c] = load8<TAIL>(x, p[c], a.H);
+        yr[c] = load8<TAIL>(y, p[c], a.H);
+        postr[c] = load8<TAIL>(post, p[c], a.H);
+        gater[c] = load8<TAIL>(gate, p[c], a.H);
+        prer[c] = load8<TAIL>(pre, p[c], a.H);
     }
-    if (a.y) {
-        float inv = 1.f;
-        if (a.post)
-            inv = 1.f / sqrtf(block_sum<THREADS>(sum, scratch[0]) / (float)a.H + a.eps);
+    float xv[CH][8], sum = 0.f;
+    if (a.y && a.post) {
 #pragma unroll
-        for (int c = 0; c < CH; ++c) {
-            const int i = (c * THREADS + (int)threadIdx.x) * VEC;
-            if (i < a.H) {
-                Vec<A, VEC> w = {}, g = {};
-                if (a.post)
-                    w = *(const Vec<A, VEC> *)(post + i);
-                if (a.gate)
-                    g = *(const Vec<A, VEC> *)(gate + i);
+        for (int c = 0; c < CH; ++c)
 #pragma unroll
-                for (int e = 0; e < VEC; ++e) {
-                    float z = yv[c][e];
-                    if (a.post)
-                        z = z * inv * widen(w.e[e]);
-                    if (a.gate)
-                        z *= widen(g.e[e]);
-                    xv[c][e] += a.scale * z;
-                }
+            for (int e = 0; e < 8; ++e) {
+                const float v = (float)yr[c].e[e];
+                sum += owns<TAIL>(p[c], e, a.H) ? v * v : 0.f;
             }
-        }
+        sum = row_sum<THREADS>(sum, scratch[0]);
     }
+    const float inv_y = 1.f / sqrtf(sum / (float)a.H + a.eps);
     sum = 0.f;
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
-        const int i = (c * THREADS + (int)threadIdx.x) * VEC;
-        Vec<X, VEC> o;
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) {
-            o.e[e] = (X)xv[c][e];
-            sum += xv[c][e] * xv[c][e];
+        for (int e = 0; e < 8; ++e) {
+            float z = (float)yr[c].e[e];
+            if (a.post)
+                z = z * inv_y * (float)postr[c].e[e];
+            if (a.gate)
+                z *= (float)gater[c].e[e];
+            xv[c][e] = (float)xr[c].e[e] + (a.y ? a.scale * z : 0.f);
+            sum += owns<TAIL>(p[c], e, a.H) ? xv[c][e] * xv[c][e] : 0.f;
         }
-        if (a.x_out && i < a.H)
-            *(Vec<X, VEC> *)((X *)a.x_out + t * a.x_out_stride + i) = o;
+        if (a.x_out)
+            store8<TAIL>((X *)a.x_out + t * a.x_out_stride, p[c], a.H, xv[c]);
     }
     if (!a.h_out)
         return;
-    const float inv = 1.f / sqrtf(block_sum<THREADS>(sum, scratch[1]) / (float)a.H + a.eps);
+    const float inv = 1.f / sqrtf(row_sum<THREADS>(sum, scratch[1]) / (float)a.H + a.eps);
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
-        const int i = (c * THREADS + (int)threadIdx.x) * VEC;
-        if (i < a.H) {
-            const Vec<A, VEC> w = *(const Vec<A, VEC> *)(pre + i);
-            Vec<A, VEC> o;
+        float h[8];
 #pragma unroll
-            for (int e = 0; e < VEC; ++e)
-                o.e[e] = (A)(xv[c][e] * inv * widen(w.e[e]));
-            *(Vec<A, VEC> *)((A *)a.h_out + t * a.h_stride + i) = o;
-        }
+        for (int e = 0; e < 8; ++e)
+            h[e] = xv[c][e] * inv * (float)prer[c].e[e];
+        store8<TAIL>((A *)a.h_out + t * a.h_stride, p[c], a.H, h);
     }
 }
 
-template <typename A, typename X, int VEC, int CH, int THREADS>
+template <typename A, typename X, int CH, int THREADS>
 int go(const NormArgs &a, hipStream_t stream)
 {
+    constexpr int ROWS = rows_of(THREADS);
     NormArgs args = a;
     void *argv[] = {&args};
-    return launch_kernel((const void *)norm_kernel<A, X, VEC, CH, THREADS>, dim3((unsigned)a.T), dim3(THREADS), 0,
-                         stream, argv);
+    const void *kernel = a.H < 8        ? (const void *)norm_kernel<A, X, 1, 64, SHORT>
+                         : a.H % 8 == 0 ? (const void *)norm_kernel<A, X, CH, THREADS, EVEN>
+                                        : (const void *)norm_kernel<A, X, CH, THREADS, ODD>;
+    return launch_kernel(kernel, dim3((unsigned)((a.T + (long long)ROWS - 1) / ROWS)), dim3(THREADS * ROWS), 0, stream,
+                         argv);
 }
 
 template <typename A, typename X>
 int dispatch(const NormArgs &a, hipStream_t stream)
 {
-    // 16 bytes a lane where every row of 16-bit elements starts on them (the
-    // residual stream's rows then start on 16 or 32)
-    const uintptr_t at = (uintptr_t)a.x | (uintptr_t)a.y | (uintptr_t)a.post | (uintptr_t)a.gate |
-                         (uintptr_t)a.pre | (uintptr_t)a.x_out | (uintptr_t)a.h_out;
-    const int64_t strides = a.x_stride | a.y_stride | a.gate_stride | a.x_out_stride | a.h_stride | (int64_t)a.H;
-    if (at % 32 == 0 && strides % 8 == 0) {
-        if (a.H <= 512 * 8)
-            return go<A, X, 8, 1, 512>(a, stream);
-        if (a.H <= 1024 * 8)
-            return go<A, X, 8, 1, 1024>(a, stream);
-        return go<A, X, 8, 4, 1024>(a, stream);
-    }
+    // one piece a thread as far as a workgroup's threads go
+    if (a.H <= 64 * 8)
+        return go<A, X, 1, 64>(a, stream);
+    if (a.H <= 128 * 8)
+        return go<A, X, 1, 128>(a, stream);
     if (a.H <= 256 * 8)
-        return go<A, X, 1, 8, 256>(a, stream);
+        return go<A, X, 1, 256>(a, stream);
+    if (a.H <= 512 * 8)
+        return go<A, X, 1, 512>(a, stream);
     if (a.H <= 1024 * 8)
-        return go<A, X, 1, 8, 1024>(a, stream);
-    return go<A, X, 1, 32, 1024>(a, stream);
+        return go<A, X, 1, 1024>(a, stream);
+    if (a.H <= 2048 * 8)
+        return go<A, X, 2, 1024>(a, stream);
+    return go<A, X, 4, 1024>(a, stream);
 }
 
 int launch_norm(const NormArgs &a, int dtype, int x_dtype, hipStream_t stream)

@@ -21,6 +21,57 @@ struct alignas(2 * N) Halves {
     uint32_t w[N / 2];
 };
 
+// N elements, at any alignment of T: one or two 16-byte accesses, which the
+// hardware takes at any address
+template <typename T, int N>
+struct __attribute__((packed, aligned(sizeof(T)))) Loose {
+    T e[N];
+};
+
+// its words, loaded and stored as whole vectors (a struct may be taken apart by
+// elements, and a branch's result then is, with a wait for it)
+template <typename T>
+using Words = uint32_t __attribute__((ext_vector_type(2 * sizeof(T))));
+template <typename T>
+using LooseWords = uint32_t __attribute__((ext_vector_type(2 * sizeof(T)), aligned(sizeof(T))));
+
+template <typename T>
+__device__ __forceinline__ Words<T> load_words(const T *p)
+{
+    return *(const LooseWords<T> *)p;
+}
+
+template <typename T>
+__device__ __forceinline__ Words<T> to_words(const Loose<T, 8> &r)
+{
+    Words<T> w;
+    __builtin_memcpy(&w, &r, sizeof(w));
+    return w;
+}
+
+template <typename T>
+__device__ __forceinline__ Loose<T, 8> from_words(const Words<T> &w)
+{
+    Loose<T, 8> r;
+    __builtin_memcpy(&r, &w, sizeof(r));
+    return r;
+}
+
+template <typename T>
+__device__ __forceinline__ void store_words(T *p, const Words<T> &w)
+{
+    *(LooseWords<T> *)p = w;
+}
+
+// A value whose address is the same in every lane and that no kernel of these
+// operators writes, read on the scalar side: a vector load would take a lane's
+// worth of work per wavefront and have its wait among those of the data.
+template <typename T>
+__device__ __forceinline__ T uniform_load(const T *p)
+{
+    return *(const __attribute__((address_space(4))) T *)p;
+}
+
 struct PlanArgs {
     int R, T, page_shift, n_free, max_pages;
     const int32_t *context_lens, *new_lens, *free_pages, *parents;
