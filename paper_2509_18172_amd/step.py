@@ -21,6 +21,7 @@ from . import (SBVR_BF16, SBVR_F16, SBVR_F32, CacheStruct, LogitsStruct, SBVRErr
 
 # These calls are short, and one step makes hundreds of them: the library's
 # functions are called without the wrappers of the same names.
+_empty = torch.empty_strided  # (half of torch.empty's time)
 _workspace_bytes = functools.lru_cache(maxsize=256)(sbvr_tree_attention_workspace_bytes)
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
@@ -75,9 +76,12 @@ class BatchPlan:
     [T] (bits of a uint64), used int32 [2] (pages taken, new tokens)."""
 
     def __init__(self, R: int, T: int, device):
-        self.query_start, self.token_request, self.positions, self.used = torch.empty(
-            R + 2 * T + 3, dtype=torch.int32, device=device).split((R + 1, T, T, 2))
-        self.slots, self.tree_mask = torch.empty((2, T), dtype=torch.int64, device=device).unbind(0)
+        self.query_start = _empty((R + 1,), (1,), dtype=torch.int32, device=device)
+        self.token_request = _empty((T,), (1,), dtype=torch.int32, device=device)
+        self.positions = torch.empty_like(self.token_request)
+        self.slots = _empty((T,), (1,), dtype=torch.int64, device=device)
+        self.tree_mask = torch.empty_like(self.slots)
+        self.used = _empty((2,), (1,), dtype=torch.int32, device=device)
 
 
 def batch_plan(context_lens, new_lens, free_pages, page_table, page_size: int, n_tokens: int, parents=None, out=None,
@@ -137,7 +141,7 @@ def _heads(t, heads, dim, cache, what):
     """The pointer and the token and head strides of a [T][heads][dim] tensor
     that goes with a cache."""
     token, head, one = t.stride()
-    if t.shape != (t.shape[0], heads, dim) or one != 1 or t.dtype != cache.dtype or t.device != cache.device:
+    if t.shape[1:] != (heads, dim) or one != 1 or t.dtype != cache.dtype or t.device != cache.device:
         raise AssertionError(f"{what} must be a {cache.dtype} tensor [tokens][{heads}][{dim}] with contiguous heads on "
                              "the cache's device")
     return t.data_ptr(), token, head
@@ -166,10 +170,10 @@ def tree_attention(q, cache: KVCache, page_table, context_lens, query_start, tre
     qp, q_token, q_head = _heads(q, H, cache.head_dim, cache, "q")
     table, max_pages, stride = _table(page_table, R, device)
     if out is None:
-        out = torch.empty((T, H, D), dtype=q.dtype, device=device)
+        out = _empty((T, H, D), (H * D, D, 1), dtype=q.dtype, device=device)
     need = _workspace_bytes(R, max_new, H, cache.kv_heads, D)
     if workspace is None and need:
-        workspace = torch.empty(need, dtype=torch.uint8, device=device)
+        workspace = _empty((need,), (1,), dtype=torch.uint8, device=device)
         if stream is not None:
             workspace.record_stream(stream)
     _check(_lib.sbvr_tree_attention(cache.address, R, T, H, qp, q_token, q_head, table, max_pages, stride,
@@ -189,28 +193,31 @@ def residual_norm(x, y=None, post_weight=None, gate=None, scale: float = 1.0, pr
     pre_weight for tokens x [T][H] (fp16, bf16 or fp32 stream), y [T][H] and
     gate [T][H] or [H] (fp16 or bf16); returns (x', h).  Without pre_weight h
     is None; without y x' is x itself.  x_out may be x."""
-    assert x.dim() == 2 and x.is_cuda and x.dtype in _DTYPE
     T, H = x.shape
     device = x.device
-    given = [t for t in (y, post_weight, gate, pre_weight, h_out) if t is not None]
-    dtype = given[0].dtype if given else x.dtype
-    assert dtype in _DTYPE, "y, gate, weights and h must be fp16 or bf16"
-    assert y is not None or (post_weight is None and gate is None), "a post_weight or a gate needs a y"
-    assert y is not None or x_out is None, "without a y there is no x' to write"
-    assert pre_weight is not None or h_out is None, "an h needs a pre_weight"
-    assert y is not None or pre_weight is not None, "nothing to compute: neither y nor pre_weight"
+    dtype = (y if y is not None else pre_weight if pre_weight is not None else x).dtype
+    assert x.is_cuda and x.dtype in _DTYPE and dtype in _DTYPE, "x must be a GPU tensor of fp16, bf16 or fp32"
     xp, x_stride = _rows(x, x.dtype, (T, H), device, "x")
-    yp, y_stride = (None, 0) if y is None else _rows(y, dtype, (T, H), device, "y")
-    if gate is None or gate.dim() == 1:
-        gp, g_stride = _dense(gate, dtype, (H,), device, "gate"), 0
+    op, o_stride, hp, h_stride, yp, y_stride, gp, g_stride = None, 0, None, 0, None, 0, None, 0
+    if y is None:
+        assert post_weight is None and gate is None and x_out is None, \
+            "post_weight, gate and x_out need a y"
+        assert pre_weight is not None, "nothing to compute: neither y nor pre_weight"
     else:
-        gp, g_stride = _rows(gate, dtype, (T, H), device, "gate")
-    op, o_stride, hp, h_stride = None, 0, None, 0
-    if y is not None:
-        x_out = torch.empty((T, H), dtype=x.dtype, device=device) if x_out is None else x_out
+        yp, y_stride = _rows(y, dtype, (T, H), device, "y")
+        if gate is not None:
+            if gate.dim() == 1:
+                gp = _dense(gate, dtype, (H,), device, "gate")
+            else:
+                gp, g_stride = _rows(gate, dtype, (T, H), device, "gate")
+        if x_out is None:
+            x_out = _empty((T, H), (H, 1), dtype=x.dtype, device=device)
         op, o_stride = _rows(x_out, x.dtype, (T, H), device, "x_out")
-    if pre_weight is not None:
-        h_out = torch.empty((T, H), dtype=dtype, device=device) if h_out is None else h_out
+    if pre_weight is None:
+        assert h_out is None, "an h needs a pre_weight"
+    else:
+        if h_out is None:
+            h_out = _empty((T, H), (H, 1), dtype=dtype, device=device)
         hp, h_stride = _rows(h_out, dtype, (T, H), device, "h_out")
     _check(_lib.sbvr_residual_norm(T, H, _DTYPE[dtype], _DTYPE[x.dtype], xp, x_stride, yp, y_stride,
                               _dense(post_weight, dtype, (H,), device, "post_weight"), gp, g_stride, float(scale),
@@ -234,11 +241,15 @@ def adjust_logits(logits, history=None, history_start=None, prompt_lens=None, re
     i32, f32 = torch.int32, torch.float32
     R = n_requests
     if R is None:
-        R = next((t.shape[0] - less for t, less in ((history_start, 1), (bias_start, 1), (query_start, 1),
-                                                    (prompt_lens, 0), (repetition, 0), (frequency, 0), (presence, 0),
-                                                    (temperature, 0)) if t is not None), T)
+        for per_request in (prompt_lens, repetition, frequency, presence, temperature):
+            if per_request is not None:
+                R = per_request.shape[0]
+                break
+        else:
+            starts = history_start if history_start is not None else bias_start if bias_start is not None else query_start
+            R = T if starts is None else starts.shape[0] - 1
     if out is None:
-        out = torch.empty((T, V), dtype=out_dtype or logits.dtype, device=device)
+        out = _empty((T, V), (V, 1), dtype=out_dtype or logits.dtype, device=device)
     assert out.dtype in _DTYPE and (out_dtype is None or out.dtype == out_dtype)
     assert (history is None) == (history_start is None), "history and history_start go together"
     assert (bias_tokens is None) == (bias_start is None) == (bias_values is None), "the three bias tensors go together"
