@@ -533,7 +533,18 @@ struct Rows {
 };
 
 // Uniform address of position p of a page plus a 32-bit lane offset is what
-// every load uses.
+// every load uses.  The offset is made opaque where it is used, or the compiler
+// widens it outside of the loop and adds 64-bit addresses per lane and load.
+__device__ __forceinline__ uint64_t lane_offset(uint32_t off)
+{
+    asm volatile("" : "+v"(off));
+    return off;
+}
+
+// Keeps loads that were written before it from being moved behind it: towards
+// their use, where they would no longer run under the work in between.
+__device__ __forceinline__ void issue_loads() { asm volatile("" ::: "memory"); }
+
 __device__ __forceinline__ const char *at_page(const void *base, int page, int p, int page_size, int64_t page_stride,
                                                uint32_t step)
 {
@@ -600,9 +611,10 @@ __global__ void __launch_bounds__(ATTN_THREADS, WGS) attn_rows_kernel(AttnArgs a
 #pragma unroll
                 for (int s = 0; s < DS; ++s) {
                     const uint32_t piece = 4 * s + 3 < pieces || 4 * s + g < pieces ? 4 * s + g : 0;
-                    kf[h][s] = *(const v4u *)(kp + (uint64_t)(k_lane + 16 * piece));
+                    kf[h][s] = *(const v4u *)(kp + lane_offset(k_lane + 16 * piece));
                 }
             }
+            issue_loads();
         };
         auto load_v = [&](int p0, const int *page) {
 #pragma unroll
@@ -610,12 +622,13 @@ __global__ void __launch_bounds__(ATTN_THREADS, WGS) attn_rows_kernel(AttnArgs a
                 const char *vp = at_page(vb, page[h], p0 + 16 * h, a.kv.page_size, a.kv.v_page_stride, v_step);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const Halves<DV> v = *(const Halves<DV> *)(vp + (uint64_t)(e * v_step) + (uint64_t)v_lane);
+                    const Halves<DV> v = *(const Halves<DV> *)(vp + (uint64_t)(e * v_step) + lane_offset(v_lane));
 #pragma unroll
                     for (int i = 0; i < DV / 2; ++i)
                         vr[4 * h + e][i] = v.w[i];
                 }
             }
+            issue_loads();
         };
         int page[2], next[2], after[2];
         auto pages_of = [&](int p0, int *id) {
@@ -644,8 +657,10 @@ __global__ void __launch_bounds__(ATTN_THREADS, WGS) attn_rows_kernel(AttnArgs a
             const bool masked = p0 + TILE > rq.ctx || (page[0] | page[1]) < 0;
             if (masked)
                 row.hide(p0, page[0] >= 0, page[1] >= 0, rq, s);
-            v4u pf[NT], vf[DV];
+            v4u pf[NT];
             row.weights(s, pf);
+            // operand i of the values: element DV c + i of the lane's eight rows
+            v4u vf[DV];
 #pragma unroll
             for (int i = 0; i < DV; ++i)
 #pragma unroll
@@ -779,22 +794,28 @@ __global__ void __launch_bounds__(ATTN_THREADS, WGS) attn_block_kernel(AttnArgs 
         const uint16_t *vb = (const uint16_t *)a.kv.v + it.kvh * a.kv.v_head_stride;
 
         v4u kin[LOADS], vin[LOADS];
-        // brings in the unit at p0 and says which of its four sixteens are there
-        auto load = [&](int p0) {
+        // the pages of the unit at p0's four sixteens
+        auto pages_of = [&](int p0, int (&id)[ATTN_WAVES]) {
+#pragma unroll
+            for (int w = 0; w < ATTN_WAVES; ++w)
+                id[w] = page_at(a, table, p0 + 16 * w, end, page_shift);
+        };
+        // brings in the unit at p0 and says which of its sixteens are there
+        auto load = [&](int p0, const int (&id)[ATTN_WAVES]) {
             int ok = 0, mine = -1;
 #pragma unroll
             for (int w = 0; w < ATTN_WAVES; ++w) {
-                const int id = page_at(a, table, p0 + 16 * w, end, page_shift);
-                ok |= (id >= 0) << w;
-                mine = w == wave ? id : mine;
+                ok |= (id[w] >= 0) << w;
+                mine = w == wave ? id[w] : mine;
             }
             const char *kp = at_page(kb, mine, p0 + 16 * wave, a.kv.page_size, a.kv.k_page_stride, k_step);
             const char *vp = at_page(vb, mine, p0 + 16 * wave, a.kv.page_size, a.kv.v_page_stride, v_step);
 #pragma unroll
             for (int i = 0; i < LOADS; ++i) {
-                kin[i] = *(const v4u *)(kp + (uint64_t)(i * LOAD_ROWS * k_step) + (uint64_t)k_lane);
-                vin[i] = *(const v4u *)(vp + (uint64_t)(i * LOAD_ROWS * v_step) + (uint64_t)v_lane);
+                kin[i] = *(const v4u *)(kp + (uint64_t)(i * LOAD_ROWS * k_step) + lane_offset(k_lane));
+                vin[i] = *(const v4u *)(vp + (uint64_t)(i * LOAD_ROWS * v_step) + lane_offset(v_lane));
             }
+            issue_loads();
             return ok;
         };
         auto store = [&](int buffer) {
@@ -808,14 +829,20 @@ __global__ void __launch_bounds__(ATTN_THREADS, WGS) attn_block_kernel(AttnArgs 
 
         Rows<DP, DS, NT, BF, true> row;
         row.begin(a, it, rows ? row0 : it.block * ROWS, rows, group);
-        int there = load(first), coming = 0;
+        // (a unit past the segment's end is the one before it once more)
+        auto next_unit = [&](int p0) { return p0 + UNIT < last ? p0 + UNIT : p0; };
+        int ids[ATTN_WAVES], ahead[ATTN_WAVES];
+        pages_of(first, ids);
+        pages_of(next_unit(first), ahead);
+        int there = load(first, ids), coming = 0;
         row.finish(a, rows);
         store(0);
-        if (first + UNIT < last)
-            coming = load(first + UNIT);
+        coming = load(next_unit(first), ahead);
         __syncthreads();
         int buffer = 0;
         for (int p0 = first; p0 < last; p0 += UNIT) {
+            const int p2 = next_unit(next_unit(p0));
+            pages_of(p2, ids);
 #pragma unroll 1
             for (int t = 0; t < UNIT / TILE; ++t) {
                 const int pt = p0 + t * TILE;
@@ -850,14 +877,11 @@ __global__ void __launch_bounds__(ATTN_THREADS, WGS) attn_block_kernel(AttnArgs 
                     });
                 row.products(pf, vf);
             }
-            if (p0 + UNIT < last) {
-                // the other buffer was last read before the barrier at the end
-                // of the step before
-                store(buffer ^ 1);
-                there = coming;
-                if (p0 + 2 * UNIT < last)
-                    coming = load(p0 + 2 * UNIT);
-            }
+            // the other buffer was last read before the barrier at the end of the
+            // step before
+            store(buffer ^ 1);
+            there = coming;
+            coming = load(p2, ids);
             buffer ^= 1;
             __syncthreads();
         }
@@ -899,17 +923,19 @@ __global__ void __launch_bounds__(ATTN_THREADS, WGS) attn_block_kernel(AttnArgs 
 
 constexpr int JOIN_WAVES = 4, JOIN_THREADS = 64 * JOIN_WAVES, JOIN_AHEAD = 4;
 
-// Joins the parts of a divided item: workgroup (i, y) takes JR rows of join i.
-// Its wavefronts share the parts and meet in LDS.  The first parts' sums are
-// loaded together with the maxima, so that one latency covers both; a CU brings
-// in no more than some ten bytes a cycle from other XCDs' results, so the rows
-// are spread over as many workgroups as is useful.
-template <int DP, int ROWS, bool BF, int SPLITS, int JR>
+// Joins the parts of a divided item (join i of workgroup (i, y)).  Few rows in
+// all: a workgroup has one row, its wavefronts share the parts and meet in LDS --
+// a CU brings in no more than some ten bytes a cycle of other XCDs' results, so
+// the rows are spread.  Many rows: a wavefront has four rows of its own.  The
+// first parts' sums are loaded together with the maxima, so that one latency
+// covers both.
+template <int DP, int ROWS, bool BF, int SPLITS, bool SPREAD>
 __global__ void __launch_bounds__(JOIN_THREADS) attn_join_kernel(AttnArgs a)
 {
-    static_assert(ROWS % JR == 0 && (JR == 1 || JR == 4), "whole row groups");
+    constexpr int JR = SPREAD ? 1 : 4, STEP = SPREAD ? JOIN_WAVES : 1;  // rows and parts of a wavefront's turn
+    static_assert(ROWS % (4 * JOIN_WAVES) == 0, "whole row groups");
     typedef float vrows __attribute__((ext_vector_type(JR)));
-    __shared__ float2 meet[JOIN_WAVES][JR][64];
+    __shared__ float2 meet[JOIN_WAVES][64];
     const Workspace<ROWS, DP, SPLITS> &ws = *(const Workspace<ROWS, DP, SPLITS> *)a.workspace;
     const Join j = ws.join[blockIdx.x];
     if (a.by_item) {
@@ -919,10 +945,10 @@ __global__ void __launch_bounds__(JOIN_THREADS) attn_join_kernel(AttnArgs a)
         if ((int)(blockIdx.x % blocks) >= row_blocks<ROWS>(a, q))
             return;
     }
-    const int i0 = blockIdx.y * JR, n = j.parts;
-    if (n == 0 || i0 >= j.rows)
-        return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int i0 = SPREAD ? blockIdx.y : (blockIdx.y * JOIN_WAVES + wave) * JR, turn = SPREAD ? wave : 0, n = j.parts;
+    if (n == 0 || i0 >= j.rows)  // (the same for the workgroup where it meets)
+        return;
     const Part<ROWS, DP> *parts = ws.part + 2 * j.range;
     auto part = [&](int k) -> const Part<ROWS, DP> & { return parts[k ? 2 * k : j.second]; };
     const int D = a.kv.head_dim, d = 2 * lane < D ? 2 * lane : 0;
@@ -933,9 +959,8 @@ __global__ void __launch_bounds__(JOIN_THREADS) attn_join_kernel(AttnArgs a)
     for (int k = 0; k < JOIN_AHEAD; ++k)
 #pragma unroll
         for (int r = 0; r < JR; ++r)
-            ahead[k][r] = wave + k * JOIN_WAVES < n
-                              ? *(const float2 *)&part(wave + k * JOIN_WAVES).o[i0 + r][d]
-                              : make_float2(0.f, 0.f);
+            ahead[k][r] = turn + k * STEP < n ? *(const float2 *)&part(turn + k * STEP).o[i0 + r][d]
+                                              : make_float2(0.f, 0.f);
     vrows top = NO_SCORE;
     for (int k = lane; k < n; k += 64) {
         const vrows m = *(const vrows *)&part(k).m[i0];
@@ -966,10 +991,10 @@ __global__ void __launch_bounds__(JOIN_THREADS) attn_join_kernel(AttnArgs a)
                                       __builtin_amdgcn_readlane(__builtin_bit_cast(int, (float)f[r]), k - k0));
         };
         const int k1 = min(n, k0 + 64);
-        int k = k0 + wave;
+        int k = k0 + turn;
         if (k0 == 0) {
 #pragma unroll
-            for (int i = 0; i < JOIN_AHEAD; ++i, k += JOIN_WAVES)
+            for (int i = 0; i < JOIN_AHEAD; ++i, k += STEP)
                 if (k < k1)
 #pragma unroll
                     for (int r = 0; r < JR; ++r) {
@@ -979,7 +1004,7 @@ __global__ void __launch_bounds__(JOIN_THREADS) attn_join_kernel(AttnArgs a)
                     }
         }
 #pragma unroll 4
-        for (; k < k1; k += JOIN_WAVES)
+        for (; k < k1; k += STEP)
 #pragma unroll
             for (int r = 0; r < JR; ++r) {
                 const float w = factor(r, k);
@@ -993,23 +1018,26 @@ __global__ void __launch_bounds__(JOIN_THREADS) attn_join_kernel(AttnArgs a)
 #pragma unroll
         for (int r = 0; r < JR; ++r)
             total[r] += __shfl_xor(total[r], s);
+    if constexpr (SPREAD) {
+        meet[wave][lane] = o[0];
+        __syncthreads();
+        if (wave != 0)
+            return;
 #pragma unroll
-    for (int r = 0; r < JR; ++r)
-        meet[wave][r][lane] = o[r];
-    __syncthreads();
+        for (int w = 1; w < JOIN_WAVES; ++w) {
+            o[0].x += meet[w][lane].x;
+            o[0].y += meet[w][lane].y;
+        }
+    }
+    if (2 * lane >= D)
+        return;
     const int group = a.heads / a.kv.kv_heads;
 #pragma unroll
     for (int r = 0; r < JR; ++r)
-        if (r % JOIN_WAVES == wave && i0 + r < j.rows && 2 * lane < D) {
-            float2 v = make_float2(0.f, 0.f);
-#pragma unroll
-            for (int w = 0; w < JOIN_WAVES; ++w) {
-                v.x += meet[w][r][lane].x;
-                v.y += meet[w][r][lane].y;
-            }
+        if (i0 + r < j.rows) {
             const float inv = inverse(total[r]);
             *(uint32_t *)(out_row(a, j.first, j.kvh, j.row0 + i0 + r, group) + 2 * lane) =
-                pack2<BF>(v.x * inv, v.y * inv);
+                pack2<BF>(o[r].x * inv, o[r].y * inv);
         }
 }
 
@@ -1027,10 +1055,14 @@ Shape shape_of(int max_new, int heads, int kv_heads)
     return rows <= 16 ? ROWS16 : rows <= 32 ? ROWS32 : rows <= 64 ? ROWS64 : ROWS128;
 }
 
-constexpr int WGS = 2;          // workgroups a CU, by registers
-constexpr int JOIN_MOST = 4096;         // workgroups beyond which a join takes four rows each
+// Workgroups a CU, by registers.  Narrow heads of few rows need few: four finish
+// 64 requests of up to 2047 positions, 64 wide, in 41 us, two in 45; at 8192
+// positions, where starting up counts less, 199 and 192 us.
+constexpr int wgs_of(Shape s, int dp) { return s == ROWS16 && dp == 64 ? 4 : 2; }
 
-template <int DP, int ROWS, bool BF>
+constexpr int JOIN_MOST = 4096;  // rows up to which a join has a workgroup for each
+
+template <int DP, int ROWS, bool BF, int WGS>
 int run_attn(const void *kernel, const AttnArgs &a, hipStream_t stream)
 {
     constexpr int SPLITS = WGS * CUS;
@@ -1047,20 +1079,21 @@ int run_attn(const void *kernel, const AttnArgs &a, hipStream_t stream)
         return st;
     const int joins = args.by_item ? (int)items : SPLITS - 1, most = min(rows, ROWS);  // the last range divides nothing
     if ((long long)joins * most <= JOIN_MOST)
-        return launch_kernel((const void *)attn_join_kernel<DP, ROWS, BF, SPLITS, 1>, dim3(joins, most),
+        return launch_kernel((const void *)attn_join_kernel<DP, ROWS, BF, SPLITS, true>, dim3(joins, most),
                              dim3(JOIN_THREADS), 0, stream, argv);
-    return launch_kernel((const void *)attn_join_kernel<DP, ROWS, BF, SPLITS, 4>, dim3(joins, (most + 3) / 4),
+    return launch_kernel((const void *)attn_join_kernel<DP, ROWS, BF, SPLITS, false>, dim3(joins, (most + 15) / 16),
                          dim3(JOIN_THREADS), 0, stream, argv);
 }
 
 template <int DP, int DS, bool BF>
 int by_shape(const AttnArgs &a, hipStream_t stream)
 {
+    constexpr int W = wgs_of(ROWS16, DP), V = wgs_of(ROWS128, DP);
     switch (shape_of(a.max_new, a.heads, a.kv.kv_heads)) {
-    case ROWS16: return run_attn<DP, 16, BF>((const void *)attn_rows_kernel<DP, DS, 1, BF, WGS>, a, stream);
-    case ROWS32: return run_attn<DP, 32, BF>((const void *)attn_rows_kernel<DP, DS, 2, BF, WGS>, a, stream);
-    case ROWS64: return run_attn<DP, 64, BF>((const void *)attn_block_kernel<DP, DS, 1, BF, WGS>, a, stream);
-    default: return run_attn<DP, 128, BF>((const void *)attn_block_kernel<DP, DS, 2, BF, WGS>, a, stream);
+    case ROWS16: return run_attn<DP, 16, BF, W>((const void *)attn_rows_kernel<DP, DS, 1, BF, W>, a, stream);
+    case ROWS32: return run_attn<DP, 32, BF, V>((const void *)attn_rows_kernel<DP, DS, 2, BF, V>, a, stream);
+    case ROWS64: return run_attn<DP, 64, BF, V>((const void *)attn_block_kernel<DP, DS, 1, BF, V>, a, stream);
+    default: return run_attn<DP, 128, BF, V>((const void *)attn_block_kernel<DP, DS, 2, BF, V>, a, stream);
     }
 }
 
@@ -1074,10 +1107,10 @@ template <int DP>
 size_t workspace_of(Shape s)
 {
     switch (s) {
-    case ROWS16: return sizeof(Workspace<16, DP, WGS * CUS>);
-    case ROWS32: return sizeof(Workspace<32, DP, WGS * CUS>);
-    case ROWS64: return sizeof(Workspace<64, DP, WGS * CUS>);
-    default: return sizeof(Workspace<128, DP, WGS * CUS>);
+    case ROWS16: return sizeof(Workspace<16, DP, wgs_of(ROWS16, DP) * CUS>);
+    case ROWS32: return sizeof(Workspace<32, DP, wgs_of(ROWS32, DP) * CUS>);
+    case ROWS64: return sizeof(Workspace<64, DP, wgs_of(ROWS64, DP) * CUS>);
+    default: return sizeof(Workspace<128, DP, wgs_of(ROWS128, DP) * CUS>);
     }
 }
 
