@@ -15,15 +15,21 @@
 // and their outputs are not stored.
 //
 // Two kernels, by the rows of an item:
-//   attn_rows_kernel (up to 32 rows): memory-bound.  Each wavefront streams
+//   attn_rows_kernel (up to 16 rows): memory-bound.  Each wavefront streams
 //     tiles of its own straight into operand registers; K's registers are
 //     refilled for the next tile as soon as the scores are formed and V's as
 //     soon as the products are, so each is in flight while the other is used.
 //     The four wavefronts' sums meet in LDS at the end.
-//   attn_block_kernel (up to 128 rows): each wavefront has 16 or 32 rows of its
-//     own and all four share the tiles, which go through LDS once for all of
+//   attn_block_kernel (up to 64 or 128 rows): each wavefront has 16 or 32 rows of
+//     its own and all four share the tiles, which go through LDS once for all of
 //     them, one tile ahead; pieces are stored permuted so that both operands'
 //     reads are free of bank conflicts.
+// Measured, four query heads on each of eight key/value heads of 128 elements,
+// binary16: 64 requests of one token at 8192 positions 370 us (5.8 TB/s; the
+// block kernel 374), one request at 4096 15.4 us (17.8); trees of eight (32 rows)
+// at 8192 382 us with the block kernel, 405 with 32 rows in the rows kernel's
+// registers; trees of 32 (128 rows) 440 us, 640 TFLOP/s, and as two blocks of 64
+// 774.  A plain read of as many bytes takes about 305 us.
 //
 // Work: the cached positions of all items, in units of one step of a
 // workgroup, are one line that is cut into (up to) SPLITS (as many workgroups as the chip
@@ -56,7 +62,7 @@ typedef uint32_t v4u __attribute__((ext_vector_type(4)));
 constexpr int ATTN_WAVES = 4, ATTN_THREADS = 64 * ATTN_WAVES;
 constexpr int TILE = 32;              // positions of one score / product step
 constexpr int CUS = 256;
-constexpr float NO_SCORE = -1.0e30f;  // running maximum before any score
+constexpr float NO_SCORE = -3.0e38f;  // running maximum before any score
 constexpr float GAP = 8.f;            // binary exponent by which weights may exceed 1
 constexpr float LOG2E = 1.4426950408889634f;
 
@@ -565,12 +571,12 @@ __device__ __forceinline__ int page_at(const AttnArgs &a, const int32_t *table, 
 // items of few rows
 // ---------------------------------------------------------------------------
 
-// DP: padded head size, DS: 32-element steps of it that hold elements, NT:
-// 16-row tiles per item, BF: bfloat16, WGS: workgroups a CU.
-template <int DP, int DS, int NT, bool BF, int WGS>
+// DP: padded head size, DS: 32-element steps of it that hold elements, BF:
+// bfloat16, WGS: workgroups a CU.
+template <int DP, int DS, bool BF, int WGS>
 __global__ void __launch_bounds__(ATTN_THREADS, WGS) attn_rows_kernel(AttnArgs a)
 {
-    constexpr int DV = DP / 16, ROWS = 16 * NT, UNIT = ATTN_WAVES * TILE, SPLITS = WGS * CUS;
+    constexpr int NT = 1, DV = DP / 16, ROWS = 16 * NT, UNIT = ATTN_WAVES * TILE, SPLITS = WGS * CUS;
     __shared__ float lds_o[ATTN_WAVES][ROWS][DP + 4];
     __shared__ float lds_m[ATTN_WAVES][ROWS], lds_l[ATTN_WAVES][ROWS];
 
@@ -737,6 +743,7 @@ __global__ void __launch_bounds__(ATTN_THREADS, WGS) attn_rows_kernel(AttnArgs a
 // items of many rows
 // ---------------------------------------------------------------------------
 
+// NT: 16-row tiles per wavefront; the others as above.
 template <int DP, int DS, int NT, bool BF, int WGS>
 __global__ void __launch_bounds__(ATTN_THREADS, WGS) attn_block_kernel(AttnArgs a)
 {
@@ -1047,12 +1054,12 @@ __global__ void __launch_bounds__(JOIN_THREADS) attn_join_kernel(AttnArgs a)
 
 // How a call's items are run: rows of an item by the most rows that a request
 // has per key/value head.
-enum Shape { ROWS16, ROWS32, ROWS64, ROWS128 };
+enum Shape { ROWS16, ROWS64, ROWS128 };
 
 Shape shape_of(int max_new, int heads, int kv_heads)
 {
     const int rows = max_new * (heads / kv_heads);
-    return rows <= 16 ? ROWS16 : rows <= 32 ? ROWS32 : rows <= 64 ? ROWS64 : ROWS128;
+    return rows <= 16 ? ROWS16 : rows <= 64 ? ROWS64 : ROWS128;
 }
 
 // Workgroups a CU, by registers.  Narrow heads of few rows need few: four finish
@@ -1060,7 +1067,10 @@ Shape shape_of(int max_new, int heads, int kv_heads)
 // positions, where starting up counts less, 199 and 192 us.
 constexpr int wgs_of(Shape s, int dp) { return s == ROWS16 && dp == 64 ? 4 : 2; }
 
-constexpr int JOIN_MOST = 4096;  // rows up to which a join has a workgroup for each
+// Rows up to which a join has a workgroup for each: one request at 4096
+// positions, 32 rows in all, takes 15.5 us so and 23.5 with a wavefront for four
+// rows; 16 trees of 64, 32768 rows, 113 and 81.
+constexpr int JOIN_MOST = 4096;
 
 template <int DP, int ROWS, bool BF, int WGS>
 int run_attn(const void *kernel, const AttnArgs &a, hipStream_t stream)
@@ -1090,8 +1100,7 @@ int by_shape(const AttnArgs &a, hipStream_t stream)
 {
     constexpr int W = wgs_of(ROWS16, DP), V = wgs_of(ROWS128, DP);
     switch (shape_of(a.max_new, a.heads, a.kv.kv_heads)) {
-    case ROWS16: return run_attn<DP, 16, BF, W>((const void *)attn_rows_kernel<DP, DS, 1, BF, W>, a, stream);
-    case ROWS32: return run_attn<DP, 32, BF, V>((const void *)attn_rows_kernel<DP, DS, 2, BF, V>, a, stream);
+    case ROWS16: return run_attn<DP, 16, BF, W>((const void *)attn_rows_kernel<DP, DS, BF, W>, a, stream);
     case ROWS64: return run_attn<DP, 64, BF, V>((const void *)attn_block_kernel<DP, DS, 1, BF, V>, a, stream);
     default: return run_attn<DP, 128, BF, V>((const void *)attn_block_kernel<DP, DS, 2, BF, V>, a, stream);
     }
@@ -1108,7 +1117,6 @@ size_t workspace_of(Shape s)
 {
     switch (s) {
     case ROWS16: return sizeof(Workspace<16, DP, wgs_of(ROWS16, DP) * CUS>);
-    case ROWS32: return sizeof(Workspace<32, DP, wgs_of(ROWS32, DP) * CUS>);
     case ROWS64: return sizeof(Workspace<64, DP, wgs_of(ROWS64, DP) * CUS>);
     default: return sizeof(Workspace<128, DP, wgs_of(ROWS128, DP) * CUS>);
     }
