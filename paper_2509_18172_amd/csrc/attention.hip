@@ -279,27 +279,6 @@ __device__ __forceinline__ int most_blocks(const AttnArgs &a)
     return (a.max_new * (a.heads / a.kv.kv_heads) + ROWS - 1) / ROWS;
 }
 
-// End of a workgroup's segment [u, stop) of an item (called by one thread).
-template <int ROWS, int SPLITS>
-__device__ __forceinline__ void note_join(const AttnArgs &a, const Cuts<SPLITS> &cuts, const Item &it, int u, int stop,
-                                          int u0, int u1, Join *join)
-{
-    const bool begins = u == it.start, divided = begins && stop < it.start + it.units;
-    if (a.by_item ? !begins : stop < u1)
-        return;
-    Join j = {};
-    if (divided) {
-        j.range = blockIdx.x;
-        j.parts = cuts.holder(it.start + it.units - 1) - j.range + 1;
-        j.second = u != u0;
-        j.row0 = it.block * ROWS;
-        j.rows = min(it.rq.n * (a.heads / a.kv.kv_heads) - j.row0, ROWS);
-        j.first = it.rq.first;
-        j.kvh = it.kvh;
-    }
-    join[a.by_item ? (it.r * a.kv.kv_heads + it.kvh) * most_blocks<ROWS>(a) + it.block : blockIdx.x] = j;
-}
-
 __device__ __forceinline__ uint16_t *out_row(const AttnArgs &a, int first, int kvh, int row, int group)
 {
     const int tok = first + row / group, head = kvh * group + row % group;
@@ -567,6 +546,60 @@ __device__ __forceinline__ int page_at(const AttnArgs &a, const int32_t *table, 
     return p < end && id < a.kv.n_pages ? max(id, -1) : -1;
 }
 
+// A workgroup's part [u, stop) of an item: the item's rows from row0 on, the
+// positions first .. last - 1 of its end, and where its pages and its head lie.
+struct Segment {
+    Item it;
+    int u, stop, row0, rows, first, last, end;
+    const int32_t *table;
+    const uint16_t *k, *v;
+};
+
+template <int ROWS, int UNIT>
+__device__ __forceinline__ Segment segment_at(const Line<ROWS, UNIT> &line, const AttnArgs &a, int u, int u1)
+{
+    Segment s;
+    s.it = line.item_at(u);
+    s.u = u;
+    s.stop = min(u1, s.it.start + s.it.units);
+    s.row0 = s.it.block * ROWS;
+    s.rows = min(s.it.rq.n * (a.heads / a.kv.kv_heads) - s.row0, ROWS);
+    s.end = s.it.rq.ctx + s.it.rq.n;
+    s.first = (u - s.it.start) * UNIT;
+    s.last = min((s.stop - s.it.start) * UNIT, s.end);
+    s.table = a.page_table + s.it.r * a.table_stride;
+    s.k = (const uint16_t *)a.kv.k + s.it.kvh * a.kv.k_head_stride;
+    s.v = (const uint16_t *)a.kv.v + s.it.kvh * a.kv.v_head_stride;
+    return s;
+}
+
+__device__ __forceinline__ bool is_whole(const Segment &s)
+{
+    return s.u == s.it.start && s.stop == s.it.start + s.it.units;
+}
+
+// End of a workgroup's segment (called by one thread).
+template <int ROWS, int SPLITS>
+__device__ __forceinline__ void note_join(const AttnArgs &a, const Cuts<SPLITS> &cuts, const Segment &s, int u0, int u1,
+                                          Join *join)
+{
+    const Item &it = s.it;
+    const bool begins = s.u == it.start, divided = begins && s.stop < it.start + it.units;
+    if (a.by_item ? !begins : s.stop < u1)
+        return;
+    Join j = {};
+    if (divided) {
+        j.range = blockIdx.x;
+        j.parts = cuts.holder(it.start + it.units - 1) - j.range + 1;
+        j.second = s.u != u0;
+        j.row0 = s.row0;
+        j.rows = s.rows;
+        j.first = it.rq.first;
+        j.kvh = it.kvh;
+    }
+    join[a.by_item ? (it.r * a.kv.kv_heads + it.kvh) * most_blocks<ROWS>(a) + it.block : blockIdx.x] = j;
+}
+
 // ---------------------------------------------------------------------------
 // items of few rows
 // ---------------------------------------------------------------------------
@@ -597,69 +630,67 @@ __global__ void __launch_bounds__(ATTN_THREADS, WGS) attn_rows_kernel(AttnArgs a
     const uint32_t k_step = 2 * (uint32_t)a.kv.k_token_stride, v_step = 2 * (uint32_t)a.kv.v_token_stride;
     const uint32_t k_lane = c * k_step, v_lane = 4 * g * v_step + 2 * (DV * c < D ? DV * c : 0);
 
-    for (int u = u0; u < u1;) {
-        const Item it = line.item_at(u);
-        const Request &rq = it.rq;
-        const int row0 = it.block * ROWS, rows = min(rq.n * group - row0, ROWS), end = rq.ctx + rq.n;
-        const int stop = min(u1, it.start + it.units);
-        const bool whole = u == it.start && stop == it.start + it.units;
-        const int first = (u - it.start) * UNIT + wave * TILE, last = min((stop - it.start) * UNIT, end);
-        const int32_t *table = a.page_table + it.r * a.table_stride;
-        const uint16_t *kb = (const uint16_t *)a.kv.k + it.kvh * a.kv.k_head_stride;
-        const uint16_t *vb = (const uint16_t *)a.kv.v + it.kvh * a.kv.v_head_stride;
-
-        v4u kf[2][DS];
-        uint32_t vr[8][DV / 2];
-        auto load_k = [&](int p0, const int *page) {
+    v4u kf[2][DS];
+    uint32_t vr[8][DV / 2];
+    auto load_k = [&](const Segment &sg, int p0, const int *page) {
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const char *kp = at_page(kb, page[h], p0 + 16 * h, a.kv.page_size, a.kv.k_page_stride, k_step);
+        for (int h = 0; h < 2; ++h) {
+            const char *kp = at_page(sg.k, page[h], p0 + 16 * h, a.kv.page_size, a.kv.k_page_stride, k_step);
 #pragma unroll
-                for (int s = 0; s < DS; ++s) {
-                    const uint32_t piece = 4 * s + 3 < pieces || 4 * s + g < pieces ? 4 * s + g : 0;
-                    kf[h][s] = *(const v4u *)(kp + lane_offset(k_lane + 16 * piece));
-                }
+            for (int s = 0; s < DS; ++s) {
+                const uint32_t piece = 4 * s + 3 < pieces || 4 * s + g < pieces ? 4 * s + g : 0;
+                kf[h][s] = *(const v4u *)(kp + lane_offset(k_lane + 16 * piece));
             }
-            issue_loads();
-        };
-        auto load_v = [&](int p0, const int *page) {
+        }
+        issue_loads();
+    };
+    auto load_v = [&](const Segment &sg, int p0, const int *page) {
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const char *vp = at_page(vb, page[h], p0 + 16 * h, a.kv.page_size, a.kv.v_page_stride, v_step);
+        for (int h = 0; h < 2; ++h) {
+            const char *vp = at_page(sg.v, page[h], p0 + 16 * h, a.kv.page_size, a.kv.v_page_stride, v_step);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const Halves<DV> v = *(const Halves<DV> *)(vp + (uint64_t)(e * v_step) + lane_offset(v_lane));
+            for (int e = 0; e < 4; ++e) {
+                const Halves<DV> v = *(const Halves<DV> *)(vp + (uint64_t)(e * v_step) + lane_offset(v_lane));
 #pragma unroll
-                    for (int i = 0; i < DV / 2; ++i)
-                        vr[4 * h + e][i] = v.w[i];
-                }
+                for (int i = 0; i < DV / 2; ++i)
+                    vr[4 * h + e][i] = v.w[i];
             }
-            issue_loads();
-        };
-        int page[2], next[2], after[2];
-        auto pages_of = [&](int p0, int *id) {
-            id[0] = page_at(a, table, p0, end, page_shift);
-            id[1] = page_at(a, table, p0 + 16, end, page_shift);
-        };
-        // a tile past the segment's end is the one before it once more
-        auto next_tile = [&](int p0) { return p0 + UNIT < last ? p0 + UNIT : p0; };
-        Rows<DP, DS, NT, BF, false> row;
-        row.begin(a, it, row0, rows, group);
+        }
+        issue_loads();
+    };
+    int page[2], next[2], after[2];
+    auto pages_of = [&](const Segment &sg, int p0, int *id) {
+        id[0] = page_at(a, sg.table, p0, sg.end, page_shift);
+        id[1] = page_at(a, sg.table, p0 + 16, sg.end, page_shift);
+    };
+    // a tile past the segment's end is the one before it once more
+    auto next_tile = [](const Segment &sg, int p0) { return p0 + UNIT < sg.last ? p0 + UNIT : p0; };
+    Rows<DP, DS, NT, BF, false> row;
+    // sends off a segment's first loads
+    auto open = [&](int u) {
+        const Segment sg = segment_at(line, a, u, u1);
+        row.begin(a, sg.it, sg.row0, sg.rows, group);
         // (a wavefront without a tile loads one too)
-        const int start = min(first, (last - 1) & ~(TILE - 1));
-        pages_of(start, page);
-        pages_of(next_tile(start), next);
-        load_k(start, page);
-        load_v(start, page);
-        row.finish(a, rows);
-        for (int p0 = first; p0 < last; p0 += UNIT) {
+        const int start = min(sg.first + wave * TILE, (sg.last - 1) & ~(TILE - 1));
+        pages_of(sg, start, page);
+        pages_of(sg, next_tile(sg, start), next);
+        load_k(sg, start, page);
+        load_v(sg, start, page);
+        return sg;
+    };
+
+    Segment seg = open(u0);
+    for (;;) {
+        const Request &rq = seg.it.rq;
+        row.finish(a, seg.rows);
+        for (int p0 = seg.first + wave * TILE; p0 < seg.last; p0 += UNIT) {
             // no branch around the loads, so that their counters stay exact: the
             // last tile is loaded once more, from L2, and not used
-            const int pn = next_tile(p0);
-            pages_of(next_tile(pn), after);
+            const int pn = next_tile(seg, p0);
+            pages_of(seg, next_tile(seg, pn), after);
             v4f s[NT][2];
             row.scores(kf, s);
-            load_k(pn, next);
+            load_k(seg, pn, next);
             const bool masked = p0 + TILE > rq.ctx || (page[0] | page[1]) < 0;
             if (masked)
                 row.hide(p0, page[0] >= 0, page[1] >= 0, rq, s);
@@ -676,10 +707,10 @@ __global__ void __launch_bounds__(ATTN_THREADS, WGS) attn_rows_kernel(AttnArgs a
             if (__builtin_expect(masked && row.hide_values(p0, page[0] >= 0, page[1] >= 0, rq, vf), 0))
                 row.odd_products(p0, page[0] >= 0, page[1] >= 0, a, rq, pf, vf, [&](int p) {
                     const int id = p - p0 < 16 ? page[0] : page[1];
-                    return (const uint16_t *)at_page(vb, id, p, a.kv.page_size, a.kv.v_page_stride, v_step);
+                    return (const uint16_t *)at_page(seg.v, id, p, a.kv.page_size, a.kv.v_page_stride, v_step);
                 });
             row.products(pf, vf);
-            load_v(pn, next);
+            load_v(seg, pn, next);
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 page[h] = next[h];
@@ -687,7 +718,11 @@ __global__ void __launch_bounds__(ATTN_THREADS, WGS) attn_rows_kernel(AttnArgs a
             }
         }
 
-        // the wavefronts' parts meet in LDS
+        // the wavefronts' parts meet in LDS, under the next segment's first loads
+        const Segment done = seg;
+        const bool more = done.stop < u1, whole = is_whole(done);
+        if (more)
+            seg = open(done.stop);
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
             if (g == 0) {
@@ -702,9 +737,9 @@ __global__ void __launch_bounds__(ATTN_THREADS, WGS) attn_rows_kernel(AttnArgs a
         }
         __syncthreads();
         if (threadIdx.x == 0)
-            note_join<ROWS>(a, cuts, it, u, stop, u0, u1, ws.join);
-        Part<ROWS, DP> &part = ws.part[2 * blockIdx.x + (u != u0)];
-        for (int i = wave; i < rows; i += ATTN_WAVES) {
+            note_join<ROWS>(a, cuts, done, u0, u1, ws.join);
+        Part<ROWS, DP> &part = ws.part[2 * blockIdx.x + (done.u != u0)];
+        for (int i = wave; i < done.rows; i += ATTN_WAVES) {
             float top = NO_SCORE;
 #pragma unroll
             for (int w = 0; w < ATTN_WAVES; ++w)
@@ -728,14 +763,15 @@ __global__ void __launch_bounds__(ATTN_THREADS, WGS) attn_rows_kernel(AttnArgs a
                     o1 += f[w] * lds_o[w][i][2 * lane + 1];
                 }
                 if (whole)
-                    *(uint32_t *)(out_row(a, rq.first, it.kvh, row0 + i, group) + 2 * lane) =
+                    *(uint32_t *)(out_row(a, done.it.rq.first, done.it.kvh, done.row0 + i, group) + 2 * lane) =
                         pack2<BF>(o0 * inv, o1 * inv);
                 else
                     *(float2 *)&part.o[i][2 * lane] = make_float2(o0, o1);
             }
         }
+        if (!more)
+            break;
         __syncthreads();
-        u = stop;
     }
 }
 
@@ -788,72 +824,72 @@ __global__ void __launch_bounds__(ATTN_THREADS, WGS) attn_block_kernel(AttnArgs 
     const uint32_t k_read = c * ROW_BYTES + 16 * (g ^ swap(c));
     const uint32_t v_read = v_row * ROW_BYTES + 16 * (((c & 3) >> 1) ^ swap(v_row)) + 8 * (c & 1);
 
-    for (int u = u0; u < u1;) {
-        const Item it = line.item_at(u);
-        const Request &rq = it.rq;
-        const int row0 = it.block * ROWS + wave * WROWS, rows = min(max(rq.n * group - row0, 0), WROWS);
-        const int end = rq.ctx + rq.n;
-        const int stop = min(u1, it.start + it.units);
-        const bool whole = u == it.start && stop == it.start + it.units;
-        const int first = (u - it.start) * UNIT, last = min((stop - it.start) * UNIT, end);
-        const int32_t *table = a.page_table + it.r * a.table_stride;
-        const uint16_t *kb = (const uint16_t *)a.kv.k + it.kvh * a.kv.k_head_stride;
-        const uint16_t *vb = (const uint16_t *)a.kv.v + it.kvh * a.kv.v_head_stride;
+    v4u kin[LOADS], vin[LOADS];
+    int ids[ATTN_WAVES], ahead[ATTN_WAVES];
+    // the pages of the unit at p0's four sixteens
+    auto pages_of = [&](const Segment &sg, int p0, int (&id)[ATTN_WAVES]) {
+#pragma unroll
+        for (int w = 0; w < ATTN_WAVES; ++w)
+            id[w] = page_at(a, sg.table, p0 + 16 * w, sg.end, page_shift);
+    };
+    // brings in the unit at p0 and says which of its sixteens are there
+    auto load = [&](const Segment &sg, int p0, const int (&id)[ATTN_WAVES]) {
+        int ok = 0, mine = -1;
+#pragma unroll
+        for (int w = 0; w < ATTN_WAVES; ++w) {
+            ok |= (id[w] >= 0) << w;
+            mine = w == wave ? id[w] : mine;
+        }
+        const char *kp = at_page(sg.k, mine, p0 + 16 * wave, a.kv.page_size, a.kv.k_page_stride, k_step);
+        const char *vp = at_page(sg.v, mine, p0 + 16 * wave, a.kv.page_size, a.kv.v_page_stride, v_step);
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            kin[i] = *(const v4u *)(kp + (uint64_t)(i * LOAD_ROWS * k_step) + lane_offset(k_lane));
+            vin[i] = *(const v4u *)(vp + (uint64_t)(i * LOAD_ROWS * v_step) + lane_offset(v_lane));
+        }
+        issue_loads();
+        return ok;
+    };
+    auto store = [&](int buffer) {
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            const int r = 16 * wave + i * LOAD_ROWS + load_row;
+            tile[buffer][0][r][load_piece ^ swap(r)] = kin[i];
+            tile[buffer][1][r][load_piece ^ swap(r)] = vin[i];
+        }
+    };
+    // (a unit past the segment's end is the one before it once more)
+    auto next_unit = [](const Segment &sg, int p0) { return p0 + UNIT < sg.last ? p0 + UNIT : p0; };
+    Rows<DP, DS, NT, BF, true> row;
+    int there = 0, coming = 0;
+    // the wavefront's own rows of a segment's
+    auto my_rows = [&](const Segment &sg) { return min(max(sg.rows - wave * WROWS, 0), WROWS); };
+    // sends off a segment's first loads
+    auto open = [&](int u) {
+        const Segment sg = segment_at(line, a, u, u1);
+        row.begin(a, sg.it, sg.row0 + (my_rows(sg) ? wave * WROWS : 0), my_rows(sg), group);
+        pages_of(sg, sg.first, ids);
+        pages_of(sg, next_unit(sg, sg.first), ahead);
+        there = load(sg, sg.first, ids);
+        return sg;
+    };
 
-        v4u kin[LOADS], vin[LOADS];
-        // the pages of the unit at p0's four sixteens
-        auto pages_of = [&](int p0, int (&id)[ATTN_WAVES]) {
-#pragma unroll
-            for (int w = 0; w < ATTN_WAVES; ++w)
-                id[w] = page_at(a, table, p0 + 16 * w, end, page_shift);
-        };
-        // brings in the unit at p0 and says which of its sixteens are there
-        auto load = [&](int p0, const int (&id)[ATTN_WAVES]) {
-            int ok = 0, mine = -1;
-#pragma unroll
-            for (int w = 0; w < ATTN_WAVES; ++w) {
-                ok |= (id[w] >= 0) << w;
-                mine = w == wave ? id[w] : mine;
-            }
-            const char *kp = at_page(kb, mine, p0 + 16 * wave, a.kv.page_size, a.kv.k_page_stride, k_step);
-            const char *vp = at_page(vb, mine, p0 + 16 * wave, a.kv.page_size, a.kv.v_page_stride, v_step);
-#pragma unroll
-            for (int i = 0; i < LOADS; ++i) {
-                kin[i] = *(const v4u *)(kp + (uint64_t)(i * LOAD_ROWS * k_step) + lane_offset(k_lane));
-                vin[i] = *(const v4u *)(vp + (uint64_t)(i * LOAD_ROWS * v_step) + lane_offset(v_lane));
-            }
-            issue_loads();
-            return ok;
-        };
-        auto store = [&](int buffer) {
-#pragma unroll
-            for (int i = 0; i < LOADS; ++i) {
-                const int r = 16 * wave + i * LOAD_ROWS + load_row;
-                tile[buffer][0][r][load_piece ^ swap(r)] = kin[i];
-                tile[buffer][1][r][load_piece ^ swap(r)] = vin[i];
-            }
-        };
-
-        Rows<DP, DS, NT, BF, true> row;
-        row.begin(a, it, rows ? row0 : it.block * ROWS, rows, group);
-        // (a unit past the segment's end is the one before it once more)
-        auto next_unit = [&](int p0) { return p0 + UNIT < last ? p0 + UNIT : p0; };
-        int ids[ATTN_WAVES], ahead[ATTN_WAVES];
-        pages_of(first, ids);
-        pages_of(next_unit(first), ahead);
-        int there = load(first, ids), coming = 0;
+    Segment seg = open(u0);
+    for (;;) {
+        const Request &rq = seg.it.rq;
+        const int rows = my_rows(seg);
         row.finish(a, rows);
         store(0);
-        coming = load(next_unit(first), ahead);
+        coming = load(seg, next_unit(seg, seg.first), ahead);
         __syncthreads();
         int buffer = 0;
-        for (int p0 = first; p0 < last; p0 += UNIT) {
-            const int p2 = next_unit(next_unit(p0));
-            pages_of(p2, ids);
+        for (int p0 = seg.first; p0 < seg.last; p0 += UNIT) {
+            const int p2 = next_unit(seg, next_unit(seg, p0));
+            pages_of(seg, p2, ids);
 #pragma unroll 1
             for (int t = 0; t < UNIT / TILE; ++t) {
                 const int pt = p0 + t * TILE;
-                if (pt >= end || rows == 0)
+                if (pt >= seg.end || rows == 0)
                     continue;
                 const char *keys = (const char *)tile[buffer][0][t * TILE], *values = (const char *)tile[buffer][1][t * TILE];
                 v4u kf[2][DS];
@@ -879,7 +915,7 @@ __global__ void __launch_bounds__(ATTN_THREADS, WGS) attn_block_kernel(AttnArgs 
                 row.weights(s, pf);
                 if (__builtin_expect(masked && row.hide_values(pt, ok0, ok1, rq, vf), 0))
                     row.odd_products(pt, ok0, ok1, a, rq, pf, vf, [&](int p) {
-                        return (const uint16_t *)at_page(vb, table[p >> page_shift], p, a.kv.page_size,
+                        return (const uint16_t *)at_page(seg.v, seg.table[p >> page_shift], p, a.kv.page_size,
                                                          a.kv.v_page_stride, v_step);
                     });
                 row.products(pf, vf);
@@ -888,14 +924,19 @@ __global__ void __launch_bounds__(ATTN_THREADS, WGS) attn_block_kernel(AttnArgs 
             // step before
             store(buffer ^ 1);
             there = coming;
-            coming = load(p2, ids);
+            coming = load(seg, p2, ids);
             buffer ^= 1;
             __syncthreads();
         }
 
+        // the segment's results leave under the next one's first loads
+        const Segment done = seg;
+        const bool more = done.stop < u1, whole = is_whole(done);
+        if (more)
+            seg = open(done.stop);
         if (threadIdx.x == 0)
-            note_join<ROWS>(a, cuts, it, u, stop, u0, u1, ws.join);
-        Part<ROWS, DP> &part = ws.part[2 * blockIdx.x + (u != u0)];
+            note_join<ROWS>(a, cuts, done, u0, u1, ws.join);
+        Part<ROWS, DP> &part = ws.part[2 * blockIdx.x + (done.u != u0)];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
             const float total = row.sum[nt][0], inv = inverse(total);
@@ -906,7 +947,7 @@ __global__ void __launch_bounds__(ATTN_THREADS, WGS) attn_block_kernel(AttnArgs 
                 part.m[wave * WROWS + i] = row.m[nt];
                 part.l[wave * WROWS + i] = total;
             }
-            uint16_t *out = out_row(a, rq.first, it.kvh, row0 + i, group);
+            uint16_t *out = out_row(a, done.it.rq.first, done.it.kvh, done.row0 + wave * WROWS + i, group);
 #pragma unroll
             for (int q = 0; q < DV; ++q) {
                 const int d = 16 * q + 4 * g;
@@ -920,7 +961,8 @@ __global__ void __launch_bounds__(ATTN_THREADS, WGS) attn_block_kernel(AttnArgs 
                     *(v4f *)&part.o[wave * WROWS + i][d] = o;
             }
         }
-        u = stop;
+        if (!more)
+            break;
     }
 }
 
