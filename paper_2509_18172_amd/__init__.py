@@ -579,6 +579,15 @@ def algorithmic_bytes(O: int, I: int, k: int, B: int = 1) -> int:
     return k * O * I // 8 + 2 * k * O * I // GROUP + 2 * I * B + 2 * O * B
 
 
-# the operators between the products of a step
-from .step import (BatchPlan, KVCache, adjust_logits, batch_plan, cache_write, residual_norm,  # noqa: E402,F401
-                   tree_attention)
+
+# The operators between the products of a step (step.py), loaded with their
+# native binding at first use: the functions above need neither it nor torch.
+_STEP = ("BatchPlan", "KVCache", "adjust_logits", "batch_plan", "cache_write", "residual_norm", "tree_attention")
+
+
+def __getattr__(name: str):
+    if name not in _STEP:
+        raise AttributeError(f"module {__name__!r} has no attribute {name!r}")
+    from . import step
+    globals().update({n: getattr(step, n) for n in _STEP})
+    return globals()[name]

@@ -53,6 +53,38 @@ def build_probe(verbose: bool = False) -> str:
     return out
 
 
+def binding_path() -> str:
+    """The extension module with the tensor helpers of the operators between
+    the products (csrc/step_bind.cpp)."""
+    return os.path.join(HERE, "_lib", "_sbvr_step.so")
+
+
+def build_binding(verbose: bool = False) -> str:
+    """Host code only: compiled against torch's headers, no GPU code in it."""
+    import sysconfig
+
+    import torch
+    from torch.utils.cpp_extension import include_paths, library_paths
+
+    out = binding_path()
+    os.makedirs(os.path.dirname(out), exist_ok=True)
+    tmp = out + ".tmp%d" % os.getpid()
+    includes = [*include_paths(), sysconfig.get_paths()["include"], os.path.join(ROOT, "include"),
+                os.path.join(os.path.dirname(os.path.dirname(HIPCC)), "include")]
+    cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-fvisibility=hidden",
+           "-DTORCH_EXTENSION_NAME=_sbvr_step", "-DTORCH_API_INCLUDE_EXTENSION_H", "-D__HIP_PLATFORM_AMD__",
+           "-D_GLIBCXX_USE_CXX11_ABI=%d" % int(torch._C._GLIBCXX_USE_CXX11_ABI),
+           *(f for p in includes for f in ("-isystem", p)), os.path.join(HERE, "csrc", "step_bind.cpp"),
+           *("-L" + p for p in library_paths()), "-lc10", "-ltorch_cpu", "-ltorch", "-ltorch_python", "-o", tmp]
+    if verbose:
+        print(" ".join(cmd))
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError("g++ failed:\n" + " ".join(cmd) + "\n" + r.stdout + r.stderr)
+    os.replace(tmp, out)
+    return out
+
+
 def build(verbose: bool = False, out: str | None = None, defines=(), jobs: int = 0) -> str:
     """Compile every source to an object (in parallel), then link libsbvr.so."""
     from concurrent.futures import ThreadPoolExecutor
@@ -93,3 +125,4 @@ def build(verbose: bool = False, out: str | None = None, defines=(), jobs: int =
 if __name__ == "__main__":
     print(build(verbose=True))
     print(build_probe(verbose=True))
+    print(build_binding(verbose=True))

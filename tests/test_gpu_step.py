@@ -759,3 +759,75 @@ def test_step_of_no_tokens(T):
     x, h = sb.residual_norm(s["x"][:0], s["y"][:0], pre_weight=s["w"])
     assert x.shape == (0, 512) and h.shape == (0, 512)
     assert sb.adjust_logits(s["logits"][:0], n_requests=3).shape == (0, 1000)
+
+
+# ---------------------------------------------------------------------------
+# refusals of the tensor helpers
+# ---------------------------------------------------------------------------
+
+def test_helpers_refuse_what_does_not_fit():
+    s = step_inputs(1)
+    T = s["T"]
+    p = sb.batch_plan(s["ctx"], s["new"], s["free"], s["table"], s["P"], T, parents=s["parents"])
+
+    def attend(q=s["q"], cache=s["cache"], table=s["table"], ctx=s["ctx"], start=p.query_start, mask=p.tree_mask, n=s["N"], **more):
+        return sb.tree_attention(q, cache, table, ctx, start, mask, n, **more)
+    bad = [
+        lambda: sb.batch_plan(s["ctx"].long(), s["new"], s["free"], s["table"], s["P"], T),
+        lambda: sb.batch_plan(s["ctx"], s["new"][:2], s["free"], s["table"], s["P"], T),
+        lambda: sb.batch_plan(s["ctx"], s["new"], s["free"], s["table"][:2], s["P"], T),
+        lambda: sb.batch_plan(s["ctx"], s["new"], s["free"], s["table"].t().contiguous().t(), s["P"], T),
+        lambda: sb.batch_plan(s["ctx"], s["new"], s["free"], s["table"], s["P"], T, parents=s["parents"][:-1]),
+        lambda: sb.cache_write(s["cache"], s["k"].bfloat16(), s["v"], p.slots),
+        lambda: sb.cache_write(s["cache"], s["k"], s["v"][:-1], p.slots),
+        lambda: sb.cache_write(s["cache"], s["k"][..., :64], s["v"], p.slots),
+        lambda: sb.cache_write(s["cache"], s["k"], s["v"], p.slots.int()),
+        lambda: attend(q=s["q"].bfloat16()),
+        lambda: attend(q=s["q"].transpose(0, 2).contiguous().transpose(0, 2)),
+        lambda: attend(ctx=s["ctx"][:2]),
+        lambda: attend(start=p.query_start[:-1]),
+        lambda: attend(mask=p.tree_mask[:-1]),
+        lambda: attend(out=torch.empty(T, 8, 128, device=DEV)),
+        lambda: attend(table=s["table"].cpu()),
+        lambda: sb.residual_norm(s["x"], s["y"].float()[:, :5]),
+        lambda: sb.residual_norm(s["x"], s["y"], post_weight=s["w"][:-1]),
+        lambda: sb.residual_norm(s["x"], post_weight=s["w"]),
+        lambda: sb.residual_norm(s["x"]),
+        lambda: sb.residual_norm(s["x"], s["y"], h_out=s["y"]),
+        lambda: sb.residual_norm(s["x"], s["y"], x_out=s["y"]),
+        lambda: sb.adjust_logits(s["logits"], frequency=s["freq"].double()),
+        lambda: sb.adjust_logits(s["logits"], history=s["draft"]),
+        lambda: sb.adjust_logits(s["logits"], bias_tokens=s["draft"]),
+        lambda: sb.adjust_logits(s["logits"], grammar=torch.zeros(2, 31, dtype=torch.int32, device=DEV)),
+        lambda: sb.adjust_logits(s["logits"], out=s["logits"], out_dtype=torch.float32),
+    ]
+    for i, call in enumerate(bad):
+        with pytest.raises(AssertionError):
+            call()
+            print("accepted:", i)
+    refused = [
+        lambda: sb.batch_plan(s["ctx"], s["new"], s["free"], s["table"], 24, T),
+        lambda: attend(n=65), lambda: attend(n=0), lambda: attend(scale=float("nan")),
+        lambda: attend(workspace=torch.empty(64, dtype=torch.uint8, device=DEV)),
+        lambda: sb.residual_norm(s["x"], s["y"], eps=-1.0),
+        lambda: sb.adjust_logits(s["logits"], draft_tokens=s["draft"]),
+        lambda: sb.adjust_logits(s["logits"].float(), out=torch.empty_like(s["logits"])),
+    ]
+    for call in refused:
+        with pytest.raises(sb.SBVRError):
+            call()
+
+
+def test_helpers_fill_what_they_are_given():
+    s = step_inputs(4)
+    p = sb.batch_plan(s["ctx"], s["new"], s["free"], s["table"].clone(), s["P"], s["T"], parents=s["parents"])
+    q = sb.BatchPlan(*[torch.full_like(getattr(p, n), -9) for n in sb.BatchPlan.__slots__])
+    assert sb.batch_plan(s["ctx"], s["new"], s["free"], s["table"].clone(), s["P"], s["T"], parents=s["parents"], out=q) is q
+    assert all(torch.equal(getattr(p, n), getattr(q, n)) for n in sb.BatchPlan.__slots__)
+    need = sb.sbvr_tree_attention_workspace_bytes(3, s["N"], 8, 2, 128)
+    ws = torch.empty(need + 16, dtype=torch.uint8, device=DEV)
+    out = torch.empty_like(s["q"])
+    sb.cache_write(s["cache"], s["k"], s["v"], p.slots)
+    got = sb.tree_attention(s["q"], s["cache"], s["table"], s["ctx"], p.query_start, p.tree_mask, s["N"], out=out, workspace=ws)
+    assert got.data_ptr() == out.data_ptr()
+    assert torch.equal(out, sb.tree_attention(s["q"], s["cache"], s["table"], s["ctx"], p.query_start, p.tree_mask, s["N"]))

@@ -153,3 +153,22 @@ def test_structs_match_the_header():
     import ctypes as C
     assert C.sizeof(sb.CacheStruct) == 8 * 8 + 5 * 4 + 4
     assert C.sizeof(sb.LogitsStruct) == 5 * 4 + 4 + 4 * 8 + 12 * 8 + 8 + 8 + 4 + 4 + 3 * 8
+
+
+def test_tensor_helpers_refuse_before_any_launch():
+    """The native helpers load here too, and say what is wrong with tensors
+    that are not theirs (these are on the CPU)."""
+    torch = pytest.importorskip("torch")
+    x = torch.zeros(2, 64, dtype=torch.float16)
+    i = torch.zeros(2, dtype=torch.int32)
+    with pytest.raises(AssertionError, match="GPU"):
+        sb.residual_norm(x, x)
+    with pytest.raises(AssertionError, match="GPU"):
+        sb.adjust_logits(x)
+    with pytest.raises(AssertionError, match="GPU"):
+        sb.batch_plan(i, i, i, i.view(2, 1), 16, 2)
+    kv = torch.zeros(2, 16, 2, 64, dtype=torch.float16)
+    with pytest.raises(AssertionError, match="GPU"):
+        sb.cache_write(sb.KVCache(kv, kv), x.view(2, 1, 64), x.view(2, 1, 64), i.long())
+    with pytest.raises(AssertionError, match="GPU"):
+        sb.tree_attention(x.view(2, 1, 64), sb.KVCache(kv, kv), i.view(2, 1), i, i, i.long(), max_new=1)
