@@ -970,7 +970,7 @@ __global__ void __launch_bounds__(ATTN_THREADS, WGS) attn_block_kernel(AttnArgs 
 // the join
 // ---------------------------------------------------------------------------
 
-constexpr int JOIN_WAVES = 4, JOIN_THREADS = 64 * JOIN_WAVES, JOIN_AHEAD = 4;
+constexpr int JOIN_WAVES = 4, JOIN_THREADS = 64 * JOIN_WAVES;
 
 // Joins the parts of a divided item (join i of workgroup (i, y)).  Few rows in
 // all: a workgroup has one row, its wavefronts share the parts and meet in LDS --
@@ -982,6 +982,7 @@ template <int DP, int ROWS, bool BF, int SPLITS, bool SPREAD>
 __global__ void __launch_bounds__(JOIN_THREADS) attn_join_kernel(AttnArgs a)
 {
     constexpr int JR = SPREAD ? 1 : 4, STEP = SPREAD ? JOIN_WAVES : 1;  // rows and parts of a wavefront's turn
+    constexpr int JOIN_AHEAD = SPREAD ? 8 : 4;
     static_assert(ROWS % (4 * JOIN_WAVES) == 0, "whole row groups");
     typedef float vrows __attribute__((ext_vector_type(JR)));
     __shared__ float2 meet[JOIN_WAVES][64];
@@ -1010,8 +1011,13 @@ __global__ void __launch_bounds__(JOIN_THREADS) attn_join_kernel(AttnArgs a)
         for (int r = 0; r < JR; ++r)
             ahead[k][r] = turn + k * STEP < n ? *(const float2 *)&part(turn + k * STEP).o[i0 + r][d]
                                               : make_float2(0.f, 0.f);
-    vrows top = NO_SCORE;
-    for (int k = lane; k < n; k += 64) {
+    vrows m0 = NO_SCORE, l0 = 0.f;  // of the first 64 parts
+    if (lane < n) {
+        m0 = *(const vrows *)&part(lane).m[i0];
+        l0 = *(const vrows *)&part(lane).l[i0];
+    }
+    vrows top = m0;
+    for (int k = lane + 64; k < n; k += 64) {
         const vrows m = *(const vrows *)&part(k).m[i0];
 #pragma unroll
         for (int r = 0; r < JR; ++r)
@@ -1028,7 +1034,8 @@ __global__ void __launch_bounds__(JOIN_THREADS) attn_join_kernel(AttnArgs a)
         // factors of 64 parts, a part a lane
         vrows f = 0.f;
         if (k0 + lane < n) {
-            const vrows m = *(const vrows *)&part(k0 + lane).m[i0], l = *(const vrows *)&part(k0 + lane).l[i0];
+            const vrows m = k0 ? *(const vrows *)&part(k0 + lane).m[i0] : m0;
+            const vrows l = k0 ? *(const vrows *)&part(k0 + lane).l[i0] : l0;
 #pragma unroll
             for (int r = 0; r < JR; ++r) {
                 f[r] = fast_exp2(m[r] - top[r]);
