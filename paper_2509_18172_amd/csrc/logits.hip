@@ -73,18 +73,18 @@ __global__ void __launch_bounds__(THREADS, THREADS == 1024 ? 2 : 1) logits_kerne
     const float inv_rep = 1.f / rep, inv_temp = temp > 0.f ? 1.f / temp : 1.f;
     const bool constrained = adjust && a.grammar && g >= 0 && g < a.grammar_count;
     const uint8_t *grammar = constrained ? (const uint8_t *)(a.grammar + g * a.grammar_stride) : nullptr;
-    // A whole tile is loaded without a branch, so that the compiler counts what
-    // it waits for: past the last whole one, the row's first tokens are loaded
-    // and not used (as is a byte of the row for a grammar that is not there).
-    const bool any_whole = a.V >= TILE;
+    // A tile is loaded without a branch, so that the compiler counts what it
+    // waits for: a piece that would pass the row's end is moved back to end with
+    // it, and its elements are moved to their places later (a byte of the row is
+    // loaded for a grammar that is not there).
+    const bool wide = a.V >= 8;
     Words<T> coming = {};
     uint32_t coming_allowed = 0;
     auto load = [&](int v) {
-        const int from = last - v >= TILE ? v : 0;
-        coming = load_words(in + from + i);
-        coming_allowed = *(grammar ? grammar + (from + i) / 8 : (const uint8_t *)in);
+        coming = load_words(in + min(v + i, a.V - 8));
+        coming_allowed = *(grammar ? grammar + min(v + i, a.V - 1) / 8 : (const uint8_t *)in);
     };
-    if (any_whole)
+    if (wide)
         load(first);
 
     Loose<int32_t, 4> history[HELD], biases[1];
@@ -146,7 +146,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 1024 ? 2 : 1) logits_kerne
         }
         if (counted || biased)
             __syncthreads();
-        if (n < TILE) {
+        if (!wide) {
             Loose<T, 8> l;
 #pragma unroll
             for (int e = 0; e < 8; ++e)
@@ -163,7 +163,15 @@ __global__ void __launch_bounds__(THREADS, THREADS == 1024 ? 2 : 1) logits_kerne
             for (int e = 0; e < 8; ++e)
                 x[e] = (float)l.e[e];
         }
-        if (any_whole)
+        if (n < TILE && wide) {
+            const int back = v0 + i - min(v0 + i, a.V - 8);
+#pragma unroll
+            for (int by = 4; by; by /= 2)
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    x[e] = back & by ? x[min(e + by, 7)] : x[e];
+        }
+        if (wide)
             load(v0 + TILE);
 
         if (counted || biased) {
@@ -198,7 +206,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 1024 ? 2 : 1) logits_kerne
 #pragma unroll
         for (int e = 0; e < 8; ++e)
             o.e[e] = (O)((allowed >> e) & 1 ? x[e] * inv_temp : -INFINITY);
-        if (n == TILE)
+        if (i + 8 <= n)
             store_words(out + v0 + i, to_words(o));
         else
 #pragma unroll
@@ -228,7 +236,7 @@ int go_logits(const sbvr_logits_args &a, hipStream_t stream)
     // that the chip holds have work; small tiles where there is less.
     const int tiles = (a.V + 8191) / 8192;
     const long long all = (long long)a.T * tiles;
-    if (all < 512)
+    if (all <= 768)
         return run_logits<T, O, 256>(a, 1, stream);
     const int ranges = (int)((tiles * 512ll + all - 1) / all);  // of a row
     return run_logits<T, O, 1024>(a, (tiles + ranges - 1) / ranges, stream);
