@@ -103,15 +103,32 @@ __device__ __forceinline__ float unpack(uint32_t w, int hi)
         return (float)__builtin_bit_cast(f16_t, (uint16_t)h);
 }
 
-// Sixteen lanes' 8-byte pieces of LDS as four rows of sixteen 16-bit elements
-// (lane i: row i / 4, elements 4 (i % 4) ..), read by columns: lane i gets
-// element i of the four rows.
+// Sixteen lanes' 8-byte pieces of LDS are four rows of sixteen 16-bit elements
+// (lane i: row i / 4, elements 4 (i % 4) ..), and lane i gets element i of the
+// four rows: at each of four addresses and HALF bytes past it.  They are waited
+// for here.  (The compiler lets its own transposing reads wait for every load
+// into LDS that is on its way.)
 typedef uint32_t v2u __attribute__((ext_vector_type(2)));
-__device__ __forceinline__ v2u read_transposed(const char *p)
+template <int HALF>
+__device__ __forceinline__ void read_transposed(const uint32_t (&at)[4], v4u (&v)[4])
 {
-    typedef short v4s __attribute__((ext_vector_type(4)));
-    typedef __attribute__((address_space(3))) v4s lds_v4s;
-    return __builtin_bit_cast(v2u, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s *)p));
+    v2u lo[4], hi[4];
+    asm volatile("ds_read_b64_tr_b16 %0, %8\n\t"
+                 "ds_read_b64_tr_b16 %4, %8 offset:%12\n\t"
+                 "ds_read_b64_tr_b16 %1, %9\n\t"
+                 "ds_read_b64_tr_b16 %5, %9 offset:%12\n\t"
+                 "ds_read_b64_tr_b16 %2, %10\n\t"
+                 "ds_read_b64_tr_b16 %6, %10 offset:%12\n\t"
+                 "ds_read_b64_tr_b16 %3, %11\n\t"
+                 "ds_read_b64_tr_b16 %7, %11 offset:%12\n\t"
+                 "s_waitcnt lgkmcnt(0)"
+                 : "=&v"(lo[0]), "=&v"(lo[1]), "=&v"(lo[2]), "=&v"(lo[3]), "=&v"(hi[0]), "=&v"(hi[1]), "=&v"(hi[2]),
+                   "=&v"(hi[3])
+                 : "v"(at[0]), "v"(at[1]), "v"(at[2]), "v"(at[3]), "n"(HALF)
+                 : "memory");
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        v[i] = v4u{lo[i][0], lo[i][1], hi[i][0], hi[i][1]};
 }
 
 // true where one of the two 16-bit values is an infinity or NaN
@@ -539,11 +556,19 @@ __device__ __forceinline__ const char *at_page(const void *base, int page, int p
 
 // The page of the sixteen positions at p (a page holds whole sixteens); -1:
 // past the end or outside the cache, read from page 0 and masked.
+__device__ __forceinline__ int table_entry(const int32_t *table, int p, int end, int page_shift)
+{
+    return uniform_load(table + (min(__builtin_amdgcn_readfirstlane(p), end - 1) >> page_shift));
+}
+
+__device__ __forceinline__ int page_of(const AttnArgs &a, int entry, int p, int end)
+{
+    return p < end && entry < a.kv.n_pages ? max(entry, -1) : -1;
+}
+
 __device__ __forceinline__ int page_at(const AttnArgs &a, const int32_t *table, int p, int end, int page_shift)
 {
-    p = __builtin_amdgcn_readfirstlane(p);
-    const int id = uniform_load(table + (min(p, end - 1) >> page_shift));
-    return p < end && id < a.kv.n_pages ? max(id, -1) : -1;
+    return page_of(a, table_entry(table, p, end, page_shift), p, end);
 }
 
 // A workgroup's part [u, stop) of an item: the item's rows from row0 on, the
@@ -650,10 +675,14 @@ __global__ void __launch_bounds__(ATTN_THREADS, WGS) attn_rows_kernel(AttnArgs a
             const char *vp = at_page(sg.v, page[h], p0 + 16 * h, a.kv.page_size, a.kv.v_page_stride, v_step);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const Halves<DV> v = *(const Halves<DV> *)(vp + (uint64_t)(e * v_step) + lane_offset(v_lane));
+                // read once: the caches need not keep it (a load of keys takes
+                // half a cache line, and its other half is still to come)
+                typedef uint32_t part_t __attribute__((ext_vector_type(DV / 2)));
+                const part_t v =
+                    __builtin_nontemporal_load((const part_t *)(vp + (uint64_t)(e * v_step) + lane_offset(v_lane)));
 #pragma unroll
                 for (int i = 0; i < DV / 2; ++i)
-                    vr[4 * h + e][i] = v.w[i];
+                    vr[4 * h + e][i] = v[i];
             }
         }
         issue_loads();
@@ -779,15 +808,39 @@ __global__ void __launch_bounds__(ATTN_THREADS, WGS) attn_rows_kernel(AttnArgs a
 // items of many rows
 // ---------------------------------------------------------------------------
 
+// One load of 1 KiB into LDS: every lane's 16 bytes at its `src` to dst + 16 lane.
+// It is complete when the wavefront's vector-memory count says so.  ONCE: the
+// caches need not keep it.
+template <bool ONCE>
+__device__ __forceinline__ void load_to_lds(const char *src, v4u *dst)
+{
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)src,
+                                     (__attribute__((address_space(3))) void *)dst, 16, 0, ONCE ? 2 : 0);
+}
+
+// Waits until the wavefront has read what it reads of LDS and its loads into LDS
+// are complete but for those of the `younger` last tiles, or of the MOST last.
+template <int MOST, int LOADS>
+__device__ __forceinline__ void wait_tiles(int younger)
+{
+    if constexpr (MOST > 0)
+        if (younger < MOST)
+            return wait_tiles<MOST - 1, LOADS>(younger);
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(MOST *LOADS) : "memory");
+}
+
 // NT: 16-row tiles per wavefront; the others as above.
 template <int DP, int DS, int NT, bool BF, int WGS>
 __global__ void __launch_bounds__(ATTN_THREADS, WGS) attn_block_kernel(AttnArgs a)
 {
     constexpr int DV = DP / 16, WROWS = 16 * NT, ROWS = WROWS * ATTN_WAVES, UNIT = 64, SPLITS = WGS * CUS;
-    constexpr int PIECES = DP / 8;         // 16-byte pieces of a stored row
-    constexpr int LOADS = UNIT * PIECES / ATTN_THREADS;  // per thread, of keys and of values
-    constexpr int LOAD_ROWS = 64 / PIECES; // rows that one load of a wavefront covers
-    __shared__ v4u tile[2][2][UNIT][PIECES];  // [buffer][keys, values][position][piece, permuted]
+    constexpr int PIECES = DP / 8;               // 16-byte pieces of a stored row
+    constexpr int STAGES = 64 / PIECES;          // tiles of 32 positions in LDS: 64 KiB
+    constexpr int AHEAD = STAGES - 1;            // of them on their way or waiting
+    constexpr int WAVE_ROWS = TILE / ATTN_WAVES; // positions of a tile that a wavefront brings in
+    constexpr int LOAD_ROWS = 64 / PIECES;       // of them in one load
+    constexpr int LOADS = WAVE_ROWS / LOAD_ROWS; // loads, of keys and of values
+    __shared__ v4u tile[STAGES][2][TILE][PIECES];  // [stage][keys, values][position][piece, permuted]
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int c = lane & 15, g = lane >> 4;
@@ -809,11 +862,17 @@ __global__ void __launch_bounds__(ATTN_THREADS, WGS) attn_block_kernel(AttnArgs 
     // piece of sixteen rows, or the pieces of one row, meet all banks once.
     auto swap = [](int r) { return PIECES == 16 ? r & 15 : (r >> 1) & 7; };
 
-    // Wavefront w brings in positions 16 w .. 16 w + 15 of a unit, LOAD_ROWS a
-    // load; lane -> (row of the load, piece).
-    const int load_row = lane / PIECES, load_piece = lane % PIECES;
-    const int from = load_piece < pieces ? load_piece : 0;
-    const uint32_t k_lane = load_row * k_step + 16 * from, v_lane = load_row * v_step + 16 * from;
+    // Wavefront w brings in positions 8 w .. 8 w + 7 of a tile, straight into LDS:
+    // a load's lanes lie one after the other there, so a lane takes the piece that
+    // belongs to its place.
+    uint32_t k_lane[LOADS], v_lane[LOADS];
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+        const int r = i * LOAD_ROWS + lane / PIECES, piece = (lane % PIECES) ^ swap(wave * WAVE_ROWS + r);
+        const int from = piece < pieces ? piece : 0;
+        k_lane[i] = r * k_step + 16 * from;
+        v_lane[i] = r * v_step + 16 * from;
+    }
 
     // Where lane (c, g) reads its operands in a stored tile: keys, piece 4 s + g
     // of row c (and 16 + c); values, transposed, elements 16 i + 4 (c % 4) .. of
@@ -824,74 +883,75 @@ __global__ void __launch_bounds__(ATTN_THREADS, WGS) attn_block_kernel(AttnArgs 
     const uint32_t k_read = c * ROW_BYTES + 16 * (g ^ swap(c));
     const uint32_t v_read = v_row * ROW_BYTES + 16 * (((c & 3) >> 1) ^ swap(v_row)) + 8 * (c & 1);
 
-    v4u kin[LOADS], vin[LOADS];
-    int ids[ATTN_WAVES], ahead[ATTN_WAVES];
-    // the pages of the unit at p0's four sixteens
-    auto pages_of = [&](const Segment &sg, int p0, int (&id)[ATTN_WAVES]) {
-#pragma unroll
-        for (int w = 0; w < ATTN_WAVES; ++w)
-            id[w] = page_at(a, sg.table, p0 + 16 * w, sg.end, page_shift);
+    int ids[2 * AHEAD];  // table entries of the sixteens that are brought in next
+    uint32_t there = 0;  // two bits a stage: which of its sixteens are there
+    auto pages_of = [&](const Segment &sg, int p0, int *id) {
+        id[0] = table_entry(sg.table, p0, sg.end, page_shift);
+        id[1] = table_entry(sg.table, p0 + 16, sg.end, page_shift);
     };
-    // brings in the unit at p0 and says which of its sixteens are there
-    auto load = [&](const Segment &sg, int p0, const int (&id)[ATTN_WAVES]) {
-        int ok = 0, mine = -1;
+    // brings in the tile at p0
+    auto load = [&](const Segment &sg, int p0, const int *entry, int stage) {
+        const int id[2] = {page_of(a, entry[0], p0, sg.end), page_of(a, entry[1], p0 + 16, sg.end)};
+        const int mine = wave < ATTN_WAVES / 2 ? id[0] : id[1], p = p0 + wave * WAVE_ROWS;
+        const char *kp = at_page(sg.k, mine, p, a.kv.page_size, a.kv.k_page_stride, k_step);
+        const char *vp = at_page(sg.v, mine, p, a.kv.page_size, a.kv.v_page_stride, v_step);
+        v4u(*const to)[TILE][PIECES] = tile[stage];
+        if (NT == 1 || sg.it.rq.n * group <= ROWS) {  // no other block of rows reads it too
 #pragma unroll
-        for (int w = 0; w < ATTN_WAVES; ++w) {
-            ok |= (id[w] >= 0) << w;
-            mine = w == wave ? id[w] : mine;
-        }
-        const char *kp = at_page(sg.k, mine, p0 + 16 * wave, a.kv.page_size, a.kv.k_page_stride, k_step);
-        const char *vp = at_page(sg.v, mine, p0 + 16 * wave, a.kv.page_size, a.kv.v_page_stride, v_step);
+            for (int i = 0; i < LOADS; ++i) {
+                load_to_lds<true>(kp + lane_offset(k_lane[i]), to[0][wave * WAVE_ROWS + i * LOAD_ROWS]);
+                load_to_lds<true>(vp + lane_offset(v_lane[i]), to[1][wave * WAVE_ROWS + i * LOAD_ROWS]);
+            }
+        } else {
 #pragma unroll
-        for (int i = 0; i < LOADS; ++i) {
-            kin[i] = *(const v4u *)(kp + (uint64_t)(i * LOAD_ROWS * k_step) + lane_offset(k_lane));
-            vin[i] = *(const v4u *)(vp + (uint64_t)(i * LOAD_ROWS * v_step) + lane_offset(v_lane));
+            for (int i = 0; i < LOADS; ++i) {
+                load_to_lds<false>(kp + lane_offset(k_lane[i]), to[0][wave * WAVE_ROWS + i * LOAD_ROWS]);
+                load_to_lds<false>(vp + lane_offset(v_lane[i]), to[1][wave * WAVE_ROWS + i * LOAD_ROWS]);
+            }
         }
         issue_loads();
-        return ok;
+        there = (there & ~(3u << (2 * stage))) | ((id[0] >= 0 ? 1u : 0u) | (id[1] >= 0 ? 2u : 0u)) << (2 * stage);
     };
-    auto store = [&](int buffer) {
-#pragma unroll
-        for (int i = 0; i < LOADS; ++i) {
-            const int r = 16 * wave + i * LOAD_ROWS + load_row;
-            tile[buffer][0][r][load_piece ^ swap(r)] = kin[i];
-            tile[buffer][1][r][load_piece ^ swap(r)] = vin[i];
-        }
-    };
-    // (a unit past the segment's end is the one before it once more)
-    auto next_unit = [](const Segment &sg, int p0) { return p0 + UNIT < sg.last ? p0 + UNIT : p0; };
     Rows<DP, DS, NT, BF, true> row;
-    int there = 0, coming = 0;
     // the wavefront's own rows of a segment's
     auto my_rows = [&](const Segment &sg) { return min(max(sg.rows - wave * WROWS, 0), WROWS); };
-    // sends off a segment's first loads
-    auto open = [&](int u) {
+    auto tiles_of = [](const Segment &sg) { return (sg.last - sg.first + TILE - 1) / TILE; };
+    // sends off a segment's first loads, its first tile to `stage`
+    auto open = [&](int u, int stage) {
         const Segment sg = segment_at(line, a, u, u1);
         row.begin(a, sg.it, sg.row0 + (my_rows(sg) ? wave * WROWS : 0), my_rows(sg), group);
-        pages_of(sg, sg.first, ids);
-        pages_of(sg, next_unit(sg, sg.first), ahead);
-        there = load(sg, sg.first, ids);
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k)
+            pages_of(sg, sg.first + k * TILE, &ids[2 * k]);
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k)
+            if (k < tiles_of(sg))
+                load(sg, sg.first + k * TILE, &ids[2 * k], (stage + k) % STAGES);
+        pages_of(sg, sg.first + AHEAD * TILE, ids);
         return sg;
     };
 
-    Segment seg = open(u0);
+    int stage = 0;
+    Segment seg = open(u0, 0);
     for (;;) {
         const Request &rq = seg.it.rq;
-        const int rows = my_rows(seg);
+        const int rows = my_rows(seg), tiles = tiles_of(seg);
         row.finish(a, rows);
-        store(0);
-        coming = load(seg, next_unit(seg, seg.first), ahead);
-        __syncthreads();
-        int buffer = 0;
-        for (int p0 = seg.first; p0 < seg.last; p0 += UNIT) {
-            const int p2 = next_unit(seg, next_unit(seg, p0));
-            pages_of(seg, p2, ids);
-#pragma unroll 1
-            for (int t = 0; t < UNIT / TILE; ++t) {
-                const int pt = p0 + t * TILE;
-                if (pt >= seg.end || rows == 0)
-                    continue;
-                const char *keys = (const char *)tile[buffer][0][t * TILE], *values = (const char *)tile[buffer][1][t * TILE];
+        for (int k = 0; k < tiles; ++k) {
+            // This tile is there and the one before it is read, in every
+            // wavefront: the next loads take its place.
+            wait_tiles<STAGES - 2, 2 * LOADS>(tiles - 1 - k);
+            __builtin_amdgcn_s_barrier();
+            issue_loads();
+            const int pt = seg.first + k * TILE, at = stage;
+            if (k + AHEAD < tiles) {
+                load(seg, pt + AHEAD * TILE, ids, (stage + AHEAD) % STAGES);
+                pages_of(seg, pt + (AHEAD + 1) * TILE, ids);
+            }
+            stage = (stage + 1) % STAGES;
+            if (rows) {
+                const char *keys = (const char *)tile[at][0];
+                const uint32_t values = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)tile[at][1];
                 v4u kf[2][DS];
 #pragma unroll
                 for (int h = 0; h < 2; ++h)
@@ -902,12 +962,13 @@ __global__ void __launch_bounds__(ATTN_THREADS, WGS) attn_block_kernel(AttnArgs 
                 row.scores(kf, s);
                 v4u vf[DV];
 #pragma unroll
-                for (int i = 0; i < DV; ++i) {
-                    const v2u lo = read_transposed(values + (v_read ^ (32 * i)));
-                    const v2u hi = read_transposed(values + 16 * ROW_BYTES + (v_read ^ (32 * i)));
-                    vf[i] = v4u{lo[0], lo[1], hi[0], hi[1]};
+                for (int i = 0; i < DV; i += 4) {
+                    const uint32_t v_at = values + v_read;
+                    const uint32_t from[4] = {v_at ^ (32 * i), v_at ^ (32 * (i + 1)), v_at ^ (32 * (i + 2)),
+                                              v_at ^ (32 * (i + 3))};
+                    read_transposed<16 * ROW_BYTES>(from, *(v4u(*)[4]) & vf[i]);
                 }
-                const bool ok0 = (there >> (2 * t)) & 1, ok1 = (there >> (2 * t + 1)) & 1;
+                const bool ok0 = (there >> (2 * at)) & 1, ok1 = (there >> (2 * at + 1)) & 1;
                 const bool masked = pt + TILE > rq.ctx || !ok0 || !ok1;
                 if (masked)
                     row.hide(pt, ok0, ok1, rq, s);
@@ -920,20 +981,13 @@ __global__ void __launch_bounds__(ATTN_THREADS, WGS) attn_block_kernel(AttnArgs 
                     });
                 row.products(pf, vf);
             }
-            // the other buffer was last read before the barrier at the end of the
-            // step before
-            store(buffer ^ 1);
-            there = coming;
-            coming = load(seg, p2, ids);
-            buffer ^= 1;
-            __syncthreads();
         }
 
         // the segment's results leave under the next one's first loads
         const Segment done = seg;
         const bool more = done.stop < u1, whole = is_whole(done);
         if (more)
-            seg = open(done.stop);
+            seg = open(done.stop, stage);
         if (threadIdx.x == 0)
             note_join<ROWS>(a, cuts, done, u0, u1, ws.join);
         Part<ROWS, DP> &part = ws.part[2 * blockIdx.x + (done.u != u0)];
@@ -1119,7 +1173,7 @@ constexpr int wgs_of(Shape s, int dp) { return s == ROWS16 && dp == 64 ? 4 : 2; 
 // Rows up to which a join has a workgroup for each: one request at 4096
 // positions, 32 rows in all, takes 15.5 us so and 23.5 with a wavefront for four
 // rows; 16 trees of 64, 32768 rows, 113 and 81.
-constexpr int JOIN_MOST = 4096;
+constexpr int JOIN_MOST = 2048;
 
 template <int DP, int ROWS, bool BF, int WGS>
 int run_attn(const void *kernel, const AttnArgs &a, hipStream_t stream)
