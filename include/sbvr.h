@@ -463,8 +463,9 @@ int sbvr_cache_write(const sbvr_kv_cache *cache, int T, const void *k, int64_t k
  *   tree_mask    uint64 [T].  1 <= R <= SBVR_REQUESTS_MAX.
  *   max_new      1 .. SBVR_TREE_MAX: no request brings more new tokens than
  *                this (the rest of a longer one is left out).
- *                R * kv_heads * (max_new * heads / kv_heads / 16 + 1) *
- *                (max_pages * page_size / 64 + 2) beyond 2^31: SBVR_E_UNSUPPORTED.
+ *                With B = max_new * heads / kv_heads / 128 rounded up,
+ *                R * kv_heads * B * (max_pages * page_size / 64 + 5) of 2^31 or
+ *                more: SBVR_E_UNSUPPORTED.
  *   out          [T][heads][head_dim] contiguous; rows past query_start[R] are
  *                left as they are.  Must not overlap the inputs.
  *   workspace    sbvr_tree_attention_workspace_bytes, 16-byte aligned; its

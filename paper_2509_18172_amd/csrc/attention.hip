@@ -168,11 +168,17 @@ __device__ __forceinline__ Request request_of(const AttnArgs &a, int r)
 
 // Where the items lie on the line of units: request r's kv_heads * row blocks
 // items one after the other, each of the request's units.  The line has fewer
-// than 2^31 units (checked by the launcher).
+// than 2^31 units (checked by the launcher).  Where the line is long enough that
+// no range is all of them, an item has `lead` empty units before its own, which
+// stand for the time that it takes to begin and end one: a workgroup whose range
+// has many short items gets fewer of them.  (64 ragged requests of up to 2047
+// positions: one token each, heads 64 wide, 40.7 us without and 37.8 with one;
+// eight tokens 73.8 and 67.0; trees of 32 119 us without, 107 with one, 93 with
+// three.)
 struct Item {
     int r, kvh, block;
     Request rq;
-    int start, units;  // first unit, number of units
+    int start, units, lead;  // first unit, number of units, the empty ones among them
 };
 
 template <int ROWS>
@@ -195,15 +201,20 @@ __device__ __forceinline__ int wave_scan(int v)
 
 // Up to 64 requests: a lane each, in every wavefront by itself.  More: each
 // lane has a run of requests, in every wavefront again.
-template <int ROWS, int UNIT>
+template <int ROWS, int UNIT, int SPLITS>
 struct Line {
+    static constexpr int LEAD = ROWS == 128 ? 3 : 1;
     const AttnArgs &a;
-    int total, per, before;
+    int total, per, before, lead;
     Request mine;  // per == 1: the lane's request
 
-    __device__ static int units_of(const AttnArgs &a, const Request &q)
+    __device__ static int items_of(const AttnArgs &a, const Request &q)
     {
-        return (q.ctx + q.n + UNIT - 1) / UNIT * row_blocks<ROWS>(a, q) * a.kv.kv_heads;
+        return row_blocks<ROWS>(a, q) * a.kv.kv_heads;
+    }
+    __device__ static int units_of(const AttnArgs &a, const Request &q, int lead)
+    {
+        return ((q.ctx + q.n + UNIT - 1) / UNIT + lead) * items_of(a, q);
     }
 
     __device__ explicit Line(const AttnArgs &a_) : a(a_)
@@ -212,12 +223,17 @@ struct Line {
         per = (a.R + 63) / 64;
         const int r0 = lane * per, r1 = min(r0 + per, a.R);
         mine = request_of(a, min(r0, a.R - 1));
-        int own = r0 < a.R ? units_of(a, mine) : 0;
-        for (int r = r0 + 1; r < r1; ++r)
-            own += units_of(a, request_of(a, r));
-        const int sum = wave_scan(own);
-        before = sum - own;
+        int own = r0 < a.R ? units_of(a, mine, 0) : 0, items = r0 < a.R ? items_of(a, mine) : 0;
+        for (int r = r0 + 1; r < r1; ++r) {
+            const Request q = request_of(a, r);
+            own += units_of(a, q, 0);
+            items += items_of(a, q);
+        }
+        const int sum = wave_scan(own), sum_items = wave_scan(items);
         total = __builtin_amdgcn_readlane(sum, 63);
+        lead = total >= (LEAD + 1) * SPLITS ? LEAD : 0;
+        before = sum - own + lead * (sum_items - items);
+        total += lead * __builtin_amdgcn_readlane(sum_items, 63);
     }
 
     // the item that holds unit u (the same in every lane)
@@ -234,7 +250,7 @@ struct Line {
             it.r = run * per;
             const int n = min(per, a.R - it.r);
             q = request_of(a, it.r + min(lane, n - 1));
-            const int own = lane < n ? units_of(a, q) : 0, sum = wave_scan(own);
+            const int own = lane < n ? units_of(a, q, lead) : 0, sum = wave_scan(own);
             at = 63 - __builtin_clzll(__ballot(lane < n && base + sum - own <= u));
             base += __builtin_amdgcn_readlane(sum - own, at);
             it.r += at;
@@ -242,7 +258,8 @@ struct Line {
         it.rq.ctx = __builtin_amdgcn_readlane(q.ctx, at);
         it.rq.n = __builtin_amdgcn_readlane(q.n, at);
         it.rq.first = __builtin_amdgcn_readlane(q.first, at);
-        it.units = (it.rq.ctx + it.rq.n + UNIT - 1) / UNIT;
+        it.lead = lead;
+        it.units = (it.rq.ctx + it.rq.n + UNIT - 1) / UNIT + lead;
         const uint32_t blocks = row_blocks<ROWS>(a, it.rq);
         const uint32_t k = __builtin_amdgcn_readfirstlane((uint32_t)(u - base) / (uint32_t)it.units);
         it.start = base + (int)k * it.units;
@@ -580,8 +597,8 @@ struct Segment {
     const uint16_t *k, *v;
 };
 
-template <int ROWS, int UNIT>
-__device__ __forceinline__ Segment segment_at(const Line<ROWS, UNIT> &line, const AttnArgs &a, int u, int u1)
+template <int ROWS, int UNIT, int SPLITS>
+__device__ __forceinline__ Segment segment_at(const Line<ROWS, UNIT, SPLITS> &line, const AttnArgs &a, int u, int u1)
 {
     Segment s;
     s.it = line.item_at(u);
@@ -590,18 +607,24 @@ __device__ __forceinline__ Segment segment_at(const Line<ROWS, UNIT> &line, cons
     s.row0 = s.it.block * ROWS;
     s.rows = min(s.it.rq.n * (a.heads / a.kv.kv_heads) - s.row0, ROWS);
     s.end = s.it.rq.ctx + s.it.rq.n;
-    s.first = (u - s.it.start) * UNIT;
-    s.last = min((s.stop - s.it.start) * UNIT, s.end);
+    s.first = max(u - s.it.start - s.it.lead, 0) * UNIT;
+    s.last = min((s.stop - s.it.start - s.it.lead) * UNIT, s.end);
     s.table = a.page_table + s.it.r * a.table_stride;
     s.k = (const uint16_t *)a.kv.k + s.it.kvh * a.kv.k_head_stride;
     s.v = (const uint16_t *)a.kv.v + s.it.kvh * a.kv.v_head_stride;
     return s;
 }
 
+// (a range may start among an item's empty units)
+__device__ __forceinline__ bool begins_item(const Segment &s) { return s.u <= s.it.start + s.it.lead; }
+
 __device__ __forceinline__ bool is_whole(const Segment &s)
 {
-    return s.u == s.it.start && s.stop == s.it.start + s.it.units;
+    return begins_item(s) && s.stop == s.it.start + s.it.units;
 }
+
+// whether the range has another item's positions
+__device__ __forceinline__ bool more_after(const Segment &s, int u1) { return s.stop + s.it.lead < u1; }
 
 // End of a workgroup's segment (called by one thread).
 template <int ROWS, int SPLITS>
@@ -609,8 +632,8 @@ __device__ __forceinline__ void note_join(const AttnArgs &a, const Cuts<SPLITS> 
                                           Join *join)
 {
     const Item &it = s.it;
-    const bool begins = s.u == it.start, divided = begins && s.stop < it.start + it.units;
-    if (a.by_item ? !begins : s.stop < u1)
+    const bool begins = begins_item(s), divided = begins && s.stop < it.start + it.units;
+    if (a.by_item ? !begins : more_after(s, u1))
         return;
     Join j = {};
     if (divided) {
@@ -644,7 +667,7 @@ __global__ void __launch_bounds__(ATTN_THREADS, WGS) attn_rows_kernel(AttnArgs a
     const int D = a.kv.head_dim, pieces = D / 8;
     const int page_shift = __builtin_ctz(a.kv.page_size);
     Workspace<ROWS, DP, SPLITS> &ws = *(Workspace<ROWS, DP, SPLITS> *)a.workspace;
-    const Line<ROWS, UNIT> line(a);
+    const Line<ROWS, UNIT, SPLITS> line(a);
     const Cuts<SPLITS> cuts(line.total);
     if ((int)blockIdx.x >= cuts.ranges()) {
         if (!a.by_item && threadIdx.x == 0)
@@ -749,7 +772,7 @@ __global__ void __launch_bounds__(ATTN_THREADS, WGS) attn_rows_kernel(AttnArgs a
 
         // the wavefronts' parts meet in LDS, under the next segment's first loads
         const Segment done = seg;
-        const bool more = done.stop < u1, whole = is_whole(done);
+        const bool more = more_after(done, u1), whole = is_whole(done);
         if (more)
             seg = open(done.stop);
 #pragma unroll
@@ -848,7 +871,7 @@ __global__ void __launch_bounds__(ATTN_THREADS, WGS) attn_block_kernel(AttnArgs 
     const int D = a.kv.head_dim, pieces = D / 8;
     const int page_shift = __builtin_ctz(a.kv.page_size);
     Workspace<ROWS, DP, SPLITS> &ws = *(Workspace<ROWS, DP, SPLITS> *)a.workspace;
-    const Line<ROWS, UNIT> line(a);
+    const Line<ROWS, UNIT, SPLITS> line(a);
     const Cuts<SPLITS> cuts(line.total);
     if ((int)blockIdx.x >= cuts.ranges()) {
         if (!a.by_item && threadIdx.x == 0)
@@ -985,7 +1008,7 @@ __global__ void __launch_bounds__(ATTN_THREADS, WGS) attn_block_kernel(AttnArgs 
 
         // the segment's results leave under the next one's first loads
         const Segment done = seg;
-        const bool more = done.stop < u1, whole = is_whole(done);
+        const bool more = more_after(done, u1), whole = is_whole(done);
         if (more)
             seg = open(done.stop, stage);
         if (threadIdx.x == 0)
@@ -1183,7 +1206,7 @@ int run_attn(const void *kernel, const AttnArgs &a, hipStream_t stream)
     const int rows = a.max_new * (a.heads / a.kv.kv_heads), blocks = (rows + ROWS - 1) / ROWS;
     const long long items = (long long)a.R * a.kv.kv_heads * blocks;
     // units of 64 positions at least, on a line numbered in 32 bits
-    if (((long long)a.max_pages * a.kv.page_size / 64 + 2) * items >= (1ll << 31))
+    if (((long long)a.max_pages * a.kv.page_size / 64 + 5) * items >= (1ll << 31))
         return SBVR_E_UNSUPPORTED;
     args.by_item = items < SPLITS;
     void *argv[] = {&args};
