@@ -8,9 +8,9 @@
 // g = lane / 16 stands for position 4g + e (e < 4) and 16 + 4g + e - 4 of a
 // 32-position tile, and the V operand is laid out the same way.
 //   K: lane (c = lane % 16, g) holds position c, elements 32 s + 8 g .. + 7.
-//   V: lane (c, g) holds elements DV c .. DV c + DV - 1 (DV = DP / 16) of its
-//      eight positions; row c of operand q is element DV c + q, picked from
-//      the eight rows with byte permutes.
+//   V: row c of operand q is element DV c + q (DV = DP / 16) of the lane's eight
+//      positions, picked from the eight rows with byte permutes, or 16 q + c,
+//      where LDS hands it out transposed.
 // head_dim below DP: lanes past the end read piece 0 instead; their Q is zero
 // and their outputs are not stored.
 //
@@ -21,23 +21,25 @@
 //     soon as the products are, so each is in flight while the other is used.
 //     The four wavefronts' sums meet in LDS at the end.
 //   attn_block_kernel (up to 64 or 128 rows): each wavefront has 16 or 32 rows of
-//     its own and all four share the tiles, which go through LDS once for all of
-//     them, one tile ahead; pieces are stored permuted so that both operands'
-//     reads are free of bank conflicts.
+//     its own and all four share the tiles, which go straight into LDS, three of
+//     32 positions ahead (seven where a head has 64 elements); pieces lie permuted
+//     so that both operands' reads are free of bank conflicts.
+// What only one block of rows reads is loaded past the caches: 64 trees of 16 at
+// 8192 positions take 359 us so and 404 otherwise.
 // Measured, four query heads on each of eight key/value heads of 128 elements,
-// binary16: 64 requests of one token at 8192 positions 370 us (5.8 TB/s; the
-// block kernel 374), one request at 4096 15.4 us (17.8); trees of eight (32 rows)
-// at 8192 382 us with the block kernel, 405 with 32 rows in the rows kernel's
-// registers; trees of 32 (128 rows) 440 us, 640 TFLOP/s, and as two blocks of 64
-// 774.  A plain read of as many bytes takes about 305 us.
+// binary16, pages token by token: 64 requests of one token at 8192 positions 365
+// us (5.9 TB/s; pages head by head 336, 6.4), one request at 4096 14.7 us, of which
+// the join is 3.9; 64 trees of eight 361 us, of 16 359 (6.0 TB/s), of 32 (128 rows)
+// 441 to 465 us, 600 TFLOP/s, by the chip's power; 64 trees of 32 at 2048 131 us and
+// as two blocks of 64 rows 217.  A plain read of as many bytes takes 317 us.
 //
-// Work: the cached positions of all items, in units of one step of a
-// workgroup, are one line that is cut into (up to) SPLITS (as many workgroups as the chip
-// holds) equal ranges,
-// whatever the requests' lengths; a workgroup runs the segments of items in
-// its range.  An item within one range is finished there; of an item that a
-// cut divides, every workgroup leaves its unnormalised sums, and a second
-// kernel joins them.  Which workgroup has what follows from the lengths alone.
+// Work: the cached positions of all items, in units of one step of a workgroup,
+// are one line that is cut into (up to) SPLITS (as many workgroups as the chip
+// holds) equal ranges, whatever the requests' lengths; a workgroup runs the
+// segments of items in its range.  An item within one range is finished there; of
+// an item that a cut divides, every workgroup leaves its unnormalised sums, and a
+// second kernel joins them.  Which workgroup has what follows from the lengths
+// alone.
 //
 // A row's running maximum is moved only when a score passes it by 2^GAP: the
 // weights then stay within the 16-bit types' range, sums and products are
@@ -680,19 +682,20 @@ __global__ void __launch_bounds__(ATTN_THREADS, WGS) attn_rows_kernel(AttnArgs a
 
     v4u kf[2][DS];
     uint32_t vr[8][DV / 2];
-    auto load_k = [&](const Segment &sg, int p0, const int *page) {
+    // (used: ~0; 0 where the tile is not used: every lane loads the first one's)
+    auto load_k = [&](const Segment &sg, int p0, const int *page, uint32_t used) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const char *kp = at_page(sg.k, page[h], p0 + 16 * h, a.kv.page_size, a.kv.k_page_stride, k_step);
 #pragma unroll
             for (int s = 0; s < DS; ++s) {
                 const uint32_t piece = 4 * s + 3 < pieces || 4 * s + g < pieces ? 4 * s + g : 0;
-                kf[h][s] = *(const v4u *)(kp + lane_offset(k_lane + 16 * piece));
+                kf[h][s] = *(const v4u *)(kp + lane_offset((k_lane + 16 * piece) & used));
             }
         }
         issue_loads();
     };
-    auto load_v = [&](const Segment &sg, int p0, const int *page) {
+    auto load_v = [&](const Segment &sg, int p0, const int *page, uint32_t used) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const char *vp = at_page(sg.v, page[h], p0 + 16 * h, a.kv.page_size, a.kv.v_page_stride, v_step);
@@ -702,7 +705,7 @@ __global__ void __launch_bounds__(ATTN_THREADS, WGS) attn_rows_kernel(AttnArgs a
                 // half a cache line, and its other half is still to come)
                 typedef uint32_t part_t __attribute__((ext_vector_type(DV / 2)));
                 const part_t v =
-                    __builtin_nontemporal_load((const part_t *)(vp + (uint64_t)(e * v_step) + lane_offset(v_lane)));
+                    __builtin_nontemporal_load((const part_t *)(vp + (uint64_t)(e * v_step) + lane_offset(v_lane & used)));
 #pragma unroll
                 for (int i = 0; i < DV / 2; ++i)
                     vr[4 * h + e][i] = v[i];
@@ -724,10 +727,11 @@ __global__ void __launch_bounds__(ATTN_THREADS, WGS) attn_rows_kernel(AttnArgs a
         row.begin(a, sg.it, sg.row0, sg.rows, group);
         // (a wavefront without a tile loads one too)
         const int start = min(sg.first + wave * TILE, (sg.last - 1) & ~(TILE - 1));
+        const uint32_t used = start == sg.first + wave * TILE ? ~0u : 0u;
         pages_of(sg, start, page);
         pages_of(sg, next_tile(sg, start), next);
-        load_k(sg, start, page);
-        load_v(sg, start, page);
+        load_k(sg, start, page, used);
+        load_v(sg, start, page, used);
         return sg;
     };
 
@@ -736,13 +740,14 @@ __global__ void __launch_bounds__(ATTN_THREADS, WGS) attn_rows_kernel(AttnArgs a
         const Request &rq = seg.it.rq;
         row.finish(a, seg.rows);
         for (int p0 = seg.first + wave * TILE; p0 < seg.last; p0 += UNIT) {
-            // no branch around the loads, so that their counters stay exact: the
-            // last tile is loaded once more, from L2, and not used
+            // no branch around the loads, so that their counters stay exact: a
+            // little of the last tile is loaded once more and not used
             const int pn = next_tile(seg, p0);
+            const uint32_t used = pn != p0 ? ~0u : 0u;
             pages_of(seg, next_tile(seg, pn), after);
             v4f s[NT][2];
             row.scores(kf, s);
-            load_k(seg, pn, next);
+            load_k(seg, pn, next, used);
             const bool masked = p0 + TILE > rq.ctx || (page[0] | page[1]) < 0;
             if (masked)
                 row.hide(p0, page[0] >= 0, page[1] >= 0, rq, s);
@@ -762,7 +767,7 @@ __global__ void __launch_bounds__(ATTN_THREADS, WGS) attn_rows_kernel(AttnArgs a
                     return (const uint16_t *)at_page(seg.v, id, p, a.kv.page_size, a.kv.v_page_stride, v_step);
                 });
             row.products(pf, vf);
-            load_v(seg, pn, next);
+            load_v(seg, pn, next, used);
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 page[h] = next[h];
@@ -1188,14 +1193,15 @@ Shape shape_of(int max_new, int heads, int kv_heads)
     return rows <= 16 ? ROWS16 : rows <= 64 ? ROWS64 : ROWS128;
 }
 
-// Workgroups a CU, by registers.  Narrow heads of few rows need few: four finish
-// 64 requests of up to 2047 positions, 64 wide, in 41 us, two in 45; at 8192
-// positions, where starting up counts less, 199 and 192 us.
+// Workgroups a CU, by registers.  Narrow heads of few rows need few: four finished
+// 64 requests of up to 2047 positions, 64 wide, in 41 us and two in 45 when this
+// was chosen; at 8192 positions, where starting up counts less, 199 and 192 us.
 constexpr int wgs_of(Shape s, int dp) { return s == ROWS16 && dp == 64 ? 4 : 2; }
 
-// Rows up to which a join has a workgroup for each: one request at 4096
-// positions, 32 rows in all, takes 15.5 us so and 23.5 with a wavefront for four
-// rows; 16 trees of 64, 32768 rows, 113 and 81.
+// Rows up to which a join has a workgroup for each.  With that and with a
+// wavefront for four rows: one request at 4096 positions, 32 rows in all, 14.3 and
+// 23.0 us; four trees of 16 at 8192, 2048 rows, 43.1 and 46.7; eight, 4096 rows,
+// 76.6 and 72.3; 16, 8192 rows, 131 and 124.
 constexpr int JOIN_MOST = 2048;
 
 template <int DP, int ROWS, bool BF, int WGS>

@@ -3,7 +3,12 @@
 //
 // A workgroup is X lanes (the 16-byte pieces of a token's keys and values, so
 // a lane works out its head and offset once) by Y tokens; four tokens a lane
-// are in flight.
+// are in flight (with eight, eight tokens take 4.0 us instead of 3.5 and 16384
+// no less; two are within 1 % of four).
+//
+// Measured in a graph, eight key/value heads of 128 elements: 16384 tokens 27.0
+// us, 4.97 TB/s read and written, which is the rate of a large copy (4.94); eight
+// tokens 3.0 us, of which an empty launch is 2.1.
 #include "step.h"
 
 namespace sbvr {

@@ -6,10 +6,15 @@
 // and finds the biases that fall in the tile with integer LDS atomics -- sums,
 // ors and maxima, so their order does not matter -- and then streams the tile
 // once, memory-bound; a thread clears the entries that it has used.  What a row
-// needs is loaded once, 4096 tokens of the history stay in registers from tile to tile (a longer one is read again, from L2), and a tile's
-// logits are loaded while the one before is stored.  (With a workgroup per tile
-// the chain of loads before the counting bound the kernel: 256 rows of 131072
-// took 63 us.)
+// needs is loaded once, 4096 tokens of the history stay in registers from tile to
+// tile (a longer one is read again, from L2), and a tile's logits are loaded while
+// the one before is stored.  (With a workgroup per tile the chain of loads before
+// the counting bound the kernel: 256 rows of 131072 took 63 us.)
+//
+// Measured in a graph, binary16 to binary32: 256 rows of 131072 with histories of
+// 4000 50 us, 4.0 TB/s read and written (a copy of as many bytes 41 us; the rest is
+// the counting, between whose barriers nothing is stored); one row of 50001 5.5 us,
+// the latency of its chain: row, history, counts, logits.
 #include "step.h"
 
 namespace sbvr {
@@ -233,7 +238,9 @@ template <typename T, typename O>
 int go_logits(const sbvr_logits_args &a, hipStream_t stream)
 {
     // Large tiles and several of them a workgroup, as far as the 512 workgroups
-    // that the chip holds have work; small tiles where there is less.
+    // that the chip holds have work; small tiles where there is less.  Large and
+    // small: 160 rows of 32000 (640 tiles) 22.5 and 17.7 us, 192 rows (768) 21.0 and
+    // 20.3, 256 rows (1024) 22.0 and 24.8, 64 rows of 131072 (1024) 18.6 and 22.0.
     const int tiles = (a.V + 8191) / 8192;
     const long long all = (long long)a.T * tiles;
     if (all <= 768)

@@ -8,6 +8,11 @@
 // follow.  Up to 512 elements a wavefront has a row of its own, four to a
 // workgroup, and no barrier.  Memory-bound for many tokens.
 //
+// Measured in a graph: 4096 rows of 8192 in bfloat16 with both norms and a gate
+// 67.5 us, 5.0 TB/s read and written, the rate of a large copy (4.94); 4096 rows of
+// 1024 10 us and 2048 14.4 us (4.7 TB/s); one row of 4096 3.9 us, of which an empty
+// launch is 2.1 and the rest two latencies and two reductions.
+//
 // Rows need no alignment beyond their elements'.  A piece that would pass the
 // row's end is moved back to end with it: of its elements the first ones belong
 // to the piece before and are neither summed nor stored.
@@ -171,7 +176,10 @@ int go(const NormArgs &a, hipStream_t stream)
 template <typename A, typename X>
 int dispatch(const NormArgs &a, hipStream_t stream)
 {
-    // one piece a thread as far as a workgroup's threads go
+    // One piece a thread as far as a workgroup's threads go: with two pieces for
+    // half the threads one row of 4096 takes 4.6 us instead of 4.2, 4096 rows of
+    // 1024 11.7 instead of 11.0, of 4096 38.0 instead of 36.5 (binary32 stream); four
+    // pieces are slower again.
     if (a.H <= 64 * 8)
         return go<A, X, 1, 64>(a, stream);
     if (a.H <= 128 * 8)

@@ -16,6 +16,11 @@
 // Ancestors: a workgroup's tokens and the 63 before them hold every ancestor
 // of a tree of at most 64, so their parents are staged in LDS and each thread
 // walks up from its token.
+//
+// Measured in a graph: one request of one token 3.9 us, of which an empty launch
+// is 2.1 and the rest the chain of the scan; 4096 requests with trees of up to 64
+// (197 thousand tokens, 5.7 MB in and out) 10.7 us, bound by the scan over the
+// requests and the walks, where a copy of as many bytes takes 1.1.
 #include "step.h"
 
 namespace sbvr {
@@ -214,6 +219,9 @@ int run_plan(const PlanArgs &a, hipStream_t stream)
 int launch_plan(const PlanArgs &a, hipStream_t stream)
 {
     static_assert(1024 * 4 == SBVR_REQUESTS_MAX, "four requests a thread");
+    // 256 requests of eight tokens: 5.6 us with 256 threads, 7.1 with 1024; 512:
+    // 9.2 us with 256 threads of 16 requests, 7.3 with 1024 of four; 4096 of 64:
+    // 27 and 11.
     return a.R <= 256 ? run_plan<256, 1>(a, stream) : run_plan<1024, 4>(a, stream);
 }
 
