@@ -27,11 +27,12 @@
 // What only one block of rows reads is loaded past the caches: 64 trees of 16 at
 // 8192 positions take 359 us so and 404 otherwise.
 // Measured, four query heads on each of eight key/value heads of 128 elements,
-// binary16, pages token by token: 64 requests of one token at 8192 positions 365
-// us (5.9 TB/s; pages head by head 336, 6.4), one request at 4096 14.7 us, of which
-// the join is 3.9; 64 trees of eight 361 us, of 16 359 (6.0 TB/s), of 32 (128 rows)
-// 441 to 465 us, 600 TFLOP/s, by the chip's power; 64 trees of 32 at 2048 131 us and
-// as two blocks of 64 rows 217.  A plain read of as many bytes takes 317 us.
+// binary16, pages token by token: 64 requests of one token at 8192 positions 345 to
+// 358 us (6.1 TB/s; pages head by head 334, 6.4; the block kernel 340 and 352), one
+// request at 4096 13.6 us (15.6), of which the join is 3.9; 64 trees of eight 361
+// us, of 16 359 (6.0 TB/s), of 32 (128 rows) 441 to 465 us, 600 TFLOP/s, by the
+// chip's power; 64 trees of 32 at 2048 131 us and as two blocks of 64 rows 217.  A
+// plain read of as many bytes takes 317 us.
 //
 // Work: the cached positions of all items, in units of one step of a workgroup,
 // are one line that is cut into (up to) SPLITS (as many workgroups as the chip
@@ -868,7 +869,9 @@ __global__ void __launch_bounds__(ATTN_THREADS, WGS) attn_block_kernel(AttnArgs 
     constexpr int WAVE_ROWS = TILE / ATTN_WAVES; // positions of a tile that a wavefront brings in
     constexpr int LOAD_ROWS = 64 / PIECES;       // of them in one load
     constexpr int LOADS = WAVE_ROWS / LOAD_ROWS; // loads, of keys and of values
-    __shared__ v4u tile[STAGES][2][TILE][PIECES];  // [stage][keys, values][position][piece, permuted]
+    // [stage][keys, values][position][piece, permuted]; aligned, since offsets are
+    // put together by exclusive or
+    __shared__ __attribute__((aligned(1024))) v4u tile[STAGES][2][TILE][PIECES];
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int c = lane & 15, g = lane >> 4;
