@@ -434,6 +434,23 @@ def test_attention_repeats_its_bits():
     assert torch.equal(a[0], a[1]) and torch.equal(a[0], a[2])
 
 
+MANY = [
+    # news, contexts, heads, kv heads, dim, dtype: items short and long, two units of work and more a workgroup
+    ([1, 1, 0, 1, 2] * 60, [(37 * r) % 311 for r in range(300)], 8, 8, 64, torch.bfloat16),
+    ([1, 3, 1, 0] * 33, [(53 * r) % 509 for r in range(132)], 16, 8, 128, torch.float16),
+    ([9, 1, 16, 0, 2, 12] * 5, [900, 3, 0, 700, 1700, 64] * 5, 16, 8, 128, torch.bfloat16),
+    ([33, 3, 17, 40] * 6, [2500, 10, 40, 1300] * 6, 16, 8, 80, torch.float16),
+    ([33, 64, 3, 33] * 6, [2450, 0, 140, 1400] * 6, 16, 8, 64, torch.bfloat16),
+]
+
+
+@pytest.mark.parametrize("case", range(len(MANY)))
+def test_attention_many_items(case):
+    news, ctx, H, KH, D, dtype = MANY[case]
+    got, want, size, _ = run_attention(news, ctx, H, KH, D, 16, dtype, seed=case, extra=1)
+    compare_attention(got, want, size, dtype, max(ctx) + max(news), sum(news))
+
+
 # ---------------------------------------------------------------------------
 # the norms
 # ---------------------------------------------------------------------------
@@ -683,6 +700,16 @@ def test_logits_long_history():
     got = check_logits(c)
     want = -0.25 * np.bincount(h[1000:], minlength=V)
     assert (got[0].cpu().numpy() == want).all()
+
+
+@pytest.mark.parametrize("V", [65536, 65543])
+@pytest.mark.parametrize("parts", ["history+params+bias+grammar+tree", "params"])
+def test_logits_many_tiles(V, parts):
+    c = logits_case(20, 5, V, torch.float16, 300, V, parts) if "tree" in parts else logits_case(100, 1, V, torch.float16, 300, V, parts)
+    want, size = logits_reference(c)
+    compare_logits(check_logits(c, torch.float32), want, size, torch.float32)
+    in_place = c["logits"].clone()
+    compare_logits(check_logits(dict(c, logits=in_place), out=in_place), want, size, torch.float16)
 
 
 # ---------------------------------------------------------------------------
