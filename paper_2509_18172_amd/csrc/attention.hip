@@ -30,7 +30,7 @@
 // binary16, pages token by token: 64 requests of one token at 8192 positions 345 to
 // 358 us (6.1 TB/s; pages head by head 334, 6.4; the block kernel 340 and 352), one
 // request at 4096 13.6 us (15.6), of which the join is 3.9; 64 trees of eight 361
-// us, of 16 359 (6.0 TB/s), of 32 (128 rows) 441 to 465 us, 600 TFLOP/s, by the
+// us, of 16 345 to 359 (6.1 TB/s), of 32 (128 rows) 441 to 465 us, 600 TFLOP/s, by the
 // chip's power; 64 trees of 32 at 2048 131 us and as two blocks of 64 rows 217.  A
 // plain read of as many bytes takes 317 us.
 //
@@ -1199,6 +1199,9 @@ Shape shape_of(int max_new, int heads, int kv_heads)
 // Workgroups a CU, by registers.  Narrow heads of few rows need few: four finished
 // 64 requests of up to 2047 positions, 64 wide, in 41 us and two in 45 when this
 // was chosen; at 8192 positions, where starting up counts less, 199 and 192 us.
+// Up to 64 rows of 128 elements with one (and seven tiles ahead), two and three (two
+// tiles ahead): 64 trees of 16 at 8192 positions 479, 345 and 426 us, 16 trees 136,
+// 114 and 122, one tree 25.6, 26.8 and 31.6.
 constexpr int wgs_of(Shape s, int dp) { return s == ROWS16 && dp == 64 ? 4 : 2; }
 
 // Rows up to which a join has a workgroup for each.  With that and with a
