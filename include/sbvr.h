@@ -451,8 +451,9 @@ int sbvr_cache_write(const sbvr_kv_cache *cache, int T, const void *k, int64_t k
  *     out[t][h] = sum_p w_p v_p / sum_p w_p,  w_p = exp(scale q[t][h] . k_p - max)
  * over the positions p that t sees; a token that sees none gets 0.  Scores,
  * exponentials' sums and products are accumulated in binary32; the weights
- * are rounded to the cache's type for the product with the values; the output
- * is rounded once.  What lies in a slot that a token does not see has no
+ * are rounded to the cache's type for the product with the values (in binary16
+ * by 2^-32 of a row's largest weight where they are small); the output is
+ * rounded once.  What lies in a slot that a token does not see has no
  * effect on it, NaN and infinities included.
  *   q            [T][heads][head_dim] of the cache's dtype, with strides as
  *                sbvr_cache_write's inputs; heads a multiple of kv_heads.

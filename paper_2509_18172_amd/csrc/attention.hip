@@ -42,10 +42,16 @@
 // second kernel joins them.  Which workgroup has what follows from the lengths
 // alone.
 //
-// A row's running maximum is moved only when a score passes it by 2^GAP: the
-// weights then stay within the 16-bit types' range, sums and products are
-// binary32, and most tiles need neither the maximum over lanes nor the
-// rescaling of the sums.
+// A row's running maximum is moved only when a score passes it by 2^GAP: most
+// tiles then need neither the maximum over lanes nor the rescaling of the sums,
+// which are binary32.  The weights are rounded to the cache's type, once: the
+// matrix cores take both factors of a product in one type, a second product for
+// the rest would be half of the matrix work again, and a weight's relative error
+// (2^-8 or 2^-11 at most) is that of the values, which are stored so.  The sum of
+// weights takes the rounded ones, so that a row of equal values keeps them.  So
+// that small weights are not lost in binary16, whose numbers end at 2^-24, the
+// maximum itself has the weight 2^LIFT there: a small weight is off by 2^-32 of
+// the largest one at most, and 131072 of them together by 2^-15.
 //
 // A request's last positions are the step's own tokens, which a row sees as
 // its tree mask says; tiles that reach into them, or into pages outside the
@@ -66,10 +72,15 @@ constexpr int ATTN_WAVES = 4, ATTN_THREADS = 64 * ATTN_WAVES;
 constexpr int TILE = 32;              // positions of one score / product step
 constexpr int CUS = 256;
 constexpr float NO_SCORE = -3.0e38f;  // running maximum before any score
-constexpr float GAP = 8.f;            // binary exponent by which weights may exceed 1
+constexpr int GAP = 8;                // binary exponent by which a weight may exceed the running maximum's
 constexpr float LOG2E = 1.4426950408889634f;
 
 __device__ __forceinline__ float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// binary exponent of the running maximum's weight; 2^(LIFT + GAP) is a number of
+// the type
+template <bool BF>
+constexpr int LIFT = BF ? 0 : 7;
 
 template <bool BF>
 __device__ __forceinline__ v4f mfma(v4u a, v4u b, v4f c)
@@ -340,7 +351,7 @@ struct Rows {
     v4u q[NT][DS];
     uint64_t mask[NT];
     v4f acc[NT][DV], sum[NT];  // sum: every element is the lane's row's sum of weights
-    float m[NT];
+    float m[NT];  // the running maximum, in binary exponents, less LIFT
     float scale2;
 
     // Rows row0 .. row0 + rows - 1 of the item: begin() sends the loads off,
@@ -424,12 +435,14 @@ struct Rows {
     }
 
     // Weights of the tile, as the products' operand.  They are formed with the
-    // maximum so far; only where one exceeds 2^GAP (compared as integers, two at
-    // a time: they are not negative) is the maximum moved and the tile done again.
+    // maximum so far; only where one exceeds 2^(LIFT + GAP) (compared as integers,
+    // two at a time: they are not negative) is the maximum moved and the tile done
+    // again.
     __device__ __forceinline__ void weights(const v4f (&s)[NT][2], v4u (&pf)[NT])
     {
         typedef uint16_t v2s __attribute__((ext_vector_type(2)));
-        constexpr uint32_t LIMIT = BF ? 0x43804380u : 0x5c005c00u;  // 2^GAP, twice
+        // 2^(LIFT + GAP), twice
+        constexpr uint32_t LIMIT = 0x10001u * (BF ? (127 + LIFT<BF> + GAP) << 7 : (15 + LIFT<BF> + GAP) << 10);
         const v2s limit = __builtin_bit_cast(v2s, LIMIT);
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
@@ -441,7 +454,7 @@ struct Rows {
             if (__ballot(__builtin_bit_cast(uint32_t, most) != LIMIT)) {
                 float top = fmaxf(fmaxf(fmaxf(s[nt][0][0], s[nt][0][1]), fmaxf(s[nt][0][2], s[nt][0][3])),
                                   fmaxf(fmaxf(s[nt][1][0], s[nt][1][1]), fmaxf(s[nt][1][2], s[nt][1][3])));
-                top = fmaxf(max4(top * scale2), m[nt]);
+                top = fmaxf(max4(top * scale2) - LIFT<BF>, m[nt]);
                 const float keep = fast_exp2(m[nt] - top);
                 m[nt] = top;
                 sum[nt] *= keep;

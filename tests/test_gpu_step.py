@@ -858,3 +858,38 @@ def test_helpers_fill_what_they_are_given():
     got = sb.tree_attention(s["q"], s["cache"], s["table"], s["ctx"], p.query_start, p.tree_mask, s["N"], out=out, workspace=ws)
     assert got.data_ptr() == out.data_ptr()
     assert torch.equal(out, sb.tree_attention(s["q"], s["cache"], s["table"], s["ctx"], p.query_start, p.tree_mask, s["N"]))
+
+
+# ---------------------------------------------------------------------------
+# attention: many small weights beside a large one
+# ---------------------------------------------------------------------------
+
+SHAPES = [  # new tokens, heads, kv heads: up to 16, 64 and 128 rows a key/value head
+    (1, 8, 8), (8, 16, 4), (16, 16, 2)]
+
+
+@pytest.mark.parametrize("new,heads,kv_heads", SHAPES)
+@pytest.mark.parametrize("dim", [64, 128])
+def test_attention_many_small_weights(new, heads, kv_heads, dim):
+    """Every 32nd position has the weight 1, all others e^-17.5 (2^-25.2, less
+    than half of the smallest binary16 number) and values 60000 times as large,
+    so that together they are a few percent of the result."""
+    N, P, gap, large = 4096, 16, 17.5, 60000.0
+    pages = N // P + 5
+    cache = make_cache(pages, P, kv_heads, dim, torch.float16, "token", fill=0.0)
+    k, v = cache.k.view(-1, kv_heads, dim), cache.v.view(-1, kv_heads, dim)
+    v.fill_(large)
+    k[:N:32, :, 0], v[:N:32] = gap, 1.0
+    table = torch.arange(pages, device=DEV, dtype=torch.int32).view(1, -1)
+    q = torch.zeros(new, heads, dim, dtype=torch.float16, device=DEV)
+    q[..., 0] = 1.0
+    mask = tree_batch([new], 1, "chain")
+    got = sb.tree_attention(q, cache, table, i32([N]), i32([0, new]), torch.tensor(mask, device=DEV), new, scale=1.0)
+    want, size = attention_reference(q, cache, table, [N], [0, new], mask, new, 1.0)
+    # A weight is rounded to a multiple of 2^-24 at the most, where the largest of its tile stands for 2^7 or
+    # more: 2^-32 of it, times 31 of 32 positions and their values.  Then the binary32 exponentials and the
+    # rounding of the result (attention_bound's terms without its allowance for vanished weights).
+    bound = 31 * 2.0 ** -32 * large + 1.01 * 2.0 ** -11 * (size + np.abs(want)) + 2.0 ** -15 * size
+    assert want.min() > 1.04
+    err = np.abs(got.double().cpu().numpy() - want)
+    assert (err <= bound).all(), (err / bound).max()
