@@ -893,3 +893,31 @@ def test_attention_many_small_weights(new, heads, kv_heads, dim):
     assert want.min() > 1.04
     err = np.abs(got.double().cpu().numpy() - want)
     assert (err <= bound).all(), (err / bound).max()
+
+
+# ---------------------------------------------------------------------------
+# attention: infinite keys, every head size
+# ---------------------------------------------------------------------------
+
+@pytest.mark.parametrize("new,heads,kv_heads", SHAPES)
+@pytest.mark.parametrize("dim", [8, 32, 40, 64, 72, 80, 96, 104, 128])
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("element", [0, 7])
+def test_attention_scores_of_minus_infinity(new, heads, kv_heads, dim, dtype, element):
+    """A key that gives every row the score -infinity has the weight 0, in the
+    context and among the step's own tokens, whatever the head's size."""
+    gen = torch.Generator(device=DEV).manual_seed(dim + element)
+    N, P = 150, 16
+    pages = (N + new + P - 1) // P
+    cache = make_cache(pages, P, kv_heads, dim, dtype, "token", gen=gen)
+    flat = cache.k.view(-1, kv_heads, dim)
+    for p in (3, 40, 149, N):  # (the first own token: the others see themselves)
+        flat[p, :, element] = float("-inf")
+    table = torch.arange(pages, device=DEV, dtype=torch.int32).view(1, -1)
+    q = torch.randn(new, heads, dim, generator=gen, device=DEV).to(dtype)
+    q[..., element] = q[..., element].abs() + 0.25
+    mask = tree_batch([new], 1, "chain")
+    got = sb.tree_attention(q, cache, table, i32([N]), i32([0, new]), torch.tensor(mask, device=DEV), new)
+    want, size = attention_reference(q, cache, table, [N], [0, new], mask, new, dim ** -0.5)
+    assert np.isfinite(want).all()
+    compare_attention(got, want, size, dtype, N + new, new)
