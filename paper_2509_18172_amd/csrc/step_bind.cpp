@@ -116,6 +116,14 @@ RowsOf rows(const Tensor &t, at::ScalarType type, int64_t n, int64_t width, cons
     return {t.data_ptr(), t.stride(0)};
 }
 
+// The stride of rows that the library must find whole, one after the other: what
+// the tensor says, which the library refuses where the rows overlap (an expanded
+// view has 0).  A single row's means nothing, and torch may report a smaller one.
+int64_t whole_rows(const Tensor &t, const RowsOf &r)
+{
+    return t.size(0) > 1 ? r.stride : std::max(r.stride, t.size(1));
+}
+
 int narrow(int64_t v, const char *what)
 {
     require(v >= INT32_MIN && v <= INT32_MAX, what);
@@ -132,8 +140,7 @@ Table table_of(const Tensor &t, int64_t R, const at::Device &device)
 {
     require(t.dim() == 2, "page_table must have two dimensions");
     const RowsOf r = rows(t, at::kInt, R, t.size(1), device, "page_table");
-    // a single row's stride means nothing, and torch may report a smaller one
-    return {(int32_t *)r.p, narrow(t.size(1), "page_table is too wide"), std::max(r.stride, t.size(1))};
+    return {(int32_t *)r.p, narrow(t.size(1), "page_table is too wide"), whole_rows(t, r)};
 }
 
 sbvr_kv_cache cache_of(const Tensor &k, const Tensor &v)
@@ -314,7 +321,7 @@ Tensor adjust_logits(const Tensor &logits, const Maybe &history, const Maybe &hi
         require(grammar->dim() == 2, "grammar must have two dimensions");
         masks = grammar->size(0);
         g = rows(*grammar, at::kInt, masks, (V + 31) / 32, device, "grammar");
-        g.stride = std::max(g.stride, grammar->size(1));
+        g.stride = whole_rows(*grammar, g);
     }
     const auto i32 = at::kInt, f32 = at::kFloat;
     const int64_t n_bias = bias_tokens && bias_tokens->dim() == 1 ? bias_tokens->size(0) : 0;

@@ -115,7 +115,8 @@ def adjust_logits(logits, history=None, history_start=None, prompt_lens=None, re
                   n_requests=None, out=None, out_dtype=None, stream=None):
     """The logits [T][V] (fp16, bf16 or fp32) with the penalties, biases,
     temperatures and grammar masks of their requests applied (every part
-    optional); out may be logits.  The number of requests R comes from the
+    optional); out may be logits.  One grammar for all rows is a row of it and
+    grammar_rows of zeros (its rows must not overlap).  The number of requests R comes from the
     parameters per request or the starts, or n_requests; without token_request
     row t is request t."""
     return _native.adjust_logits(logits, history, history_start, prompt_lens, repetition, frequency, presence,

@@ -921,3 +921,24 @@ def test_attention_scores_of_minus_infinity(new, heads, kv_heads, dim, dtype, el
     want, size = attention_reference(q, cache, table, [N], [0, new], mask, new, dim ** -0.5)
     assert np.isfinite(want).all()
     compare_attention(got, want, size, dtype, N + new, new)
+
+
+def test_helpers_refuse_rows_that_overlap():
+    """An expanded page table or grammar, and rows closer than they are wide:
+    the rows past the first would be looked for behind it."""
+    s = step_inputs(1)
+    p = sb.batch_plan(s["ctx"], s["new"], s["free"], s["table"], s["P"], s["T"], parents=s["parents"])
+    table, words = s["table"][0].clone(), torch.zeros(32, dtype=torch.int32, device=DEV)
+    for rows in (lambda t, n: t.expand(n, -1), lambda t, n: t.as_strided((n, t.numel() - n + 1), (1, 1))):
+        with pytest.raises(sb.SBVRError):
+            sb.batch_plan(s["ctx"], s["new"], s["free"], rows(table, 3), s["P"], s["T"])
+        with pytest.raises(sb.SBVRError):
+            sb.tree_attention(s["q"], s["cache"], rows(table, 3), s["ctx"], p.query_start, p.tree_mask, s["N"])
+        with pytest.raises(sb.SBVRError):
+            grammar = rows(words, s["T"])
+            V = 32 * grammar.shape[1] - 24
+            sb.adjust_logits(torch.zeros(s["T"], V, device=DEV), grammar=grammar)
+    # one row for all is a row number for all
+    l = torch.zeros(s["T"], 1000, device=DEV)
+    got = sb.adjust_logits(l, grammar=words.view(1, 32), grammar_rows=torch.zeros(s["T"], dtype=torch.int32, device=DEV))
+    assert bool(torch.isneginf(got).all())
