@@ -24,9 +24,10 @@ struct Api {
     decltype(&sbvr_adjust_logits) adjust_logits;
 } api;
 
-// SBVRError and torch's query of a device's current stream; never released, as
-// the interpreter may be gone before this module's statics are
-py::handle status_error, current_stream;
+// SBVRError, torch's query of a device's current stream and its change of the
+// current device (which returns the one before); never released, as the
+// interpreter may be gone before this module's statics are
+py::handle status_error, current_stream, exchange_device;
 
 [[noreturn]] void refuse(const std::string &what)
 {
@@ -48,11 +49,44 @@ void check(int status, const char *call)
     }
 }
 
-hipStream_t stream_of(const py::object &stream, const at::Device &device)
-{
-    const py::object handle = stream.is_none() ? current_stream(device.index()) : stream.attr("cuda_stream");
-    return (hipStream_t)handle.cast<uintptr_t>();
-}
+// The GPU of a call's tensors as the current one, as long as the call lasts, and
+// the stream of the call.  A default stream's handle is 0 on every GPU, and the
+// runtime takes that for the current one's.
+class Scope {
+  public:
+    Scope(const at::Device &device, const py::object &stream)
+        : now(device.index()), before(exchange_device(now).cast<int>())
+    {
+        try {
+            const py::object handle = stream.is_none() ? current_stream(now) : stream.attr("cuda_stream");
+            require(stream.is_none() || stream.attr("device_index").cast<int>() == now,
+                    "stream must be one of the tensors' GPU");
+            raw = (hipStream_t)handle.cast<uintptr_t>();
+        } catch (...) {
+            leave();
+            throw;
+        }
+    }
+    ~Scope() { leave(); }
+    Scope(const Scope &) = delete;
+    Scope &operator=(const Scope &) = delete;
+    hipStream_t stream() const { return raw; }
+
+  private:
+    void leave() noexcept
+    {
+        if (before == now)
+            return;
+        try {
+            exchange_device(before);
+        } catch (py::error_already_set &e) {
+            e.discard_as_unraisable("the current GPU");
+        }
+    }
+
+    int now, before;
+    hipStream_t raw;
+};
 
 int dtype_of(const Tensor &t)
 {
@@ -170,6 +204,7 @@ py::tuple batch_plan(const Tensor &context_lens, const Tensor &new_lens, const T
 {
     require(context_lens.is_cuda() && context_lens.dim() == 1, "context_lens must be a list on a GPU");
     const at::Device device = context_lens.device();
+    const Scope scope(device, stream);
     const int64_t R = context_lens.size(0), T = n_tokens;
     const Table table = table_of(page_table, R, device);
     require(T >= 0, "n_tokens must not be negative");
@@ -190,7 +225,7 @@ py::tuple batch_plan(const Tensor &context_lens, const Tensor &new_lens, const T
                          dense<int32_t>(o[2], i32, {T}, device, "positions"),
                          dense<int64_t>(o[3], i64, {T}, device, "slots"),
                          dense<uint64_t>(o[4], i64, {T}, device, "tree_mask"),
-                         dense<int32_t>(o[5], i32, {2}, device, "used"), stream_of(stream, device)),
+                         dense<int32_t>(o[5], i32, {2}, device, "used"), scope.stream()),
           "sbvr_batch_plan");
     return py::make_tuple(o[0], o[1], o[2], o[3], o[4], o[5]);
 }
@@ -200,12 +235,12 @@ void cache_write(const Tensor &k_cache, const Tensor &v_cache, const Tensor &k, 
 {
     const sbvr_kv_cache cache = cache_of(k_cache, v_cache);
     const at::Device device = k_cache.device();
+    const Scope scope(device, stream);
     const void *kp = heads_of(k, cache.kv_heads, k_cache, "k"), *vp = heads_of(v, cache.kv_heads, k_cache, "v");
     const int64_t T = k.size(0);
     require(v.size(0) == T, "k and v must have the same tokens");
     check(api.cache_write(&cache, narrow(T, "too many tokens"), kp, k.stride(0), k.stride(1), vp, v.stride(0),
-                          v.stride(1), dense<int64_t>(slots, at::kLong, {T}, device, "slots"),
-                          stream_of(stream, device)),
+                          v.stride(1), dense<int64_t>(slots, at::kLong, {T}, device, "slots"), scope.stream()),
           "sbvr_cache_write");
 }
 
@@ -215,6 +250,7 @@ Tensor tree_attention(const Tensor &q, const Tensor &k_cache, const Tensor &v_ca
 {
     const sbvr_kv_cache cache = cache_of(k_cache, v_cache);
     const at::Device device = k_cache.device();
+    const Scope scope(device, stream);
     require(q.dim() == 3 && context_lens.dim() == 1, "q must have three dimensions, context_lens one");
     const int64_t T = q.size(0), H = q.size(1), D = q.size(2), R = context_lens.size(0);
     const void *qp = heads_of(q, H, k_cache, "q");
@@ -239,7 +275,7 @@ Tensor tree_attention(const Tensor &q, const Tensor &k_cache, const Tensor &v_ca
                              dense<uint64_t>(tree_mask, at::kLong, {T}, device, "tree_mask"), n,
                              scale ? (float)*scale : 1.f / std::sqrt((float)D), op,
                              ws.defined() ? ws.data_ptr() : nullptr, ws.defined() ? (size_t)ws.numel() : 0,
-                             stream_of(stream, device)),
+                             scope.stream()),
           "sbvr_tree_attention");
     return o;
 }
@@ -250,6 +286,7 @@ py::tuple residual_norm(const Tensor &x, const Maybe &y, const Maybe &post_weigh
 {
     require(x.dim() == 2 && x.is_cuda() && dtype_of(x) >= 0, "x must be a GPU tensor [tokens][width] of fp16, bf16 or fp32");
     const at::Device device = x.device();
+    const Scope scope(device, stream);
     const int64_t T = x.size(0), H = x.size(1);
     const at::ScalarType xt = x.scalar_type(), type = (y ? *y : pre_weight ? *pre_weight : x).scalar_type();
     const RowsOf xr = rows(x, xt, T, H, device, "x");
@@ -278,7 +315,7 @@ py::tuple residual_norm(const Tensor &x, const Maybe &y, const Maybe &post_weigh
     check(api.residual_norm(narrow(T, "too many tokens"), narrow(H, "too wide"), dtype_of(typed), dtype_of(x), xr.p,
                             xr.stride, yr.p, yr.stride, dense(post_weight, type, {H}, device, "post_weight"), gr.p,
                             gr.stride, (float)scale, dense(pre_weight, type, {H}, device, "pre_weight"), (float)eps, xo.p,
-                            xo.stride, hr.p, hr.stride, stream_of(stream, device)),
+                            xo.stride, hr.p, hr.stride, scope.stream()),
           "sbvr_residual_norm");
     if (!h.defined())
         return py::make_tuple(x2, py::none());
@@ -295,6 +332,7 @@ Tensor adjust_logits(const Tensor &logits, const Maybe &history, const Maybe &hi
     require(logits.dim() == 2 && logits.is_cuda() && dtype_of(logits) >= 0,
             "logits must be a GPU tensor [rows][vocabulary] of fp16, bf16 or fp32");
     const at::Device device = logits.device();
+    const Scope scope(device, stream);
     const int64_t T = logits.size(0), V = logits.size(1);
     require(!history == !history_start, "history and history_start go together");
     require(!bias_tokens == !bias_start && !bias_tokens == !bias_values, "the three bias tensors go together");
@@ -353,13 +391,14 @@ Tensor adjust_logits(const Tensor &logits, const Maybe &history, const Maybe &hi
     a.draft_tokens = dense<int32_t>(draft_tokens, i32, {T}, device, "draft_tokens");
     a.query_start = dense<int32_t>(query_start, i32, {R + 1}, device, "query_start");
     a.tree_mask = dense<uint64_t>(tree_mask, at::kLong, {T}, device, "tree_mask");
-    check(api.adjust_logits(&a, stream_of(stream, device)), "sbvr_adjust_logits");
+    check(api.adjust_logits(&a, scope.stream()), "sbvr_adjust_logits");
     return o;
 }
 
-// The library's functions by name, the class of its errors, and torch's query
-// of a device's current stream.
-void connect(const std::map<std::string, uintptr_t> &address, const py::object &error, const py::object &stream)
+// The library's functions by name, the class of its errors, torch's query of a
+// device's current stream and its change of the current device.
+void connect(const std::map<std::string, uintptr_t> &address, const py::object &error, const py::object &stream,
+             const py::object &device)
 {
     api.batch_plan = (decltype(api.batch_plan))address.at("sbvr_batch_plan");
     api.cache_write = (decltype(api.cache_write))address.at("sbvr_cache_write");
@@ -371,6 +410,8 @@ void connect(const std::map<std::string, uintptr_t> &address, const py::object &
     status_error.inc_ref();
     current_stream = stream;
     current_stream.inc_ref();
+    exchange_device = device;
+    exchange_device.inc_ref();
 }
 
 }  // namespace

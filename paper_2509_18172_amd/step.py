@@ -8,7 +8,8 @@ checked (AssertionError), outputs come from torch, and a non-zero status raises
 A step in order: ``batch_plan`` (pages, slots, masks), per layer
 ``residual_norm`` -> products -> ``cache_write`` -> ``tree_attention`` ->
 products, and ``adjust_logits`` on the last product.  ``stream``: a
-torch.cuda.Stream, by default the tensors' device's current one.
+torch.cuda.Stream of the tensors' device, by default its current one; the call
+is made with that device as the current one.
 """
 from __future__ import annotations
 
@@ -19,7 +20,7 @@ import os
 
 import torch
 
-from . import SBVRError, _lib, _stream
+from . import SBVRError, _lib
 from .build import binding_path
 
 
@@ -31,15 +32,31 @@ def _load():
     loader = importlib.machinery.ExtensionFileLoader("_sbvr_step", path)
     module = importlib.util.module_from_spec(importlib.util.spec_from_loader("_sbvr_step", loader))
     loader.exec_module(module)
-    names = ("sbvr_batch_plan", "sbvr_cache_write", "sbvr_tree_attention_workspace_bytes", "sbvr_tree_attention",
-             "sbvr_residual_norm", "sbvr_adjust_logits")
-    # (the raw query spares building a stream object)
-    current = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: _stream())
-    module.connect({n: C.cast(getattr(_lib, n), C.c_void_p).value for n in names}, SBVRError, current)
     return module
 
 
 _native = _load()
+
+FUNCTIONS = ("sbvr_batch_plan", "sbvr_cache_write", "sbvr_tree_attention_workspace_bytes", "sbvr_tree_attention",
+             "sbvr_residual_norm", "sbvr_adjust_logits")
+
+
+def _exchange_device(index: int) -> int:
+    before = torch.cuda.current_device()
+    torch.cuda.set_device(index)
+    return before
+
+
+def _connect():
+    """Hands the binding the library's functions and what it asks of torch
+    (the raw forms spare objects of streams and devices)."""
+    stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+        lambda index: torch.cuda.current_stream(index).cuda_stream)
+    device = getattr(torch._C, "_cuda_exchangeDevice", None) or _exchange_device
+    _native.connect({n: C.cast(getattr(_lib, n), C.c_void_p).value for n in FUNCTIONS}, SBVRError, stream, device)
+
+
+_connect()
 
 
 class BatchPlan:

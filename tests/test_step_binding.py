@@ -25,29 +25,36 @@ class Shell(torch.Tensor):
         raise AssertionError(f"{func} on a tensor without memory")
 
 
-NAMES = ("sbvr_batch_plan", "sbvr_cache_write", "sbvr_tree_attention_workspace_bytes", "sbvr_tree_attention",
-         "sbvr_residual_norm", "sbvr_adjust_logits")
+class Calls(list):
+    """The calls (name, arguments) that reach the library, and for each the
+    current device then."""
+    def __init__(self):
+        self.status, self.device, self.seen = 0, [0], []
+
+    def exchange(self, index):
+        before, self.device[0] = self.device[0], index
+        return before
 
 
 @pytest.fixture
 def calls():
-    """The list of calls (name, arguments) that reach the library."""
-    noted, kept, address = [], [], {}
-    for name in NAMES:
+    noted, kept, address = Calls(), [], {}
+    for name in step.FUNCTIONS:
         real = getattr(sb._lib, name)
 
         def note(*args, name=name):
             if name == "sbvr_adjust_logits":
                 args = (sb.LogitsStruct.from_buffer_copy(C.string_at(args[0], C.sizeof(sb.LogitsStruct))), *args[1:])
-            if name != "sbvr_tree_attention_workspace_bytes":
-                noted.append((name, args))
-            return 0
+            if name == "sbvr_tree_attention_workspace_bytes":
+                return 0
+            noted.append((name, args))
+            noted.seen.append(noted.device[0])
+            return noted.status
         kept.append(C.CFUNCTYPE(real.restype, *real.argtypes)(note))
         address[name] = C.cast(kept[-1], C.c_void_p).value
-    step._native.connect(address, sb.SBVRError, lambda index: 0)
+    step._native.connect(address, sb.SBVRError, lambda index: 0, noted.exchange)
     yield noted
-    real = {name: C.cast(getattr(sb._lib, name), C.c_void_p).value for name in NAMES}
-    step._native.connect(real, sb.SBVRError, getattr(torch._C, "_cuda_getCurrentRawStream", lambda index: 0))
+    step._connect()
 
 
 def plan(R=3, T=4, table=None, device="cuda:0", **more):
@@ -97,3 +104,49 @@ def test_a_single_rows_stride_means_nothing(calls, stride):
     adjust(V=320, grammar=Shell(1, 10, stride=(stride, 1)))
     (_, a), (_, b), (_, c) = calls
     assert min(a[10], b[9], c[0].grammar_stride) >= 10
+
+
+# ---------------------------------------------------------------------------
+# devices
+# ---------------------------------------------------------------------------
+
+def norm(device):
+    x, w = Shell(2, 64, dtype=torch.float16, device=device), Shell(64, dtype=torch.float16, device=device)
+    return sb.residual_norm(x, pre_weight=w, h_out=Shell(2, 64, dtype=torch.float16, device=device))
+
+
+def write(device):
+    half = [Shell(*shape, dtype=torch.float16, device=device) for shape in ((5, 16, 2, 64), (4, 2, 64))]
+    sb.cache_write(sb.KVCache(half[0], half[0]), half[1], half[1], Shell(4, dtype=torch.int64, device=device))
+
+
+CALLS = {"batch_plan": lambda device: plan(device=device), "tree_attention": lambda device: attend(device=device),
+         "adjust_logits": lambda device: adjust(device=device), "residual_norm": norm, "cache_write": write}
+
+
+@pytest.mark.parametrize("name", CALLS)
+def test_a_call_is_made_on_its_tensors_device(calls, name):
+    """The default stream has the handle 0 on every GPU, which the runtime
+    takes for the current one's: the tensors' GPU is the current one while the
+    library is called, and the one before it afterwards."""
+    for device in (1, 0, 3):
+        CALLS[name](f"cuda:{device}")
+        assert [c[0] for c in calls] == ["sbvr_" + name] and calls.seen == [device] and calls.device == [0]
+        calls.clear()
+        calls.seen.clear()
+
+
+@pytest.mark.parametrize("name", CALLS)
+def test_the_device_is_left_when_a_call_is_refused(calls, name):
+    calls.status = -1
+    with pytest.raises(sb.SBVRError):
+        CALLS[name]("cuda:2")
+    assert calls.seen == [2] and calls.device == [0]
+
+
+def test_a_stream_of_another_device_is_refused(calls):
+    class Stream:
+        cuda_stream, device_index = 64, 1
+    with pytest.raises(AssertionError, match="stream"):
+        plan(stream=Stream)
+    assert not calls and calls.device == [0]
