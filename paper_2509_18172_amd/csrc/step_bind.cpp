@@ -4,6 +4,7 @@
 // microseconds on the GPU: from Python, over ctypes, a residual_norm took 10.7
 // us of the host, a batch_plan 14.6.  The library's functions are handed over as
 // addresses by the package, which has loaded it.
+#include <c10/core/StreamGuard.h>
 #include <torch/extension.h>
 
 #include <string>
@@ -51,17 +52,25 @@ void check(int status, const char *call)
 
 // The GPU of a call's tensors as the current one, as long as the call lasts, and
 // the stream of the call.  A default stream's handle is 0 on every GPU, and the
-// runtime takes that for the current one's.
+// runtime takes that for the current one's.  A given stream is torch's current one
+// meanwhile, so that outputs and workspaces come from its memory: what another
+// stream has just freed may still be in use there.
 class Scope {
   public:
     Scope(const at::Device &device, const py::object &stream)
         : now(device.index()), before(exchange_device(now).cast<int>())
     {
         try {
-            const py::object handle = stream.is_none() ? current_stream(now) : stream.attr("cuda_stream");
-            require(stream.is_none() || stream.attr("device_index").cast<int>() == now,
-                    "stream must be one of the tensors' GPU");
-            raw = (hipStream_t)handle.cast<uintptr_t>();
+            if (stream.is_none()) {
+                raw = (hipStream_t)current_stream(now).cast<uintptr_t>();
+            } else {
+                const int index = stream.attr("device_index").cast<int>();
+                require(index == now, "stream must be one of the tensors' GPU");
+                raw = (hipStream_t)stream.attr("cuda_stream").cast<uintptr_t>();
+                current.reset_stream(c10::Stream::unpack3(stream.attr("stream_id").cast<c10::StreamId>(),
+                                                          (c10::DeviceIndex)index,
+                                                          (c10::DeviceType)stream.attr("device_type").cast<int>()));
+            }
         } catch (...) {
             leave();
             throw;
@@ -75,6 +84,7 @@ class Scope {
   private:
     void leave() noexcept
     {
+        current.reset();
         if (before == now)
             return;
         try {
@@ -86,6 +96,7 @@ class Scope {
 
     int now, before;
     hipStream_t raw;
+    c10::OptionalStreamGuard current;
 };
 
 int dtype_of(const Tensor &t)
@@ -265,8 +276,6 @@ Tensor tree_attention(const Tensor &q, const Tensor &k_cache, const Tensor &v_ca
         ws = *workspace;
     } else if (need) {
         ws = empty({(int64_t)need}, at::kByte, device);
-        if (!stream.is_none())  // its memory is not to be reused before that stream is done with it
-            py::cast(ws).attr("record_stream")(stream);
     }
     check(api.tree_attention(&cache, r, narrow(T, "too many tokens"), h, qp, q.stride(0), q.stride(1), table.p,
                              table.pages, table.stride,

@@ -9,7 +9,8 @@ A step in order: ``batch_plan`` (pages, slots, masks), per layer
 ``residual_norm`` -> products -> ``cache_write`` -> ``tree_attention`` ->
 products, and ``adjust_logits`` on the last product.  ``stream``: a
 torch.cuda.Stream of the tensors' device, by default its current one; the call
-is made with that device as the current one.
+is made with that device and stream as the current ones, so outputs and
+workspaces belong to the stream as they do under ``torch.cuda.stream(stream)``.
 """
 from __future__ import annotations
 

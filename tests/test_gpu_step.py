@@ -942,3 +942,30 @@ def test_helpers_refuse_rows_that_overlap():
     l = torch.zeros(s["T"], 1000, device=DEV)
     got = sb.adjust_logits(l, grammar=words.view(1, 32), grammar_rows=torch.zeros(s["T"], dtype=torch.int32, device=DEV))
     assert bool(torch.isneginf(got).all())
+
+
+def test_memory_of_a_call_belongs_to_its_stream():
+    """What a call on a given stream allocates is no block that the current
+    stream has just freed (its kernels may still use it), and is not handed to the
+    current stream when it is freed."""
+    s = step_inputs(1)
+    side = torch.cuda.Stream()
+    kept = step_run(s)  # (the current stream's own results, of the same sizes)
+    sizes = sorted({t.numel() * t.element_size() for t in kept} | {
+        sb.sbvr_tree_attention_workspace_bytes(3, s["N"], 8, 2, 128), 4 * 4, 2 * 4})
+    freed = [torch.empty(n, dtype=torch.uint8, device=DEV) for n in sizes for _ in range(3)]
+    blocks = {t.data_ptr() for t in freed}
+    del freed
+    torch.cuda.synchronize()
+    before = torch.cuda.current_stream(), torch.cuda.current_device()
+    p = sb.batch_plan(s["ctx"], s["new"], s["free"], s["table"], s["P"], s["T"], parents=s["parents"], stream=side)
+    got = [getattr(p, n) for n in sb.BatchPlan.__slots__]
+    got += step_run(s, stream=side)
+    assert (torch.cuda.current_stream(), torch.cuda.current_device()) == before
+    own = [t for t in got if all(t is not u for u in (s["cache"].k, s["cache"].v))]
+    side.synchronize()
+    assert not blocks & {t.data_ptr() for t in own}
+    mine = {t.data_ptr() for t in own}
+    del got, own, p
+    again = [torch.empty(n, dtype=torch.uint8, device=DEV) for n in sizes for _ in range(3)]
+    assert not mine & {t.data_ptr() for t in again}
