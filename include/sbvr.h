@@ -76,7 +76,7 @@ const char *sbvr_status_string(int status);
  * 1.06 sbvr_gemv_grouped and sbvr_gemv_grouped_a8, 1.07 sbvr_encode_cached,
  * 1.08 the operators between the products of a step: sbvr_batch_plan,
  * sbvr_cache_write, sbvr_tree_attention, sbvr_residual_norm,
- * sbvr_adjust_logits. */
+ * sbvr_adjust_logits, 1.09 sbvr_tree_attention_whole. */
 int sbvr_version(void);
 
 /*
@@ -477,6 +477,20 @@ int sbvr_tree_attention(const sbvr_kv_cache *cache, int R, int T, int heads, con
                         int64_t q_head_stride, const int32_t *page_table, int max_pages, int64_t table_stride,
                         const int32_t *context_lens, const int32_t *query_start, const uint64_t *tree_mask,
                         int max_new, float scale, void *out, void *workspace, size_t ws_bytes, hipStream_t stream);
+
+/*
+ * The same, with every row of out written.  A request that sbvr_tree_attention
+ * would cut, because it brings more new tokens than max_new or has more tokens
+ * than max_pages * page_size, is not computed in part: all its rows are NaN.
+ * (A prompt chunk of more than SBVR_TREE_MAX tokens, for which sbvr_batch_plan
+ * has no masks, is such a request: it goes in several steps.)  Rows of no request,
+ * past query_start[R] or before query_start[0], are 0.
+ */
+int sbvr_tree_attention_whole(const sbvr_kv_cache *cache, int R, int T, int heads, const void *q,
+                              int64_t q_token_stride, int64_t q_head_stride, const int32_t *page_table, int max_pages,
+                              int64_t table_stride, const int32_t *context_lens, const int32_t *query_start,
+                              const uint64_t *tree_mask, int max_new, float scale, void *out, void *workspace,
+                              size_t ws_bytes, hipStream_t stream);
 
 #define SBVR_NORM_MAX_WIDTH 32768
 

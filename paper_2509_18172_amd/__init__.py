@@ -33,7 +33,7 @@ EXPORTED = (
     "sbvr_pack_indexed", "sbvr_unpack_indexed", "sbvr_gemv_indexed", "sbvr_gemv_indexed_a8", "sbvr_encode",
     "sbvr_decompress_indexed", "sbvr_gemm_prefill", "sbvr_gemv_grouped", "sbvr_gemv_grouped_a8",
     "sbvr_encode_cached", "sbvr_batch_plan", "sbvr_cache_write", "sbvr_tree_attention_workspace_bytes",
-    "sbvr_tree_attention", "sbvr_residual_norm", "sbvr_adjust_logits",
+    "sbvr_tree_attention", "sbvr_tree_attention_whole", "sbvr_residual_norm", "sbvr_adjust_logits",
 )
 
 # enum sbvr_dtype and the limits of the operators between the products
@@ -114,6 +114,8 @@ def _load():
         "sbvr_tree_attention_workspace_bytes": (sz, [i32, i32, i32, i32, i32]),
         "sbvr_tree_attention": (i32, [vp, i32, i32, i32, vp, i64, i64, vp, i32, i64, vp, vp, vp, i32, f32, vp, vp, sz,
                                       vp]),
+        "sbvr_tree_attention_whole": (i32, [vp, i32, i32, i32, vp, i64, i64, vp, i32, i64, vp, vp, vp, i32, f32, vp, vp,
+                                            sz, vp]),
         "sbvr_residual_norm": (i32, [i32, i32, i32, i32, vp, i64, vp, i64, vp, vp, i64, f32, vp, f32, vp, i64, vp, i64,
                                      vp]),
         "sbvr_adjust_logits": (i32, [vp, vp]),
@@ -281,6 +283,15 @@ def sbvr_tree_attention(cache, R, T, heads, q, q_token_stride, q_head_stride, pa
     return _lib.sbvr_tree_attention(None if cache is None else C.addressof(cache), R, T, heads, q, q_token_stride,
                                     q_head_stride, page_table, max_pages, table_stride, context_lens, query_start,
                                     tree_mask, max_new, scale, out, workspace, ws_bytes, stream)
+
+
+def sbvr_tree_attention_whole(cache, R, T, heads, q, q_token_stride, q_head_stride, page_table, max_pages, table_stride,
+                              context_lens, query_start, tree_mask, max_new, scale, out, workspace=None, ws_bytes=0,
+                              stream=0) -> int:
+    """cache: a CacheStruct (or None)."""
+    return _lib.sbvr_tree_attention_whole(None if cache is None else C.addressof(cache), R, T, heads, q, q_token_stride,
+                                          q_head_stride, page_table, max_pages, table_stride, context_lens, query_start,
+                                          tree_mask, max_new, scale, out, workspace, ws_bytes, stream)
 
 
 def sbvr_residual_norm(T, H, dtype, x_dtype, x, x_stride, y, y_stride, post_weight, gate, gate_stride, scale,

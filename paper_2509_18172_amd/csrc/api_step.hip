@@ -57,6 +57,35 @@ int check_attn_shape(int R, int max_new, int heads, int kv_heads, int head_dim)
     return SBVR_OK;
 }
 
+int tree_attention(bool whole, const sbvr_kv_cache *cache, int R, int T, int heads, const void *q,
+                   int64_t q_token_stride, int64_t q_head_stride, const int32_t *page_table, int max_pages,
+                   int64_t table_stride, const int32_t *context_lens, const int32_t *query_start,
+                   const uint64_t *tree_mask, int max_new, float scale, void *out, void *workspace, size_t ws_bytes,
+                   hipStream_t stream)
+{
+    int st = check_cache(cache);
+    if (st != SBVR_OK)
+        return st;
+    if ((st = check_attn_shape(R, max_new, heads, cache->kv_heads, cache->head_dim)) != SBVR_OK)
+        return st;
+    if (T < 0 || max_pages < 1 || table_stride < max_pages || !stride_ok(table_stride) ||
+        !piece_stride_ok(q_token_stride) || !piece_stride_ok(q_head_stride) || !isfinite(scale))
+        return SBVR_E_INVALID_ARG;
+    if (T == 0)
+        return SBVR_OK;
+    if (!q || !page_table || !context_lens || !query_start || !tree_mask || !out)
+        return SBVR_E_INVALID_ARG;
+    const size_t need = attn_workspace_bytes(R, max_new, heads, cache->kv_heads, cache->head_dim);
+    if (ws_bytes < need || (need && !workspace))
+        return SBVR_E_WORKSPACE;
+    if (!aligned(q, 16) || !aligned(page_table, 4) || !aligned(context_lens, 4) || !aligned(query_start, 4) ||
+        !aligned(tree_mask, 8) || !aligned(out, 16) || (need && !aligned(workspace, 16)))
+        return SBVR_E_ALIGNMENT;
+    const AttnArgs a{*cache, R, T, heads, max_pages, max_new, whole ? 0 : max_new, q, q_token_stride, q_head_stride,
+                     page_table, table_stride, context_lens, query_start, tree_mask, scale, out, workspace, 0, 0};
+    return launch_attn(a, stream);
+}
+
 }  // namespace
 
 extern "C" {
@@ -116,27 +145,20 @@ int sbvr_tree_attention(const sbvr_kv_cache *cache, int R, int T, int heads, con
                         const int32_t *context_lens, const int32_t *query_start, const uint64_t *tree_mask,
                         int max_new, float scale, void *out, void *workspace, size_t ws_bytes, hipStream_t stream)
 {
-    int st = check_cache(cache);
-    if (st != SBVR_OK)
-        return st;
-    if ((st = check_attn_shape(R, max_new, heads, cache->kv_heads, cache->head_dim)) != SBVR_OK)
-        return st;
-    if (T < 0 || max_pages < 1 || table_stride < max_pages || !stride_ok(table_stride) ||
-        !piece_stride_ok(q_token_stride) || !piece_stride_ok(q_head_stride) || !isfinite(scale))
-        return SBVR_E_INVALID_ARG;
-    if (T == 0)
-        return SBVR_OK;
-    if (!q || !page_table || !context_lens || !query_start || !tree_mask || !out)
-        return SBVR_E_INVALID_ARG;
-    const size_t need = attn_workspace_bytes(R, max_new, heads, cache->kv_heads, cache->head_dim);
-    if (ws_bytes < need || (need && !workspace))
-        return SBVR_E_WORKSPACE;
-    if (!aligned(q, 16) || !aligned(page_table, 4) || !aligned(context_lens, 4) || !aligned(query_start, 4) ||
-        !aligned(tree_mask, 8) || !aligned(out, 16) || (need && !aligned(workspace, 16)))
-        return SBVR_E_ALIGNMENT;
-    const AttnArgs a{*cache, R, T, heads, max_pages, max_new, q, q_token_stride, q_head_stride, page_table,
-                     table_stride, context_lens, query_start, tree_mask, scale, out, workspace, 0};
-    return launch_attn(a, stream);
+    return tree_attention(false, cache, R, T, heads, q, q_token_stride, q_head_stride, page_table, max_pages,
+                          table_stride, context_lens, query_start, tree_mask, max_new, scale, out, workspace, ws_bytes,
+                          stream);
+}
+
+int sbvr_tree_attention_whole(const sbvr_kv_cache *cache, int R, int T, int heads, const void *q,
+                              int64_t q_token_stride, int64_t q_head_stride, const int32_t *page_table, int max_pages,
+                              int64_t table_stride, const int32_t *context_lens, const int32_t *query_start,
+                              const uint64_t *tree_mask, int max_new, float scale, void *out, void *workspace,
+                              size_t ws_bytes, hipStream_t stream)
+{
+    return tree_attention(true, cache, R, T, heads, q, q_token_stride, q_head_stride, page_table, max_pages,
+                          table_stride, context_lens, query_start, tree_mask, max_new, scale, out, workspace, ws_bytes,
+                          stream);
 }
 
 int sbvr_residual_norm(int T, int H, int dtype, int x_dtype, const void *x, int64_t x_stride, const void *y,

@@ -86,6 +86,9 @@ struct PlanArgs {
 struct AttnArgs {
     sbvr_kv_cache kv;
     int R, T, heads, max_pages, max_new;
+    // the most of a request's new tokens that are computed where not all of them
+    // are: max_new, or 0 if every row of the output is to be written
+    int cut;
     const void *q;
     int64_t q_token_stride, q_head_stride;
     const int32_t *page_table;
@@ -96,6 +99,7 @@ struct AttnArgs {
     void *out;
     void *workspace;
     int by_item;  // set by the launcher: joins are numbered by item
+    int joins;    // and the number of joins
 };
 
 struct NormArgs {

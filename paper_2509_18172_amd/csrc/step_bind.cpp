@@ -21,6 +21,7 @@ struct Api {
     decltype(&sbvr_cache_write) cache_write;
     decltype(&sbvr_tree_attention_workspace_bytes) workspace_bytes;
     decltype(&sbvr_tree_attention) tree_attention;
+    decltype(&sbvr_tree_attention_whole) tree_attention_whole;
     decltype(&sbvr_residual_norm) residual_norm;
     decltype(&sbvr_adjust_logits) adjust_logits;
 } api;
@@ -277,14 +278,14 @@ Tensor tree_attention(const Tensor &q, const Tensor &k_cache, const Tensor &v_ca
     } else if (need) {
         ws = empty({(int64_t)need}, at::kByte, device);
     }
-    check(api.tree_attention(&cache, r, narrow(T, "too many tokens"), h, qp, q.stride(0), q.stride(1), table.p,
-                             table.pages, table.stride,
-                             dense<int32_t>(context_lens, at::kInt, {R}, device, "context_lens"),
-                             dense<int32_t>(query_start, at::kInt, {R + 1}, device, "query_start"),
-                             dense<uint64_t>(tree_mask, at::kLong, {T}, device, "tree_mask"), n,
-                             scale ? (float)*scale : 1.f / std::sqrt((float)D), op,
-                             ws.defined() ? ws.data_ptr() : nullptr, ws.defined() ? (size_t)ws.numel() : 0,
-                             scope.stream()),
+    // a new output has no content that rows could keep
+    const auto call = out ? api.tree_attention : api.tree_attention_whole;
+    check(call(&cache, r, narrow(T, "too many tokens"), h, qp, q.stride(0), q.stride(1), table.p, table.pages,
+               table.stride, dense<int32_t>(context_lens, at::kInt, {R}, device, "context_lens"),
+               dense<int32_t>(query_start, at::kInt, {R + 1}, device, "query_start"),
+               dense<uint64_t>(tree_mask, at::kLong, {T}, device, "tree_mask"), n,
+               scale ? (float)*scale : 1.f / std::sqrt((float)D), op, ws.defined() ? ws.data_ptr() : nullptr,
+               ws.defined() ? (size_t)ws.numel() : 0, scope.stream()),
           "sbvr_tree_attention");
     return o;
 }
@@ -413,6 +414,8 @@ void connect(const std::map<std::string, uintptr_t> &address, const py::object &
     api.cache_write = (decltype(api.cache_write))address.at("sbvr_cache_write");
     api.workspace_bytes = (decltype(api.workspace_bytes))address.at("sbvr_tree_attention_workspace_bytes");
     api.tree_attention = (decltype(api.tree_attention))address.at("sbvr_tree_attention");
+    api.tree_attention_whole =
+        (decltype(api.tree_attention_whole))address.at("sbvr_tree_attention_whole");
     api.residual_norm = (decltype(api.residual_norm))address.at("sbvr_residual_norm");
     api.adjust_logits = (decltype(api.adjust_logits))address.at("sbvr_adjust_logits");
     status_error = error;

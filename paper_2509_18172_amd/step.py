@@ -39,7 +39,7 @@ def _load():
 _native = _load()
 
 FUNCTIONS = ("sbvr_batch_plan", "sbvr_cache_write", "sbvr_tree_attention_workspace_bytes", "sbvr_tree_attention",
-             "sbvr_residual_norm", "sbvr_adjust_logits")
+             "sbvr_tree_attention_whole", "sbvr_residual_norm", "sbvr_adjust_logits")
 
 
 def _exchange_device(index: int) -> int:
@@ -112,7 +112,11 @@ def tree_attention(q, cache: KVCache, page_table, context_lens, query_start, tre
     """Attention of a step's tokens q [T][heads][head_dim] over the cache,
     which already holds their keys and values; max_new: the most new tokens of
     a request; scale: 1 / sqrt(head_dim) by default.  Returns [T][heads]
-    [head_dim].  workspace: a uint8 tensor of
+    [head_dim]: 0 in rows of no request (a padded plan's), and NaN in all rows of
+    a request that brings more than max_new tokens, as a prompt chunk of more than
+    64 does, or more than its row of the table holds.  A given out keeps what it
+    has in rows of no request and in those that max_new or the table leave out.
+    workspace: a uint8 tensor of
     sbvr_tree_attention_workspace_bytes, by default a new one."""
     return _native.tree_attention(q, cache.k, cache.v, page_table, context_lens, query_start, tree_mask, max_new, scale,
                                   out, workspace, stream)

@@ -969,3 +969,71 @@ def test_memory_of_a_call_belongs_to_its_stream():
     del got, own, p
     again = [torch.empty(n, dtype=torch.uint8, device=DEV) for n in sizes for _ in range(3)]
     assert not mine & {t.data_ptr() for t in again}
+
+
+# ---------------------------------------------------------------------------
+# attention: rows of no request, and requests that do not fit
+# ---------------------------------------------------------------------------
+
+def poison(shape, dtype):
+    """Leaves memory of this size full of 7s to the next allocation."""
+    t = torch.full(shape, 7.0, dtype=dtype, device=DEV)
+    del t
+
+
+@pytest.mark.parametrize("new,heads,kv_heads", SHAPES)
+@pytest.mark.parametrize("room", [0, 1, 70])
+@pytest.mark.parametrize("requests", [1, 3, 200])
+def test_attention_of_a_padded_plan(new, heads, kv_heads, room, requests):
+    """Rows past the plan's last token are 0, the others what they are without
+    them."""
+    gen = torch.Generator(device=DEV).manual_seed(requests)
+    P, D, R = 16, 64, requests
+    news = [new if r % 2 == 0 else new // 2 for r in range(R)]  # (an empty request among them)
+    ctx = [(37 * r) % 100 for r in range(R)]
+    T, width = sum(news), 8
+    cache = make_cache(R * width, P, kv_heads, D, torch.float16, "token", gen=gen)
+    table = torch.arange(R * width, dtype=torch.int32, device=DEV).view(R, width)
+    q = torch.randn(T + room, heads, D, generator=gen, device=DEV).half()
+    start = i32([sum(news[:r]) for r in range(R + 1)])
+    mask = torch.tensor(tree_batch(news, 3) + [0] * room, device=DEV)
+    given = torch.full((T + room, heads, D), 5.0, dtype=torch.float16, device=DEV)
+    sb.tree_attention(q, cache, table, i32(ctx), start, mask, new, out=given)
+    poison(given.shape, torch.float16)
+    got = sb.tree_attention(q, cache, table, i32(ctx), start, mask, new)
+    assert torch.equal(got[:T], given[:T])
+    assert bool((got[T:] == 0).all()) and bool((given[T:] == 5).all())
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("long", [9, 65, 300])
+def test_attention_of_a_prompt_too_long_for_it(dtype, long):
+    """A request of more new tokens than max_new (beyond 64 the plan has no
+    masks for it), or than its pages hold, is NaN in every row; the requests beside
+    it are not touched."""
+    gen = torch.Generator(device=DEV).manual_seed(long)
+    P, KH, H, D, most = 16, 2, 8, 128, min(long - 1, 64)
+    news, ctx = [3, long, 2, 5], [40, 7, 30, 60]
+    T, pages = sum(news), 25
+    free = torch.arange(200, dtype=torch.int32, device=DEV)
+    table = torch.full((4, pages), -1, dtype=torch.int32, device=DEV)
+    table[:, :4] = torch.arange(200, 216, dtype=torch.int32, device=DEV).view(4, 4)
+    cache = make_cache(216, P, KH, D, dtype, "token", gen=gen)
+    p = sb.batch_plan(i32(ctx), i32(news), free, table, P, T + 4)
+    q = torch.randn(T + 4, H, D, generator=gen, device=DEV).to(dtype)
+    # request 3's table ends inside its new tokens: 60 cached ones and 4 of 5 fit
+    short = table.clone()[:, :4].contiguous() if long < 50 else table
+    cut = [1, 3] if long < 50 else [1]
+    poison(q.shape, dtype)
+    got = sb.tree_attention(q, cache, short, i32(ctx), p.query_start, p.tree_mask, most)
+    start = p.query_start.tolist()
+    want, size = attention_reference(q, cache, short, [c if r not in cut else 0 for r, c in enumerate(ctx)], start,
+                                     [0 if t >= T else m for t, m in enumerate(p.tree_mask.tolist())], 5, D ** -0.5)
+    for r in range(4):
+        rows = got[start[r]:start[r + 1]].double().cpu().numpy()
+        if r in cut:
+            assert np.isnan(rows).all()
+        else:
+            bound = attention_bound(want[start[r]:start[r + 1]], size[start[r]:start[r + 1]], dtype, 80, 8.0)
+            assert (np.abs(rows - want[start[r]:start[r + 1]]) <= bound).all()
+    assert bool((got[T:] == 0).all())

@@ -172,3 +172,15 @@ def test_tensor_helpers_refuse_before_any_launch():
         sb.cache_write(sb.KVCache(kv, kv), x.view(2, 1, 64), x.view(2, 1, 64), i.long())
     with pytest.raises(AssertionError, match="GPU"):
         sb.tree_attention(x.view(2, 1, 64), sb.KVCache(kv, kv), i.view(2, 1), i, i, i.long(), max_new=1)
+
+
+@pytest.mark.parametrize("bad,status", [
+    (dict(R=0), INVALID), (dict(max_new=65), INVALID), (dict(heads=30), INVALID), (dict(stride=19), INVALID),
+    (dict(q=None), INVALID), (dict(out=None), INVALID), (dict(R=4097), UNSUPPORTED), (dict(ws_bytes=100), WORKSPACE),
+    (dict(out=FAKE + 8), ALIGNMENT), (dict(T=0, q=None, out=None, ws=None, ws_bytes=0), sb.SBVR_OK)])
+def test_whole_attention_refuses_alike(bad, status):
+    a = dict(R=2, T=8, heads=32, q=FAKE, qt=4096, qh=128, table=FAKE, pages=20, stride=20, ctx=FAKE, start=FAKE, mask=FAKE,
+             max_new=4, scale=0.1, out=FAKE, ws=FAKE, ws_bytes=1 << 30)
+    assert sb.sbvr_tree_attention_whole(cache(), *{**a, **bad}.values()) == status
+    assert attention(**bad) == status
+    assert sb.sbvr_tree_attention_whole(None, *a.values()) == INVALID
