@@ -197,6 +197,10 @@ int sbvr_adjust_logits(const sbvr_logits_args *a, hipStream_t stream)
         (a->out_dtype != a->dtype && a->out_dtype != SBVR_F32) || !stride_ok(a->logits_stride) ||
         !stride_ok(a->out_stride) || (a->T > 1 && a->out_stride < a->V))
         return SBVR_E_INVALID_ARG;
+    if (a->T > (1 << 16) - 1 || a->V > (1 << 30))
+        return SBVR_E_UNSUPPORTED;
+    if (a->T == 0)  // (an empty list may have no address: the checks of what goes together are for rows)
+        return SBVR_OK;
     if (a->history && !a->history_start)
         return SBVR_E_INVALID_ARG;
     if (a->bias_tokens && (!a->bias_start || !a->bias_values))
@@ -207,10 +211,6 @@ int sbvr_adjust_logits(const sbvr_logits_args *a, hipStream_t stream)
     const int drafts = (a->draft_tokens != nullptr) + (a->query_start != nullptr) + (a->tree_mask != nullptr);
     if (drafts != 0 && drafts != 3)
         return SBVR_E_INVALID_ARG;
-    if (a->T > (1 << 16) - 1 || a->V > (1 << 30))
-        return SBVR_E_UNSUPPORTED;
-    if (a->T == 0)
-        return SBVR_OK;
     if (!a->logits || !a->out)
         return SBVR_E_INVALID_ARG;
     const size_t ia = a->dtype == SBVR_F32 ? 4 : 2, oa = a->out_dtype == SBVR_F32 ? 4 : 2;

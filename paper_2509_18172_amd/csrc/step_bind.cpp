@@ -346,7 +346,7 @@ Tensor adjust_logits(const Tensor &logits, const Maybe &history, const Maybe &hi
     const int64_t T = logits.size(0), V = logits.size(1);
     require(!history == !history_start, "history and history_start go together");
     require(!bias_tokens == !bias_start && !bias_tokens == !bias_values, "the three bias tensors go together");
-    int64_t R = T;
+    int64_t R = std::max<int64_t>(T, 1);  // no rows: a request all the same
     if (n_requests) {
         R = *n_requests;
     } else {

@@ -1037,3 +1037,21 @@ def test_attention_of_a_prompt_too_long_for_it(dtype, long):
             bound = attention_bound(want[start[r]:start[r + 1]], size[start[r]:start[r + 1]], dtype, 80, 8.0)
             assert (np.abs(rows - want[start[r]:start[r + 1]]) <= bound).all()
     assert bool((got[T:] == 0).all())
+
+
+def test_a_whole_step_of_no_tokens():
+    """What an empty plan hands on is taken by every operator of the step."""
+    s = step_inputs(1)
+    p = sb.batch_plan(s["ctx"], i32([0, 0, 0]), s["free"], s["table"], s["P"], 0)
+    before = s["cache"].k.clone()
+    sb.cache_write(s["cache"], s["k"][:0], s["v"][:0], p.slots)
+    assert torch.equal(s["cache"].k, before)
+    assert sb.tree_attention(s["q"][:0], s["cache"], s["table"], s["ctx"], p.query_start, p.tree_mask, s["N"]).shape[0] == 0
+    l = s["logits"][:0]
+    assert sb.adjust_logits(l).shape == (0, 1000)
+    got = sb.adjust_logits(l, frequency=s["freq"], token_request=p.token_request, query_start=p.query_start,
+                           tree_mask=p.tree_mask, draft_tokens=s["draft"][:0], history=s["draft"],
+                           history_start=i32([0, 4, 8, 12]), bias_tokens=s["draft"][:0], bias_values=s["freq"][:0],
+                           bias_start=i32([0, 0, 0, 0]), grammar=torch.empty(0, 32, dtype=torch.int32, device=DEV),
+                           grammar_rows=p.token_request, out_dtype=torch.float32)
+    assert got.shape == (0, 1000) and got.dtype == torch.float32

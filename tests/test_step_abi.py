@@ -184,3 +184,16 @@ def test_whole_attention_refuses_alike(bad, status):
     assert sb.sbvr_tree_attention_whole(cache(), *{**a, **bad}.values()) == status
     assert attention(**bad) == status
     assert sb.sbvr_tree_attention_whole(None, *a.values()) == INVALID
+
+
+def test_logits_of_no_rows_need_no_lists():
+    """An empty tensor has no address: which of the lists are there says nothing
+    where there are no rows.  What is wrong at any size is refused all the same."""
+    none = dict(T=0, logits=None, out=None, token_request=None)
+    for given in (dict(query_start=FAKE), dict(draft_tokens=FAKE), dict(tree_mask=FAKE, query_start=FAKE),
+                  dict(history=FAKE), dict(history_start=FAKE), dict(bias_tokens=FAKE), dict(bias_start=FAKE),
+                  dict(grammar=FAKE, grammar_stride=4, grammar_count=0), dict(grammar=FAKE, grammar_stride=0, grammar_count=0)):
+        assert logits(**none, **given) == sb.SBVR_OK, given
+    for bad in (dict(R=0), dict(V=0), dict(dtype=3), dict(out_dtype=sb.SBVR_BF16), dict(logits_stride=-1)):
+        assert logits(**{**none, **bad}) == INVALID, bad
+    assert logits(**none, V=(1 << 30) + 1) == UNSUPPORTED

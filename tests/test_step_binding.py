@@ -150,3 +150,16 @@ def test_a_stream_of_another_device_is_refused(calls):
     with pytest.raises(AssertionError, match="stream"):
         plan(stream=Stream)
     assert not calls and calls.device == [0]
+
+
+# ---------------------------------------------------------------------------
+# no rows
+# ---------------------------------------------------------------------------
+
+def test_logits_of_no_rows_are_a_request_at_least(calls):
+    """Where nothing says how many requests there are, each row is one; the
+    library takes no fewer than one."""
+    adjust(T=0)
+    adjust(T=0, n_requests=3)
+    adjust(T=2)
+    assert [c[1][0].R for c in calls] == [1, 3, 2]
