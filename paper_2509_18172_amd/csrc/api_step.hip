@@ -182,6 +182,8 @@ int sbvr_residual_norm(int T, int H, int dtype, int x_dtype, const void *x, int6
         return SBVR_OK;
     if (!x || (!x_out && !h_out) || (h_out && !pre_weight))
         return SBVR_E_INVALID_ARG;
+    if (T > 1 && x_out == x && x_out_stride != x_stride)  // rows would be written before they are read
+        return SBVR_E_INVALID_ARG;
     const size_t xa = x_dtype == SBVR_F32 ? 4 : 2;
     if (!aligned(x, xa) || !aligned(x_out, xa) || !aligned(y, 2) || !aligned(post_weight, 2) || !aligned(gate, 2) ||
         !aligned(pre_weight, 2) || !aligned(h_out, 2))

@@ -197,3 +197,10 @@ def test_logits_of_no_rows_need_no_lists():
     for bad in (dict(R=0), dict(V=0), dict(dtype=3), dict(out_dtype=sb.SBVR_BF16), dict(logits_stride=-1)):
         assert logits(**{**none, **bad}) == INVALID, bad
     assert logits(**none, V=(1 << 30) + 1) == UNSUPPORTED
+
+
+def test_norm_in_place_needs_one_stride():
+    """x_out may be x where each row lies on itself; with other strides rows
+    would be written that are still to be read."""
+    assert norm(xs=64, xos=128) == INVALID and norm(xs=128, xos=64) == INVALID
+    assert norm(xs=0, xos=64) == INVALID
