@@ -224,6 +224,9 @@ int sbvr_adjust_logits(const sbvr_logits_args *a, hipStream_t stream)
             return SBVR_E_ALIGNMENT;
     if (!aligned(a->logits, ia) || !aligned(a->out, oa) || !aligned(a->tree_mask, 8))
         return SBVR_E_ALIGNMENT;
+    // elements would be written before they are read
+    if (a->out == a->logits && (a->out_dtype != a->dtype || (a->T > 1 && a->out_stride != a->logits_stride)))
+        return SBVR_E_INVALID_ARG;
     return launch_logits(*a, stream);
 }
 

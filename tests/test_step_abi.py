@@ -204,3 +204,10 @@ def test_norm_in_place_needs_one_stride():
     would be written that are still to be read."""
     assert norm(xs=64, xos=128) == INVALID and norm(xs=128, xos=64) == INVALID
     assert norm(xs=0, xos=64) == INVALID
+
+
+def test_logits_in_place_need_one_type_and_stride():
+    """out may be logits where each element lies on itself."""
+    assert logits() == INVALID  # (binary16 to binary32)
+    same = dict(out_dtype=sb.SBVR_F16)
+    assert logits(**same, out_stride=128) == INVALID and logits(**same, logits_stride=0) == INVALID
