@@ -59,19 +59,32 @@ def binding_path() -> str:
     return os.path.join(HERE, "_lib", "_sbvr_step.so")
 
 
-def build_binding(verbose: bool = False) -> str:
-    """Host code only: compiled against torch's headers, no GPU code in it."""
+def build_binding(verbose: bool = False) -> str | None:
+    """Host code only: compiled against torch's headers, no GPU code in it.
+    Where torch or the C++ compiler is missing nothing is built, and None
+    returned: the library needs neither."""
+    import importlib.util
+    import shutil
+    import sys
     import sysconfig
+
+    out, compiler = binding_path(), os.environ.get("CXX", "g++")
+    os.makedirs(os.path.dirname(out), exist_ok=True)
+    missing = [name for name, there in (("torch", importlib.util.find_spec("torch")), (compiler, shutil.which(compiler)))
+               if not there]
+    if missing:
+        if os.path.exists(out):  # made for another build of the library
+            os.remove(out)
+        print(f"the tensor binding is not built: {' and '.join(missing)} not found", file=sys.stderr)
+        return None
 
     import torch
     from torch.utils.cpp_extension import include_paths, library_paths
 
-    out = binding_path()
-    os.makedirs(os.path.dirname(out), exist_ok=True)
     tmp = out + ".tmp%d" % os.getpid()
     includes = [*include_paths(), sysconfig.get_paths()["include"], os.path.join(ROOT, "include"),
                 os.path.join(os.path.dirname(os.path.dirname(HIPCC)), "include")]
-    cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-fvisibility=hidden",
+    cmd = [compiler, "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-fvisibility=hidden",
            "-DTORCH_EXTENSION_NAME=_sbvr_step", "-DTORCH_API_INCLUDE_EXTENSION_H", "-D__HIP_PLATFORM_AMD__",
            "-D_GLIBCXX_USE_CXX11_ABI=%d" % int(torch._C._GLIBCXX_USE_CXX11_ABI),
            *(f for p in includes for f in ("-isystem", p)), os.path.join(HERE, "csrc", "step_bind.cpp"),
