@@ -13,6 +13,10 @@ tree -- its tokens share the reading of the weights -- and every token whose
 parent is accepted and chose it is accepted too.  The accepted tokens' keys and
 values move to the front of the step's slots, and the next step continues there.
 
+The verified tokens have to be those that single steps choose, up to the first
+choice that rounding may turn: several tokens of a step run other products and
+other attention kernels than one.  The program fails where they are not.
+
     python examples/verify_drafts.py [--tokens 64]
 """
 import argparse
@@ -130,8 +134,15 @@ def draft(text):
     return tokens, parents
 
 
-def generate(model, prompt, n, verify, repetition=1.05):
-    """n greedy tokens after the prompt: (tokens, steps taken)."""
+# Leads over the second choice, in parts of the largest logit, that rounding may
+# turn: some two dozen binary16 roundings of 2^-11 lie between the runs, behind norms
+# that may stretch them a few times, 2e-2 of the largest logit for each of the two.
+NEAR = 4e-2
+
+
+def generate(model, prompt, n, verify, repetition=1.05, propose=draft, leads=None):
+    """n greedy tokens after the prompt: (tokens, steps taken).  propose: the
+    tree for a text; leads: a list that gets each token's lead."""
     text, steps = list(prompt), 0
     for i in range(0, len(prompt) - 1, 64):
         chunk = prompt[i:min(i + 64, len(prompt) - 1)]
@@ -139,7 +150,7 @@ def generate(model, prompt, n, verify, repetition=1.05):
         model.keep(list(range(len(chunk))))
     penalty = torch.tensor([repetition], device="cuda")
     while len(text) < len(prompt) + n:
-        tokens, parents = draft(text) if verify else (text[-1:], [-1])
+        tokens, parents = propose(text) if verify else (text[-1:], [-1])
         logits = model.step(tokens, parents)
         past = torch.tensor(text[:-1], dtype=torch.int32, device="cuda")  # the last one is the tree's root
         plan, T = model.plan, len(tokens)
@@ -149,9 +160,14 @@ def generate(model, prompt, n, verify, repetition=1.05):
                                   tree_mask=plan.tree_mask, draft_tokens=torch.tensor(tokens, dtype=torch.int32, device="cuda"),
                                   out_dtype=torch.float32)
         choice = logits.argmax(dim=1).tolist()
+        if leads is not None:
+            best = logits.topk(2, dim=1).values
+            lead = ((best[:, 0] - best[:, 1]) / logits.abs().amax(dim=1)).tolist()
         accepted = [0]
         while True:
             text.append(choice[accepted[-1]])
+            if leads is not None:
+                leads.append(lead[accepted[-1]])
             child = next((j for j in range(T) if parents[j] == accepted[-1] and tokens[j] == text[-1]), None)
             if child is None:
                 break
@@ -161,16 +177,26 @@ def generate(model, prompt, n, verify, repetition=1.05):
     return text[len(prompt):len(prompt) + n], steps
 
 
+def first_difference(plain, verified):
+    """The number of tokens that both have from the start."""
+    return next((i for i, (a, b) in enumerate(zip(plain, verified)) if a != b), min(len(plain), len(verified)))
+
+
 def main():
     ap = argparse.ArgumentParser(description=__doc__, formatter_class=argparse.RawDescriptionHelpFormatter)
     ap.add_argument("--tokens", type=int, default=64)
     args = ap.parse_args()
     prompt = torch.randint(0, 1000, (100,), generator=torch.Generator().manual_seed(1)).tolist() * 2
-    plain, steps = generate(Decoder(), prompt, args.tokens, verify=False)
+    leads = []
+    plain, steps = generate(Decoder(), prompt, args.tokens, verify=False, leads=leads)
     print(f"plain:    {args.tokens} tokens in {steps} steps")
     verified, steps = generate(Decoder(), prompt, args.tokens, verify=True)
-    same = sum(a == b for a, b in zip(plain, verified))
-    print(f"verified: {args.tokens} tokens in {steps} steps, {same} of them the plain run's")
+    same = first_difference(plain, verified)
+    print(f"verified: {args.tokens} tokens in {steps} steps, the first {same} the plain run's")
+    if same < args.tokens:
+        print(f"token {same} led by {leads[same]:.4f} of the largest logit; rounding may turn {NEAR}")
+        if leads[same] > NEAR:
+            sys.exit("verified decoding is not plain decoding")
 
 
 if __name__ == "__main__":

@@ -69,3 +69,45 @@ def test_generation(example):
     verified, fewer = example.generate(example.Decoder(), prompt, 24, verify=True)
     assert len(verified) == 24 and fewer <= 24
     assert verified[0] == plain[0]
+
+
+@pytest.mark.parametrize("seed", [0, 1, 2])
+def test_verified_tokens_are_the_plain_ones(example, seed):
+    """With drafts that hold the plain run's next three tokens, each beside a
+    wrong one, every step takes four tokens, up to the first choice that
+    rounding may turn; and the tokens are the plain run's."""
+    n, prompt = 40, torch.randint(0, 1000, (50,), generator=torch.Generator().manual_seed(seed)).tolist()
+    leads = []
+    plain, _ = example.generate(example.Decoder(seed=seed), prompt, n + 4, verify=False, leads=leads)
+    known = prompt + plain
+    assert len(plain) == n + 4 and len(leads) == n + 4
+
+    def propose(text):
+        tokens, parents, at = [text[-1]], [-1], 0
+        for token in known[len(text):len(text) + 3]:
+            tokens += [(token + 1) % 1000, token]
+            parents += [at, at]
+            at = len(tokens) - 1
+        return tokens + [(known[min(len(text) + 3, len(known) - 1)] + 1) % 1000], parents + [at]
+    verified, steps = example.generate(example.Decoder(seed=seed), prompt, n, verify=True, propose=propose)
+    same = example.first_difference(plain[:n], verified)
+    assert same == n or leads[same] <= example.NEAR, (same, leads[same])
+    assert same >= 4 and steps <= -(-same // 4) + n - same, (steps, same)
+
+
+def test_the_program_fails_where_tokens_differ(example, monkeypatch):
+    """A step that keeps the wrong tokens is found."""
+    monkeypatch.setattr("sys.argv", ["verify_drafts.py", "--tokens", "24"])
+    example.main()
+    generate, changed = example.generate, []
+
+    def spoilt(model, prompt, n, verify, **more):
+        tokens, steps = generate(model, prompt, n, verify, **more)
+        if verify:
+            tokens[changed[0]] = (tokens[changed[0]] + 1) % 1000
+        else:
+            changed.append(max(range(n), key=lambda i: more["leads"][i]))
+        return tokens, steps
+    monkeypatch.setattr(example, "generate", spoilt)
+    with pytest.raises(SystemExit):
+        example.main()
