@@ -26,16 +26,22 @@
 //   attn_block_kernel (up to 64 or 128 rows): each wavefront has 16 or 32 rows of
 //     its own and all four share the tiles, which go straight into LDS, three of
 //     32 positions ahead (seven where a head has 64 elements); pieces lie permuted
-//     so that both operands' reads are free of bank conflicts.
+//     so that sixteen lanes' reads of an operand meet every bank once.  (The
+//     counters call a third of the LDS cycles conflicts all the same; which
+//     accesses have them has not been found.)
 // What only one block of rows reads is loaded past the caches: 64 trees of 16 at
 // 8192 positions take 359 us so and 404 otherwise.
 // Measured, four query heads on each of eight key/value heads of 128 elements,
 // binary16, pages token by token: 64 requests of one token at 8192 positions 345 to
-// 358 us (6.1 TB/s; pages head by head 334, 6.4; the block kernel 340 and 352), one
-// request at 4096 13.6 us (15.6), of which the join is 3.9; 64 trees of eight 361
-// us, of 16 345 to 359 (6.1 TB/s), of 32 (128 rows) 441 to 465 us, 600 TFLOP/s, by the
-// chip's power; 64 trees of 32 at 2048 131 us and as two blocks of 64 rows 217.  A
-// plain read of as many bytes takes 317 us.
+// 358 us (6.1 TB/s; pages head by head 334 to 337, 6.4), one request at 4096 13.6 to
+// 14.5 us, of which the join is 3.9; 64 trees of eight 361 us, of 16 345 to 366 (5.9 to
+// 6.1 TB/s), of 32 (128 rows) 441 to 465 us, 600 TFLOP/s; 64 trees of 32 at 2048 131 to
+// 133 us and as two blocks of 64 rows 217.  A plain read of as many bytes takes 317
+// us.  With 128 rows the time follows the clock, which falls under this load: four
+// trees of 16 with eight rows a token at 131072 positions, 30 runs, 388 us at 2.18 GHz to
+// 483 at 1.75, the same cycles.  Within a wavefront a tile's scores, weights and
+// products follow one another, with two wavefronts a SIMD and a barrier a tile; no
+// pipe is near full (matrix cores 34 %, vector work 40 %, LDS 24 % of the cycles).
 //
 // Work: the cached positions of all items, in units of one step of a workgroup,
 // are one line that is cut into (up to) SPLITS (as many workgroups as the chip
@@ -1253,7 +1259,12 @@ __global__ void __launch_bounds__(JOIN_THREADS) attn_join_kernel(AttnArgs a)
 // ---------------------------------------------------------------------------
 
 // How a call's items are run: rows of an item by the most rows that a request
-// has per key/value head.
+// has per key/value head.  Up to 16 rows by the rows kernel, as against the block
+// kernel with 64: one request at 4096 positions 13.6 and 15.6 us, 64 requests up to
+// 2047 with heads of 64 32.4 and 40.0; but with heads of 128 that fill the chip the
+// block kernel is a little better, 64 at 8192 345 to 358 and 340 (pages head by head
+// 334 and 352), 64 up to 2047 59.8 to 62 and 58.3, 512 up to 400 111 and 105.  The rule
+// goes by rows alone.
 enum Shape { ROWS16, ROWS64, ROWS128 };
 
 Shape shape_of(int max_new, int heads, int kv_heads)

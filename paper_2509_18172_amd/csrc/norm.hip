@@ -1,7 +1,7 @@
 // The norms around a block with its gate and residual scale: z = rms(y) * w,
 // x' = x + scale * gate * z, h = rms(x') * w', one pass over the rows.
 //
-// A row is held in registers by THREADS threads, CH pieces of eight elements
+// A row is held by THREADS threads, in registers, CH pieces of eight elements
 // each, so x, y and the gate are read once and x' and h written once; the two
 // means are sums in a fixed order.  Every load is sent off at the start, without
 // a branch, so that one latency covers them; the first reduction and the second
@@ -12,6 +12,12 @@
 // 67.5 us, 5.0 TB/s read and written, the rate of a large copy (4.94); 4096 rows of
 // 1024 10 us and 2048 14.4 us (4.7 TB/s); one row of 4096 3.9 us, of which an empty
 // launch is 2.1 and the rest two latencies and two reductions.
+//
+// Above 16384 elements a thread has four pieces, and some of the row does not fit
+// the 128 registers that 1024 threads leave each: 20 to 100 bytes a lane go to
+// scratch.  512 rows of 16384 24.5 us (4.1 TB/s), of 32768 60.1 us (3.4) with a binary32
+// stream and 34 us (3.9 to 4.0) with a 16-bit one.  Widths that are no multiple of 8
+// load and store at any address: 1000 rows of 5003 16.4 to 18.2 us, of 5000 14.6.
 //
 // Rows need no alignment beyond their elements'.  A piece that would pass the
 // row's end is moved back to end with it: of its elements the first ones belong

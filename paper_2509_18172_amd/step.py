@@ -11,6 +11,9 @@ products, and ``adjust_logits`` on the last product.  ``stream``: a
 torch.cuda.Stream of the tensors' device, by default its current one; the call
 is made with that device and stream as the current ones, so outputs and
 workspaces belong to the stream as they do under ``torch.cuda.stream(stream)``.
+
+Forward only: results carry no gradient, whatever the inputs say, and what is
+written in place (page_table, a cache, x_out, out) is not marked as changed.
 """
 from __future__ import annotations
 
