@@ -76,7 +76,9 @@ const char *sbvr_status_string(int status);
  * 1.06 sbvr_gemv_grouped and sbvr_gemv_grouped_a8, 1.07 sbvr_encode_cached,
  * 1.08 the operators between the products of a step: sbvr_batch_plan,
  * sbvr_cache_write, sbvr_tree_attention, sbvr_residual_norm,
- * sbvr_adjust_logits, 1.09 sbvr_tree_attention_whole. */
+ * sbvr_adjust_logits, 1.09 sbvr_tree_attention_whole, 1.10 sbvr_rotary,
+ * sbvr_rotary_write, sbvr_beam_select and the operators on pages
+ * (sbvr_page_usage, sbvr_page_fork, sbvr_page_compact, sbvr_page_copy). */
 int sbvr_version(void);
 
 /*
@@ -569,6 +571,191 @@ typedef struct sbvr_logits_args {
 } sbvr_logits_args;
 
 int sbvr_adjust_logits(const sbvr_logits_args *args, hipStream_t stream);
+
+#define SBVR_ROTARY_DIM_MAX 512
+
+/*
+ * Rotation of queries and keys by their positions, which may have several axes
+ * (an image's time, row and column).  A head's first 2 * pairs elements are
+ * pairs: element i with i + pairs, or, interleaved, 2 i with 2 i + 1.  Pair i of
+ * token t turns by
+ *     angle = positions[pair_axis[i]][t] * frequencies[i]
+ *     (a, b) -> (a cos(angle) - b sin(angle), b cos(angle) + a sin(angle))
+ * or, inverse, by the negative angle, which is also the gradient's rotation.  The
+ * elements behind the pairs are copied.  Angles are binary64 up to the turn that
+ * they leave, sines, cosines and sums binary32; each output is rounded once.
+ *   T         >= 0 tokens.
+ *   heads, kv_heads   of q and k, 0 .. 4096, not both 0 (0: that tensor is not read).
+ *   head_dim  a multiple of 8, 8 .. SBVR_ROTARY_DIM_MAX (larger: SBVR_E_UNSUPPORTED).
+ *   pairs     1 .. head_dim / 2.
+ *   dtype     SBVR_F16, SBVR_BF16 or SBVR_F32, of q, k and the outputs.
+ *   q, k, q_out, k_out   [T][heads][head_dim] with the given token and head strides
+ *             (elements, multiples of 8, not negative), 16-byte aligned.  Rows of an
+ *             output must not overlap.  q_out may be q itself, k_out k, with the
+ *             same strides; apart from that inputs and outputs must not overlap.
+ *   positions int32 [axes][T], row stride position_stride; any value.
+ *   pair_axis int32 [pairs], or NULL: axis 0 for all.  A pair whose axis is outside
+ *             0 .. axes - 1 is not turned.
+ *   frequencies  binary32 [pairs].
+ * The struct is read during the call.
+ */
+typedef struct sbvr_rotary_args {
+    int32_t T, heads, kv_heads, head_dim, dtype, pairs, axes, interleaved, inverse;
+    const void *q;
+    int64_t q_token_stride, q_head_stride;
+    const void *k;
+    int64_t k_token_stride, k_head_stride;
+    void *q_out;
+    int64_t q_out_token_stride, q_out_head_stride;
+    void *k_out;
+    int64_t k_out_token_stride, k_out_head_stride;
+    const int32_t *positions;
+    int64_t position_stride;
+    const int32_t *pair_axis;
+    const float *frequencies;
+} sbvr_rotary_args;
+
+int sbvr_rotary(const sbvr_rotary_args *args, hipStream_t stream);
+
+/*
+ * The same, with the keys turned on their way into the cache, and the values
+ * written beside them: sbvr_rotary and sbvr_cache_write in one pass.  kv_heads,
+ * head_dim and dtype of args are the cache's (SBVR_F16 or SBVR_BF16, head_dim at
+ * most 128), k must be given and k_out NULL.  heads may be 0.
+ *   v      [T][kv_heads][head_dim] with the given strides, as k.
+ *   slots  int64 [T]; a token whose slot is negative or past the cache is not
+ *          written (its query is turned all the same).  Two tokens must not share
+ *          a slot.
+ */
+int sbvr_rotary_write(const sbvr_rotary_args *args, const sbvr_kv_cache *cache, const void *v, int64_t v_token_stride,
+                      int64_t v_head_stride, const int64_t *slots, hipStream_t stream);
+
+#define SBVR_BEAMS_MAX 32
+#define SBVR_BEAM_KEEP_MAX 64
+
+/*
+ * The selection of a beam search.  Request r has B beams; logits row r * B + b is
+ * beam b's next token and scores[r][b] the logarithm of its probability so far.
+ * A continuation (b, v) has the score
+ *     s(b, v) = scores[r][b] + logits[v] - log(sum_u exp(logits[u]))      (row r * B + b)
+ * and one is better than another if its score is higher or, of equal ones, its beam
+ * is lower, or its token in the same beam.
+ *     tokens, parents, scores_out [R][n]: the n best continuations whose token is
+ *         no end token, best first: token, beam and score; -1, -1 and -infinity
+ *         past the last one there is.
+ *     ended, ended_tokens [R][B]: beam b's best continuation with an end token
+ *         where it is among the n best of all the request's: its score and token;
+ *         else -infinity and -1.
+ * Beams whose score is -infinity (or no finite number) have no continuations, and
+ * their logits are not read; nor has a token whose logit is -infinity or NaN, which
+ * adds nothing to the sum.  A logit of +infinity counts as the largest binary32 number.
+ * Exponentials are summed in binary32 within a lane and in binary64 from there on,
+ * scores are binary64 and rounded to binary32 at the end; the continuations of one
+ * beam are ordered by their logits.
+ *   R, B, V  R >= 0 requests of 1 <= B <= SBVR_BEAMS_MAX beams, V tokens (at most
+ *            2^30; R * B at most 65535), else SBVR_E_UNSUPPORTED.
+ *   n        >= 1, n + n_end at most SBVR_BEAM_KEEP_MAX (else SBVR_E_UNSUPPORTED).
+ *   logits   [R * B][V] of dtype (any sbvr_dtype), row stride logits_stride.
+ *   scores   binary32 [R][B].
+ *   end_tokens  int32 [n_end], n_end >= 0 (0: none, and not read).
+ *   workspace   sbvr_beam_select_workspace_bytes, 16-byte aligned; its content
+ *            needs no preparation and is not kept.
+ * Inputs and outputs must not overlap.  The struct is read during the call.
+ */
+typedef struct sbvr_beam_args {
+    int32_t R, B, V, n, n_end, dtype;
+    const void *logits;
+    int64_t logits_stride;
+    const float *scores;
+    const int32_t *end_tokens;
+    int32_t *tokens, *parents;
+    float *scores_out, *ended;
+    int32_t *ended_tokens;
+} sbvr_beam_args;
+
+size_t sbvr_beam_select_workspace_bytes(int R, int B, int V, int n, int n_end);
+int sbvr_beam_select(const sbvr_beam_args *args, void *workspace, size_t ws_bytes, hipStream_t stream);
+
+/*
+ * PAGES THAT SEQUENCES SHARE.  The rows of a page table (requests, or the beams of
+ * requests) may name the same page, as long as it is full: only its last, partly
+ * filled page must be a row's own.  Row r uses the first ceil(context_lens[r] /
+ * page_size) entries of its row of the table, at most max_pages; a negative length
+ * counts as 0.  Entries outside 0 .. n_pages - 1 name no page.  These tables and
+ * lists are int32; rows R are 0 .. SBVR_REQUESTS_MAX, pages of a cache 1 ..
+ * SBVR_POOL_MAX (more: SBVR_E_UNSUPPORTED).
+ */
+#define SBVR_POOL_MAX (1 << 22)
+
+/*
+ * Which pages are used, and which are free: a page is given back by leaving it
+ * out of every row.
+ *   refs        [n_pages] (output): how many entries in use name the page.
+ *   free_pages  [n_pages] (output): the pages that none names, ascending, then -1:
+ *               what sbvr_batch_plan and sbvr_page_fork take pages from.
+ *   counts      [2] (output): free pages, used pages.
+ *   workspace   sbvr_page_usage_workspace_bytes, 16-byte aligned; its content
+ *               needs no preparation and is not kept.
+ */
+size_t sbvr_page_usage_workspace_bytes(int R, int max_pages, int n_pages);
+int sbvr_page_usage(int R, int page_size, int n_pages, const int32_t *context_lens, const int32_t *page_table,
+                    int max_pages, int64_t table_stride, int32_t *refs, int32_t *free_pages, int32_t *counts,
+                    void *workspace, size_t ws_bytes, hipStream_t stream);
+
+/*
+ * New rows from old ones, as a beam search continues its beams: rows_out rows in
+ * `groups` equal groups, as the rows_in old ones; row i of group g continues the old
+ * row parents[i] of the same group (numbered from 0 within it; any other number: the
+ * row is empty).  A row has its parent's length and shares its full pages.  The
+ * partly filled one goes to the first row that continues the parent; each further row
+ * takes the next free page, into which its content has to be copied (sbvr_page_copy
+ * with the lists given here, before the next tokens are written).
+ *   groups      >= 1, a divisor of rows_in and of rows_out.
+ *   free_pages  [n_free]: unused pages, taken in order from number *taken on
+ *               (int32 on the device, such as the first of sbvr_batch_plan's used; NULL:
+ *               0); -1 in the list, or its end: there is none.
+ *   out_table   [rows_out][out_stride] (output): max_pages entries of every row are
+ *               written, -1 behind those in use and where there was no free page.
+ *   out_lens    [rows_out] (output).
+ *   src, dst, tokens  [rows_out] (output): the copies: page, page, and the number
+ *               of tokens; -1, -1 and 0 for a row that needs none or found no page.
+ *   used        [1] (output): pages that were needed.
+ * Inputs and outputs must not overlap.
+ */
+int sbvr_page_fork(int groups, int rows_in, int rows_out, int page_size, const int32_t *context_lens,
+                   const int32_t *page_table, int max_pages, int64_t table_stride, const int32_t *parents,
+                   const int32_t *free_pages, int n_free, const int32_t *taken, int32_t *out_table,
+                   int64_t out_stride, int32_t *out_lens, int32_t *src, int32_t *dst, int32_t *tokens, int32_t *used,
+                   hipStream_t stream);
+
+/*
+ * Pages moved together: with U pages in use, the k-th (from the lowest) of those
+ * numbered U or higher moves to the k-th free page below U, so that the pages in use
+ * are 0 .. U - 1.  The content is moved by sbvr_page_copy with the lists given here.
+ *   out_table   [R][out_stride] (output): max_pages entries of every row are written,
+ *               -1 behind those in use and where an entry names no page.  May be
+ *               page_table itself (same stride).
+ *   src, dst    [n_pages / 2] (output): the moves in ascending order, then -1.
+ *   counts      [2] (output): pages in use, pages moved.
+ *   workspace   sbvr_page_compact_workspace_bytes, as for sbvr_page_usage.
+ * Apart from out_table = page_table, inputs and outputs must not overlap.
+ */
+size_t sbvr_page_compact_workspace_bytes(int R, int max_pages, int n_pages);
+int sbvr_page_compact(int R, int page_size, int n_pages, const int32_t *context_lens, const int32_t *page_table,
+                      int max_pages, int64_t table_stride, int32_t *out_table, int64_t out_stride, int32_t *src,
+                      int32_t *dst, int32_t *counts, void *workspace, size_t ws_bytes, hipStream_t stream);
+
+/*
+ * Copies within caches: for each i < n the first tokens[i] tokens (NULL: all; never
+ * more than a page) of page src[i] to page dst[i], keys and values, in every one of
+ * the n_caches caches (a model's layers), which must be alike but for their
+ * addresses.  A copy whose src or dst is outside 0 .. n_pages - 1 is skipped.  No dst
+ * may be another copy's src or dst.
+ *   caches  a host array, read during the call.
+ *   src, dst, tokens  int32 [n], n >= 0.
+ */
+int sbvr_page_copy(const sbvr_kv_cache *caches, int n_caches, int n, const int32_t *src, const int32_t *dst,
+                   const int32_t *tokens, hipStream_t stream);
 
 #ifdef __cplusplus
 }

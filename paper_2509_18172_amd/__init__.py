@@ -34,6 +34,9 @@ EXPORTED = (
     "sbvr_decompress_indexed", "sbvr_gemm_prefill", "sbvr_gemv_grouped", "sbvr_gemv_grouped_a8",
     "sbvr_encode_cached", "sbvr_batch_plan", "sbvr_cache_write", "sbvr_tree_attention_workspace_bytes",
     "sbvr_tree_attention", "sbvr_tree_attention_whole", "sbvr_residual_norm", "sbvr_adjust_logits",
+    "sbvr_rotary", "sbvr_rotary_write", "sbvr_beam_select_workspace_bytes", "sbvr_beam_select",
+    "sbvr_page_usage_workspace_bytes", "sbvr_page_usage", "sbvr_page_fork", "sbvr_page_compact_workspace_bytes",
+    "sbvr_page_compact", "sbvr_page_copy",
 )
 
 # enum sbvr_dtype and the limits of the operators between the products
@@ -42,6 +45,10 @@ REQUESTS_MAX = 4096
 TREE_MAX = 64
 PAGE_MAX = 4096
 NORM_MAX_WIDTH = 32768
+ROTARY_DIM_MAX = 512
+BEAMS_MAX = 32
+BEAM_KEEP_MAX = 64
+POOL_MAX = 1 << 22
 
 
 class CacheStruct(C.Structure):
@@ -62,6 +69,24 @@ class LogitsStruct(C.Structure):
                                              "bias_values", "grammar")]
                 + [("grammar_stride", C.c_int64), ("grammar_rows", C.c_void_p), ("grammar_count", C.c_int32)]
                 + [(n, C.c_void_p) for n in ("draft_tokens", "query_start", "tree_mask")])
+
+
+class RotaryStruct(C.Structure):
+    """sbvr_rotary_args"""
+    _fields_ = ([(n, C.c_int32) for n in ("T", "heads", "kv_heads", "head_dim", "dtype", "pairs", "axes", "interleaved",
+                                          "inverse")]
+                + [f for n in ("q", "k", "q_out", "k_out")
+                   for f in ((n, C.c_void_p), (n + "_token_stride", C.c_int64), (n + "_head_stride", C.c_int64))]
+                + [("positions", C.c_void_p), ("position_stride", C.c_int64), ("pair_axis", C.c_void_p),
+                   ("frequencies", C.c_void_p)])
+
+
+class BeamStruct(C.Structure):
+    """sbvr_beam_args"""
+    _fields_ = ([(n, C.c_int32) for n in ("R", "B", "V", "n", "n_end", "dtype")]
+                + [("logits", C.c_void_p), ("logits_stride", C.c_int64)]
+                + [(n, C.c_void_p) for n in ("scores", "end_tokens", "tokens", "parents", "scores_out", "ended",
+                                             "ended_tokens")])
 
 
 class SBVRError(RuntimeError):
@@ -119,6 +144,16 @@ def _load():
         "sbvr_residual_norm": (i32, [i32, i32, i32, i32, vp, i64, vp, i64, vp, vp, i64, f32, vp, f32, vp, i64, vp, i64,
                                      vp]),
         "sbvr_adjust_logits": (i32, [vp, vp]),
+        "sbvr_rotary": (i32, [vp, vp]),
+        "sbvr_rotary_write": (i32, [vp, vp, vp, i64, i64, vp, vp]),
+        "sbvr_beam_select_workspace_bytes": (sz, [i32, i32, i32, i32, i32]),
+        "sbvr_beam_select": (i32, [vp, vp, sz, vp]),
+        "sbvr_page_usage_workspace_bytes": (sz, [i32, i32, i32]),
+        "sbvr_page_usage": (i32, [i32, i32, i32, vp, vp, i32, i64, vp, vp, vp, vp, sz, vp]),
+        "sbvr_page_fork": (i32, [i32, i32, i32, i32, vp, vp, i32, i64, vp, vp, i32, vp, vp, i64, vp, vp, vp, vp, vp, vp]),
+        "sbvr_page_compact_workspace_bytes": (sz, [i32, i32, i32]),
+        "sbvr_page_compact": (i32, [i32, i32, i32, vp, vp, i32, i64, vp, i64, vp, vp, vp, vp, sz, vp]),
+        "sbvr_page_copy": (i32, [vp, i32, i32, vp, vp, vp, vp]),
     }
     for name, (res, args) in sig.items():
         f = getattr(lib, name)
@@ -303,6 +338,59 @@ def sbvr_residual_norm(T, H, dtype, x_dtype, x, x_stride, y, y_stride, post_weig
 def sbvr_adjust_logits(args, stream=0) -> int:
     """args: a LogitsStruct (or None)."""
     return _lib.sbvr_adjust_logits(None if args is None else C.addressof(args), stream)
+
+
+def sbvr_rotary(args, stream=0) -> int:
+    """args: a RotaryStruct (or None)."""
+    return _lib.sbvr_rotary(None if args is None else C.addressof(args), stream)
+
+
+def sbvr_rotary_write(args, cache, v, v_token_stride, v_head_stride, slots, stream=0) -> int:
+    """args: a RotaryStruct, cache: a CacheStruct (or None)."""
+    return _lib.sbvr_rotary_write(None if args is None else C.addressof(args), None if cache is None else C.addressof(cache),
+                                  v, v_token_stride, v_head_stride, slots, stream)
+
+
+def sbvr_beam_select_workspace_bytes(R, B, V, n, n_end=0) -> int:
+    return _lib.sbvr_beam_select_workspace_bytes(R, B, V, n, n_end)
+
+
+def sbvr_beam_select(args, workspace, ws_bytes, stream=0) -> int:
+    """args: a BeamStruct (or None)."""
+    return _lib.sbvr_beam_select(None if args is None else C.addressof(args), workspace, ws_bytes, stream)
+
+
+def sbvr_page_usage_workspace_bytes(R, max_pages, n_pages) -> int:
+    return _lib.sbvr_page_usage_workspace_bytes(R, max_pages, n_pages)
+
+
+def sbvr_page_usage(R, page_size, n_pages, context_lens, page_table, max_pages, table_stride, refs, free_pages, counts,
+                    workspace, ws_bytes, stream=0) -> int:
+    return _lib.sbvr_page_usage(R, page_size, n_pages, context_lens, page_table, max_pages, table_stride, refs, free_pages,
+                                counts, workspace, ws_bytes, stream)
+
+
+def sbvr_page_fork(groups, rows_in, rows_out, page_size, context_lens, page_table, max_pages, table_stride, parents,
+                   free_pages, n_free, taken, out_table, out_stride, out_lens, src, dst, tokens, used, stream=0) -> int:
+    return _lib.sbvr_page_fork(groups, rows_in, rows_out, page_size, context_lens, page_table, max_pages, table_stride,
+                               parents, free_pages, n_free, taken, out_table, out_stride, out_lens, src, dst, tokens, used,
+                               stream)
+
+
+def sbvr_page_compact_workspace_bytes(R, max_pages, n_pages) -> int:
+    return _lib.sbvr_page_compact_workspace_bytes(R, max_pages, n_pages)
+
+
+def sbvr_page_compact(R, page_size, n_pages, context_lens, page_table, max_pages, table_stride, out_table, out_stride, src,
+                      dst, counts, workspace, ws_bytes, stream=0) -> int:
+    return _lib.sbvr_page_compact(R, page_size, n_pages, context_lens, page_table, max_pages, table_stride, out_table,
+                                  out_stride, src, dst, counts, workspace, ws_bytes, stream)
+
+
+def sbvr_page_copy(caches, n, src, dst, tokens=None, stream=0) -> int:
+    """caches: a sequence of CacheStructs (or None)."""
+    array = (CacheStruct * max(len(caches), 1))(*caches) if caches is not None else None
+    return _lib.sbvr_page_copy(array, len(caches) if caches is not None else 0, n, src, dst, tokens, stream)
 
 
 # --------------------------------------------------------------------------
@@ -593,7 +681,9 @@ def algorithmic_bytes(O: int, I: int, k: int, B: int = 1) -> int:
 
 # The operators between the products of a step (step.py), loaded with their
 # native binding at first use: the functions above need neither it nor torch.
-_STEP = ("BatchPlan", "KVCache", "adjust_logits", "batch_plan", "cache_write", "residual_norm", "tree_attention")
+_STEP = ("BatchPlan", "BeamChoice", "KVCache", "PageCompaction", "PageFork", "PageUsage", "adjust_logits", "batch_plan",
+         "beam_select", "cache_write", "page_compact", "page_copy", "page_fork", "page_usage", "residual_norm", "rotary",
+         "rotary_write", "tree_attention")
 
 
 def __getattr__(name: str):

@@ -11,7 +11,7 @@ ROOT = os.path.dirname(HERE)
 SOURCES = [os.path.join(HERE, "csrc", f) for f in ("api.hip", "pack.hip", "gemv_b1.hip", "gemv_b1s.hip", "gemm_sbs.hip",
                                                   "decompress.hip", "encode.hip", "prefill.hip", "api_step.hip",
                                                   "plan.hip", "cache_write.hip", "attention.hip", "norm.hip",
-                                                  "logits.hip")]
+                                                  "logits.hip", "rotary.hip", "beam.hip", "pages.hip")]
 # The encoder's binary64 arithmetic is its definition: no fused multiply-add.
 SOURCE_FLAGS = {
     "encode.hip": ["-ffp-contract=off"],

@@ -136,7 +136,7 @@ const char *sbvr_status_string(int status)
     }
 }
 
-int sbvr_version(void) { return 109; }
+int sbvr_version(void) { return 110; }
 
 size_t sbvr_packed_plane_bytes(int O, int I, int k)
 {

@@ -86,6 +86,93 @@ int tree_attention(bool whole, const sbvr_kv_cache *cache, int R, int T, int hea
     return launch_attn(a, stream);
 }
 
+// A [T][heads][head_dim] tensor that is read.
+int check_heads(const void *p, int64_t token_stride, int64_t head_stride)
+{
+    if (!piece_stride_ok(token_stride) || !piece_stride_ok(head_stride))
+        return SBVR_E_INVALID_ARG;
+    return !p ? SBVR_E_INVALID_ARG : !aligned(p, 16) ? SBVR_E_ALIGNMENT : SBVR_OK;
+}
+
+// One that is written, in place where it is `in`: its rows must not overlap.
+int check_heads_out(const void *p, int64_t token_stride, int64_t head_stride, int T, int heads, int head_dim,
+                    const void *in, int64_t in_token_stride, int64_t in_head_stride)
+{
+    const int st = check_heads(p, token_stride, head_stride);
+    if (st != SBVR_OK)
+        return st;
+    const int64_t token = T > 1 ? token_stride : head_dim, head = heads > 1 ? head_stride : head_dim;
+    const __int128 row = (__int128)(heads - 1) * head + head_dim, column = (__int128)(T - 1) * token + head_dim;
+    if (token < head_dim || head < head_dim || (T > 1 && heads > 1 && token < row && head < column))
+        return SBVR_E_INVALID_ARG;
+    if (p == in && ((T > 1 && token_stride != in_token_stride) || (heads > 1 && head_stride != in_head_stride)))
+        return SBVR_E_INVALID_ARG;
+    return SBVR_OK;
+}
+
+// cache: what the keys are written to, or NULL
+int check_rotary(const sbvr_rotary_args *a, const sbvr_kv_cache *cache)
+{
+    if (!a || a->T < 0 || a->heads < 0 || a->kv_heads < 0 || a->heads + (int64_t)a->kv_heads < 1 || a->head_dim < 8 ||
+        a->head_dim % 8 != 0 || a->pairs < 1 || a->pairs > a->head_dim / 2 || a->axes < 1 || a->dtype < SBVR_F16 ||
+        a->dtype > SBVR_F32 || (a->interleaved & ~1) || (a->inverse & ~1) || !stride_ok(a->position_stride) ||
+        (a->axes > 1 && a->position_stride < a->T))
+        return SBVR_E_INVALID_ARG;
+    if (cache && (a->kv_heads != cache->kv_heads || a->head_dim != cache->head_dim || a->dtype != cache->dtype || a->k_out))
+        return SBVR_E_INVALID_ARG;
+    if (a->heads > 4096 || a->kv_heads > 4096 || a->head_dim > SBVR_ROTARY_DIM_MAX)
+        return SBVR_E_UNSUPPORTED;
+    if (a->T == 0)
+        return SBVR_OK;
+    if (!a->positions || !a->frequencies)
+        return SBVR_E_INVALID_ARG;
+    int st = SBVR_OK;
+    if (a->heads && (st = check_heads(a->q, a->q_token_stride, a->q_head_stride)) != SBVR_OK)
+        return st;
+    if (a->heads && (st = check_heads_out(a->q_out, a->q_out_token_stride, a->q_out_head_stride, a->T, a->heads,
+                                          a->head_dim, a->q, a->q_token_stride, a->q_head_stride)) != SBVR_OK)
+        return st;
+    if (a->kv_heads && (st = check_heads(a->k, a->k_token_stride, a->k_head_stride)) != SBVR_OK)
+        return st;
+    if (a->kv_heads && !cache &&
+        (st = check_heads_out(a->k_out, a->k_out_token_stride, a->k_out_head_stride, a->T, a->kv_heads, a->head_dim, a->k,
+                              a->k_token_stride, a->k_head_stride)) != SBVR_OK)
+        return st;
+    if (!aligned(a->positions, 4) || !aligned(a->frequencies, 4) || !aligned(a->pair_axis, 4))
+        return SBVR_E_ALIGNMENT;
+    return SBVR_OK;
+}
+
+int check_beam_shape(int R, int B, int V, int n, int n_end)
+{
+    if (R < 0 || B < 1 || V < 1 || n < 1 || n_end < 0)
+        return SBVR_E_INVALID_ARG;
+    if (B > SBVR_BEAMS_MAX || V > (1 << 30) || (int64_t)n + n_end > SBVR_BEAM_KEEP_MAX || (int64_t)R * B > (1 << 16) - 1)
+        return SBVR_E_UNSUPPORTED;
+    return SBVR_OK;
+}
+
+int check_table_shape(int R, int max_pages, int64_t table_stride, int page_size)
+{
+    if (R < 0 || max_pages < 1 || table_stride < max_pages || !stride_ok(table_stride) ||
+        check_page_size(page_size) != SBVR_OK)
+        return SBVR_E_INVALID_ARG;
+    return R > SBVR_REQUESTS_MAX || max_pages > SBVR_POOL_MAX ? SBVR_E_UNSUPPORTED : SBVR_OK;
+}
+
+int check_pool(int n_pages)
+{
+    return n_pages < 1 ? SBVR_E_INVALID_ARG : n_pages > SBVR_POOL_MAX ? SBVR_E_UNSUPPORTED : SBVR_OK;
+}
+
+bool alike(const sbvr_kv_cache &a, const sbvr_kv_cache &b)
+{
+    return a.k_page_stride == b.k_page_stride && a.k_token_stride == b.k_token_stride &&
+           a.k_head_stride == b.k_head_stride && a.v_page_stride == b.v_page_stride &&
+           a.v_token_stride == b.v_token_stride && a.v_head_stride == b.v_head_stride && a.n_pages == b.n_pages &&
+           a.page_size == b.page_size && a.kv_heads == b.kv_heads && a.head_dim == b.head_dim && a.dtype == b.dtype;
+}
+
 }  // namespace
 
 extern "C" {
@@ -228,6 +315,163 @@ int sbvr_adjust_logits(const sbvr_logits_args *a, hipStream_t stream)
     if (a->out == a->logits && (a->out_dtype != a->dtype || (a->T > 1 && a->out_stride != a->logits_stride)))
         return SBVR_E_INVALID_ARG;
     return launch_logits(*a, stream);
+}
+
+int sbvr_rotary(const sbvr_rotary_args *a, hipStream_t stream)
+{
+    const int st = check_rotary(a, nullptr);
+    if (st != SBVR_OK || a->T == 0)
+        return st;
+    RotaryArgs args = {};
+    args.r = *a;
+    return launch_rotary(args, stream);
+}
+
+int sbvr_rotary_write(const sbvr_rotary_args *a, const sbvr_kv_cache *cache, const void *v, int64_t v_token_stride,
+                      int64_t v_head_stride, const int64_t *slots, hipStream_t stream)
+{
+    int st = check_cache(cache);
+    if (st != SBVR_OK || (st = check_rotary(a, cache)) != SBVR_OK)
+        return st;
+    if (a->T == 0)
+        return SBVR_OK;
+    if ((st = check_heads(v, v_token_stride, v_head_stride)) != SBVR_OK)
+        return st;
+    if (!slots)
+        return SBVR_E_INVALID_ARG;
+    if (!aligned(slots, 8))
+        return SBVR_E_ALIGNMENT;
+    return launch_rotary(RotaryArgs{*a, *cache, v, v_token_stride, v_head_stride, slots}, stream);
+}
+
+size_t sbvr_beam_select_workspace_bytes(int R, int B, int V, int n, int n_end)
+{
+    return check_beam_shape(R, B, V, n, n_end) == SBVR_OK ? beam_workspace_bytes(R, B, V, n, n_end) : 0;
+}
+
+int sbvr_beam_select(const sbvr_beam_args *a, void *workspace, size_t ws_bytes, hipStream_t stream)
+{
+    if (!a || a->dtype < SBVR_F16 || a->dtype > SBVR_F32 || !stride_ok(a->logits_stride))
+        return SBVR_E_INVALID_ARG;
+    const int st = check_beam_shape(a->R, a->B, a->V, a->n, a->n_end);
+    if (st != SBVR_OK || a->R == 0)
+        return st;
+    if (!a->logits || !a->scores || !a->tokens || !a->parents || !a->scores_out || !a->ended || !a->ended_tokens ||
+        (a->n_end && !a->end_tokens))
+        return SBVR_E_INVALID_ARG;
+    if (ws_bytes < beam_workspace_bytes(a->R, a->B, a->V, a->n, a->n_end) || !workspace)
+        return SBVR_E_WORKSPACE;
+    const void *words[] = {a->scores, a->end_tokens, a->tokens, a->parents, a->scores_out, a->ended, a->ended_tokens};
+    for (const void *p : words)
+        if (!aligned(p, 4))
+            return SBVR_E_ALIGNMENT;
+    if (!aligned(a->logits, a->dtype == SBVR_F32 ? 4 : 2) || !aligned(workspace, 16))
+        return SBVR_E_ALIGNMENT;
+    return launch_beam(*a, workspace, stream);
+}
+
+size_t sbvr_page_usage_workspace_bytes(int R, int max_pages, int n_pages)
+{
+    return check_table_shape(R, max_pages, max_pages, 16) == SBVR_OK && check_pool(n_pages) == SBVR_OK
+               ? usage_workspace_bytes(n_pages)
+               : 0;
+}
+
+int sbvr_page_usage(int R, int page_size, int n_pages, const int32_t *context_lens, const int32_t *page_table,
+                    int max_pages, int64_t table_stride, int32_t *refs, int32_t *free_pages, int32_t *counts,
+                    void *workspace, size_t ws_bytes, hipStream_t stream)
+{
+    int st = check_table_shape(R, max_pages, table_stride, page_size);
+    if (st != SBVR_OK || (st = check_pool(n_pages)) != SBVR_OK)
+        return st;
+    if ((R && (!context_lens || !page_table)) || !refs || !free_pages || !counts)
+        return SBVR_E_INVALID_ARG;
+    if (ws_bytes < usage_workspace_bytes(n_pages) || !workspace)
+        return SBVR_E_WORKSPACE;
+    if (!aligned(context_lens, 4) || !aligned(page_table, 4) || !aligned(refs, 4) || !aligned(free_pages, 4) ||
+        !aligned(counts, 4) || !aligned(workspace, 16))
+        return SBVR_E_ALIGNMENT;
+    const PageTable t{R, __builtin_ctz(page_size), max_pages, context_lens, page_table, table_stride};
+    return launch_usage(UsageArgs{t, n_pages, refs, free_pages, counts, (uint32_t *)workspace}, stream);
+}
+
+int sbvr_page_fork(int groups, int rows_in, int rows_out, int page_size, const int32_t *context_lens,
+                   const int32_t *page_table, int max_pages, int64_t table_stride, const int32_t *parents,
+                   const int32_t *free_pages, int n_free, const int32_t *taken, int32_t *out_table,
+                   int64_t out_stride, int32_t *out_lens, int32_t *src, int32_t *dst, int32_t *tokens, int32_t *used,
+                   hipStream_t stream)
+{
+    if (groups < 1 || rows_in < 0 || rows_out < 0 || rows_in % groups || rows_out % groups || n_free < 0)
+        return SBVR_E_INVALID_ARG;
+    int st = check_table_shape(rows_in, max_pages, table_stride, page_size);
+    if (st != SBVR_OK || (st = check_table_shape(rows_out, max_pages, out_stride, page_size)) != SBVR_OK)
+        return st;
+    if ((rows_in && (!context_lens || !page_table)) || (n_free && !free_pages) || !used ||
+        (rows_out && (!parents || !out_table || !out_lens || !src || !dst || !tokens)) ||
+        (rows_out && out_table == page_table))
+        return SBVR_E_INVALID_ARG;
+    const void *words[] = {context_lens, page_table, parents, free_pages, taken, out_table, out_lens, src, dst, tokens,
+                           used};
+    for (const void *p : words)
+        if (!aligned(p, 4))
+            return SBVR_E_ALIGNMENT;
+    const PageTable t{rows_in, __builtin_ctz(page_size), max_pages, context_lens, page_table, table_stride};
+    const ForkArgs a{t, rows_out, rows_in / groups, rows_out / groups > 0 ? rows_out / groups : 1, n_free, parents,
+                     free_pages, taken, out_table, out_stride, out_lens, src, dst, tokens, used};
+    return launch_fork(a, stream);
+}
+
+size_t sbvr_page_compact_workspace_bytes(int R, int max_pages, int n_pages)
+{
+    return check_table_shape(R, max_pages, max_pages, 16) == SBVR_OK && check_pool(n_pages) == SBVR_OK
+               ? compact_workspace_bytes(n_pages)
+               : 0;
+}
+
+int sbvr_page_compact(int R, int page_size, int n_pages, const int32_t *context_lens, const int32_t *page_table,
+                      int max_pages, int64_t table_stride, int32_t *out_table, int64_t out_stride, int32_t *src,
+                      int32_t *dst, int32_t *counts, void *workspace, size_t ws_bytes, hipStream_t stream)
+{
+    int st = check_table_shape(R, max_pages, table_stride, page_size);
+    if (st != SBVR_OK || (st = check_table_shape(R, max_pages, out_stride, page_size)) != SBVR_OK ||
+        (st = check_pool(n_pages)) != SBVR_OK)
+        return st;
+    if ((R && (!context_lens || !page_table || !out_table)) || (n_pages > 1 && (!src || !dst)) || !counts ||
+        (R > 1 && out_table == page_table && out_stride != table_stride))
+        return SBVR_E_INVALID_ARG;
+    if (ws_bytes < compact_workspace_bytes(n_pages) || !workspace)
+        return SBVR_E_WORKSPACE;
+    const void *words[] = {context_lens, page_table, out_table, src, dst, counts};
+    for (const void *p : words)
+        if (!aligned(p, 4))
+            return SBVR_E_ALIGNMENT;
+    if (!aligned(workspace, 16))
+        return SBVR_E_ALIGNMENT;
+    const PageTable t{R, __builtin_ctz(page_size), max_pages, context_lens, page_table, table_stride};
+    const CompactArgs a{t, n_pages, out_table, out_stride, src, dst, counts, (uint32_t *)workspace,
+                        (int32_t *)((char *)workspace + usage_workspace_bytes(n_pages))};
+    return launch_compact(a, stream);
+}
+
+int sbvr_page_copy(const sbvr_kv_cache *caches, int n_caches, int n, const int32_t *src, const int32_t *dst,
+                   const int32_t *tokens, hipStream_t stream)
+{
+    if (!caches || n_caches < 1 || n < 0)
+        return SBVR_E_INVALID_ARG;
+    for (int i = 0; i < n_caches; ++i) {
+        const int st = check_cache(&caches[i]);
+        if (st != SBVR_OK)
+            return st;
+        if (!alike(caches[0], caches[i]))
+            return SBVR_E_INVALID_ARG;
+    }
+    if (n == 0)
+        return SBVR_OK;
+    if (!src || !dst)
+        return SBVR_E_INVALID_ARG;
+    if (!aligned(src, 4) || !aligned(dst, 4) || !aligned(tokens, 4))
+        return SBVR_E_ALIGNMENT;
+    return launch_page_copy(caches, n_caches, n, src, dst, tokens, stream);
 }
 
 }  // extern "C"

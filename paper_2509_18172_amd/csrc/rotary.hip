@@ -1,0 +1,180 @@
+// Rotation of queries and keys by their positions, and the same with the cache
+// write: (a, b) -> (a cos - b sin, b cos + a sin) for the pairs of every head.
+//
+// Memory-bound for many tokens, a latency for few.  A workgroup takes the work of
+// some tokens, or a part of one's: pieces of eight pairs of a head (two loads and
+// two stores of 16 bytes), and pieces of eight elements that are only copied (what
+// lies behind the pairs, and the values).  The sine and cosine of a pair are the
+// same in all heads, so they are computed once a workgroup, into LDS.  The angle's
+// turn is taken in binary64: a binary32 product of position 100000 and a frequency
+// is off by 4e-3, and one in 64 bits costs a few instructions a pair.
+//
+// A piece that the pairs do not fill is moved by elements.  No piece is loaded by
+// a lane that another lane stores, so the outputs may be the inputs.
+#include "step.h"
+
+namespace sbvr {
+
+constexpr int ROTARY_THREADS = 256;
+
+struct RotaryShape {
+    int turned, copied, valued;  // pieces of a head that are turned, only copied, and of its values
+    int units;                   // pieces of a token
+    int split, tokens;           // pieces and tokens of a workgroup (split < units: one token)
+    int width;                   // pairs rounded up to pieces
+};
+
+// i / d for 0 <= i < 2^24
+__device__ __forceinline__ int small_div(int i, int d, float inverse)
+{
+    int q = (int)((float)i * inverse);
+    q -= q * d > i;
+    q += (q + 1) * d <= i;
+    return q;
+}
+
+// T: element type; EVEN: every piece is whole (pairs a multiple of 8); WRITE: keys
+// and values go into the cache.
+template <typename T, bool EVEN, bool WRITE>
+__global__ void __launch_bounds__(ROTARY_THREADS) rotary_kernel(RotaryArgs args, RotaryShape s, int page_shift)
+{
+    extern __shared__ __attribute__((aligned(16))) float turn[];  // cosines, then sines, of [tokens][width]
+    const sbvr_rotary_args &a = args.r;
+    const int n = a.pairs, heads = a.heads + a.kv_heads;
+    float *cosine = turn, *sine = turn + s.tokens * s.width;
+    for (long long t0 = (long long)blockIdx.x * s.tokens; t0 < a.T; t0 += (long long)gridDim.x * s.tokens) {
+        const int tokens = (int)min((long long)s.tokens, a.T - t0);
+        __syncthreads();
+        for (int i = threadIdx.x; i < tokens * s.width; i += ROTARY_THREADS) {
+            const int t = small_div(i, s.width, 1.f / (float)s.width), p = min(i - t * s.width, n - 1);
+            const int axis = a.pair_axis ? a.pair_axis[p] : 0;
+            const bool turns = axis >= 0 && axis < a.axes;
+            const int position = a.positions[(turns ? axis : 0) * a.position_stride + t0 + t];
+            double angle = (double)position * (double)a.frequencies[p] * 0.15915494309189535;  // in turns
+            angle -= rint(angle);
+            float c = 1.f, sn = 0.f;
+            if (turns)
+                sincospif(2.f * (float)angle, &sn, &c);
+            cosine[i] = c;
+            sine[i] = a.inverse ? -sn : sn;
+        }
+        __syncthreads();
+
+        const int first = blockIdx.y * s.split, last = min(first + s.split, tokens * s.units);
+        const int turned = heads * s.turned, copied = heads * s.copied;
+        for (int i = first + (int)threadIdx.x; i < last; i += ROTARY_THREADS) {
+            const int dt = small_div(i, s.units, 1.f / (float)s.units);
+            const long long t = t0 + dt;
+            int j = i - dt * s.units;
+            // which head, and which piece of it
+            const bool turns = j < turned, value = WRITE && j >= turned + copied;
+            const int per = turns ? s.turned : value ? s.valued : s.copied;
+            j -= turns ? 0 : value ? turned + copied : turned;
+            int head = small_div(j, per, 1.f / (float)per);
+            const int piece = j - head * per;
+            const bool key = value || head >= a.heads;
+            head -= !value && key ? a.heads : 0;
+            const T *in = value ? (const T *)args.v + t * args.v_token_stride + head * args.v_head_stride
+                          : key ? (const T *)a.k + t * a.k_token_stride + head * a.k_head_stride
+                                : (const T *)a.q + t * a.q_token_stride + head * a.q_head_stride;
+            T *out;
+            bool keep = true;
+            if (WRITE && key) {
+                const sbvr_kv_cache &c = args.kv;
+                const long long slot = args.slots[t];
+                keep = slot >= 0 && slot < (long long)c.n_pages << page_shift;
+                const long long at = slot & ((1 << page_shift) - 1);
+                out = value ? (T *)c.v + (slot >> page_shift) * c.v_page_stride + at * c.v_token_stride + head * c.v_head_stride
+                            : (T *)c.k + (slot >> page_shift) * c.k_page_stride + at * c.k_token_stride + head * c.k_head_stride;
+            } else {
+                out = key ? (T *)a.k_out + t * a.k_out_token_stride + head * a.k_out_head_stride
+                          : (T *)a.q_out + t * a.q_out_token_stride + head * a.q_out_head_stride;
+            }
+            if (!turns) {
+                const int at = (value ? 0 : 2 * n) + 8 * piece;
+                if (!keep)
+                    continue;
+                if (EVEN || value || at + 8 <= a.head_dim)
+                    store_words(out + at, load_words(in + at));
+                else
+                    for (int e = at; e < a.head_dim; ++e)
+                        out[e] = in[e];
+                continue;
+            }
+            const float *c = cosine + dt * s.width + 8 * piece, *sn = sine + dt * s.width + 8 * piece;
+            const int p0 = 8 * piece;
+            if (EVEN || p0 + 8 <= n) {
+                const int a0 = a.interleaved ? 2 * p0 : p0, b0 = a.interleaved ? 2 * p0 + 8 : n + p0;
+                const Loose<T, 8> x = from_words<T>(load_words(in + a0)), y = from_words<T>(load_words(in + b0));
+                Loose<T, 8> xo, yo;
+                if (a.interleaved) {
+    #pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float u = (float)x.e[2 * e], v = (float)x.e[2 * e + 1];
+                        xo.e[2 * e] = (T)(u * c[e] - v * sn[e]);
+                        xo.e[2 * e + 1] = (T)(v * c[e] + u * sn[e]);
+                        const float w = (float)y.e[2 * e], z = (float)y.e[2 * e + 1];
+                        yo.e[2 * e] = (T)(w * c[e + 4] - z * sn[e + 4]);
+                        yo.e[2 * e + 1] = (T)(z * c[e + 4] + w * sn[e + 4]);
+                    }
+                } else {
+    #pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const float u = (float)x.e[e], v = (float)y.e[e];
+                        xo.e[e] = (T)(u * c[e] - v * sn[e]);
+                        yo.e[e] = (T)(v * c[e] + u * sn[e]);
+                    }
+                }
+                if (keep) {
+                    store_words(out + a0, to_words(xo));
+                    store_words(out + b0, to_words(yo));
+                }
+            } else if (keep) {
+                for (int p = p0; p < n; ++p) {
+                    const int ia = a.interleaved ? 2 * p : p, ib = a.interleaved ? 2 * p + 1 : n + p;
+                    const float u = (float)in[ia], v = (float)in[ib];
+                    out[ia] = (T)(u * c[p - p0] - v * sn[p - p0]);
+                    out[ib] = (T)(v * c[p - p0] + u * sn[p - p0]);
+                }
+            }
+        }
+    }
+}
+
+template <typename T, bool WRITE>
+int run_rotary(const RotaryArgs &a, hipStream_t stream)
+{
+    const sbvr_rotary_args &r = a.r;
+    RotaryShape s;
+    s.turned = (r.pairs + 7) / 8;
+    s.copied = (r.head_dim - 2 * r.pairs + 7) / 8;
+    s.valued = r.head_dim / 8;
+    s.width = 8 * s.turned;
+    s.units = (r.heads + r.kv_heads) * (s.turned + s.copied) + (WRITE ? r.kv_heads * s.valued : 0);
+    // four pieces a thread where there are many tokens, one where there are few
+    const int target = (long long)r.T * s.units > 1024ll * ROTARY_THREADS ? 4 * ROTARY_THREADS : ROTARY_THREADS;
+    s.tokens = s.units > target ? 1 : target / s.units;
+    const int fit = (int)(SBVR_MAX_DYN_LDS / 4 / (2 * sizeof(float) * s.width));
+    if (s.tokens > fit)
+        s.tokens = fit;
+    s.split = s.tokens > 1 || s.units <= target ? s.tokens * s.units : target;
+    const int splits = (s.tokens * s.units + s.split - 1) / s.split;
+    const long long groups = (r.T + (long long)s.tokens - 1) / s.tokens, most = (1 << 22) / splits;
+    const dim3 grid((unsigned)(groups < most ? groups : most), splits);
+    RotaryArgs args = a;
+    int page_shift = WRITE ? __builtin_ctz(a.kv.page_size) : 0;
+    void *argv[] = {&args, &s, &page_shift};
+    const void *kernel = r.pairs % 8 == 0 ? (const void *)rotary_kernel<T, true, WRITE> : (const void *)rotary_kernel<T, false, WRITE>;
+    return launch_kernel(kernel, grid, dim3(ROTARY_THREADS), 2 * sizeof(float) * s.tokens * s.width, stream, argv);
+}
+
+int launch_rotary(const RotaryArgs &a, hipStream_t stream)
+{
+    switch (a.r.dtype) {
+    case SBVR_F16: return a.slots ? run_rotary<f16_t, true>(a, stream) : run_rotary<f16_t, false>(a, stream);
+    case SBVR_BF16: return a.slots ? run_rotary<bf16_t, true>(a, stream) : run_rotary<bf16_t, false>(a, stream);
+    default: return run_rotary<float, false>(a, stream);
+    }
+}
+
+}  // namespace sbvr

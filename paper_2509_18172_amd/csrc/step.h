@@ -1,5 +1,6 @@
 // Shared by the operators between the products of a step (plan, cache write,
-// attention, norms, logits): element types, launch parameters and a search.
+// attention, norms, logits, rotation, beams, pages): element types, launch
+// parameters and a search.
 #pragma once
 
 #include <hip/hip_fp16.h>
@@ -110,6 +111,47 @@ struct NormArgs {
     float scale, eps;
 };
 
+// sbvr_rotary and sbvr_rotary_write: v and slots are given for the latter.
+struct RotaryArgs {
+    sbvr_rotary_args r;
+    sbvr_kv_cache kv;
+    const void *v;
+    int64_t v_token_stride, v_head_stride;
+    const int64_t *slots;
+};
+
+struct PageTable {
+    int R, page_shift, max_pages;
+    const int32_t *context_lens, *page_table;
+    int64_t table_stride;
+};
+
+struct UsageArgs {
+    PageTable t;
+    int n_pages;
+    int32_t *refs, *free_pages, *counts;
+    uint32_t *marks;  // the workspace: a bit per page
+};
+
+struct ForkArgs {
+    PageTable t;  // R: old rows
+    int rows_out, group_in, group_out, n_free;
+    const int32_t *parents, *free_pages, *taken;
+    int32_t *out_table;
+    int64_t out_stride;
+    int32_t *out_lens, *src, *dst, *tokens, *used;
+};
+
+struct CompactArgs {
+    PageTable t;
+    int n_pages;
+    int32_t *out_table;
+    int64_t out_stride;
+    int32_t *src, *dst, *counts;
+    uint32_t *marks;  // the workspace: a bit per page, and behind them
+    int32_t *number;  // the number of the move of a page that moves
+};
+
 int launch_plan(const PlanArgs &a, hipStream_t stream);
 int launch_cache_write(const sbvr_kv_cache &c, int T, const void *k, int64_t k_token_stride, int64_t k_head_stride,
                        const void *v, int64_t v_token_stride, int64_t v_head_stride, const int64_t *slots,
@@ -118,6 +160,16 @@ size_t attn_workspace_bytes(int R, int max_new, int heads, int kv_heads, int hea
 int launch_attn(const AttnArgs &a, hipStream_t stream);
 int launch_norm(const NormArgs &a, int dtype, int x_dtype, hipStream_t stream);
 int launch_logits(const sbvr_logits_args &a, hipStream_t stream);
+int launch_rotary(const RotaryArgs &a, hipStream_t stream);
+size_t beam_workspace_bytes(int R, int B, int V, int n, int n_end);
+int launch_beam(const sbvr_beam_args &a, void *workspace, hipStream_t stream);
+size_t usage_workspace_bytes(int n_pages);
+int launch_usage(const UsageArgs &a, hipStream_t stream);
+int launch_fork(const ForkArgs &a, hipStream_t stream);
+size_t compact_workspace_bytes(int n_pages);
+int launch_compact(const CompactArgs &a, hipStream_t stream);
+int launch_page_copy(const sbvr_kv_cache *caches, int n_caches, int n, const int32_t *src, const int32_t *dst,
+                     const int32_t *tokens, hipStream_t stream);
 
 // The last index i of the ascending start[0 .. n] with start[i] <= v, for
 // start[0] <= v < start[n]: the owner of item v, empty owners skipped.

@@ -24,6 +24,16 @@ struct Api {
     decltype(&sbvr_tree_attention_whole) tree_attention_whole;
     decltype(&sbvr_residual_norm) residual_norm;
     decltype(&sbvr_adjust_logits) adjust_logits;
+    decltype(&sbvr_rotary) rotary;
+    decltype(&sbvr_rotary_write) rotary_write;
+    decltype(&sbvr_beam_select_workspace_bytes) beam_workspace_bytes;
+    decltype(&sbvr_beam_select) beam_select;
+    decltype(&sbvr_page_usage_workspace_bytes) usage_workspace_bytes;
+    decltype(&sbvr_page_usage) page_usage;
+    decltype(&sbvr_page_fork) page_fork;
+    decltype(&sbvr_page_compact_workspace_bytes) compact_workspace_bytes;
+    decltype(&sbvr_page_compact) page_compact;
+    decltype(&sbvr_page_copy) page_copy;
 } api;
 
 // SBVRError, torch's query of a device's current stream and its change of the
@@ -405,6 +415,282 @@ Tensor adjust_logits(const Tensor &logits, const Maybe &history, const Maybe &hi
     return o;
 }
 
+// A [tokens][heads][head_dim] tensor of a type, with contiguous heads.
+struct HeadsOf {
+    void *p = nullptr;
+    int64_t token_stride = 0, head_stride = 0;
+};
+
+HeadsOf heads_like(const Tensor &t, const Tensor &model, const char *what)
+{
+    if (t.dim() != 3 || t.sizes() != model.sizes() || t.stride(2) != 1 || t.scalar_type() != model.scalar_type() ||
+        t.device() != model.device())
+        refuse(std::string(what) + " must have contiguous heads and be " +
+               text(model.scalar_type(), model.sizes(), model.device()));
+    return {t.data_ptr(), t.stride(0), t.stride(1)};
+}
+
+// What rotary and rotary_write have in common: everything but the outputs.
+sbvr_rotary_args rotary_args(const Maybe &q, const Maybe &k, const Tensor &positions, const Tensor &frequencies,
+                             const Maybe &axes, bool interleaved, bool inverse, const at::Device &device)
+{
+    const Tensor &x = q ? *q : *k;
+    require(x.dim() == 3 && dtype_of(x) >= 0, "q and k must be [tokens][heads][head_dim] of fp16, bf16 or fp32");
+    require(!q || !k || (k->dim() == 3 && k->size(0) == q->size(0) && k->size(2) == q->size(2) &&
+                         k->scalar_type() == q->scalar_type()),
+            "q and k must have the same tokens, head_dim and type");
+    const int64_t T = x.size(0);
+    sbvr_rotary_args a = {};
+    a.T = narrow(T, "too many tokens");
+    a.head_dim = narrow(x.size(2), "head_dim is too large");
+    a.dtype = dtype_of(x);
+    a.interleaved = interleaved;
+    a.inverse = inverse;
+    if (q) {
+        const HeadsOf h = heads_like(*q, *q, "q");
+        a.heads = narrow(q->size(1), "too many heads");
+        a.q = h.p;
+        a.q_token_stride = h.token_stride;
+        a.q_head_stride = h.head_stride;
+    }
+    if (k) {
+        const HeadsOf h = heads_like(*k, *k, "k");
+        a.kv_heads = narrow(k->size(1), "too many heads");
+        a.k = h.p;
+        a.k_token_stride = h.token_stride;
+        a.k_head_stride = h.head_stride;
+        require(k->device() == device, "q and k must be on one GPU");
+    }
+    require(positions.dim() == 1 || positions.dim() == 2, "positions must be [tokens] or [axes][tokens]");
+    if (positions.dim() == 1) {
+        a.axes = 1;
+        a.positions = dense<int32_t>(positions, at::kInt, {T}, device, "positions");
+        a.position_stride = T;
+    } else {
+        const RowsOf r = rows(positions, at::kInt, positions.size(0), T, device, "positions");
+        a.axes = narrow(positions.size(0), "too many axes");
+        a.positions = (const int32_t *)r.p;
+        a.position_stride = whole_rows(positions, r);
+    }
+    require(frequencies.dim() == 1, "frequencies must have one dimension");
+    const int64_t n = frequencies.size(0);
+    a.pairs = narrow(n, "too many frequencies");
+    a.frequencies = dense<float>(frequencies, at::kFloat, {n}, device, "frequencies");
+    a.pair_axis = dense<int32_t>(axes, at::kInt, {n}, device, "axes");
+    return a;
+}
+
+Tensor rotated(const Tensor &x, const Maybe &out)
+{
+    return out ? *out : empty(x.sizes(), x.scalar_type(), x.device());
+}
+
+py::tuple rotary(const Maybe &q, const Maybe &k, const Tensor &positions, const Tensor &frequencies, const Maybe &axes,
+                 bool interleaved, bool inverse, const Maybe &q_out, const Maybe &k_out, const py::object &stream)
+{
+    require(q || k, "neither q nor k");
+    require((q || !q_out) && (k || !k_out), "an output needs its input");
+    const at::Device device = (q ? *q : *k).device();
+    require(device.is_cuda(), "q and k must be on a GPU");
+    const Scope scope(device, stream);
+    sbvr_rotary_args a = rotary_args(q, k, positions, frequencies, axes, interleaved, inverse, device);
+    Tensor qo, ko;
+    if (q) {
+        qo = rotated(*q, q_out);
+        const HeadsOf h = heads_like(qo, *q, "q_out");
+        a.q_out = h.p;
+        a.q_out_token_stride = h.token_stride;
+        a.q_out_head_stride = h.head_stride;
+    }
+    if (k) {
+        ko = rotated(*k, k_out);
+        const HeadsOf h = heads_like(ko, *k, "k_out");
+        a.k_out = h.p;
+        a.k_out_token_stride = h.token_stride;
+        a.k_out_head_stride = h.head_stride;
+    }
+    check(api.rotary(&a, scope.stream()), "sbvr_rotary");
+    return py::make_tuple(q ? py::cast(qo) : py::none(), k ? py::cast(ko) : py::none());
+}
+
+py::object rotary_write(const Maybe &q, const Tensor &k_cache, const Tensor &v_cache, const Tensor &k, const Tensor &v,
+                        const Tensor &slots, const Tensor &positions, const Tensor &frequencies, const Maybe &axes,
+                        bool interleaved, bool inverse, const Maybe &q_out, const py::object &stream)
+{
+    const sbvr_kv_cache cache = cache_of(k_cache, v_cache);
+    const at::Device device = k_cache.device();
+    const Scope scope(device, stream);
+    require(q || !q_out, "an output needs its input");
+    heads_of(k, cache.kv_heads, k_cache, "k");
+    const void *vp = heads_of(v, cache.kv_heads, k_cache, "v");
+    require(v.size(0) == k.size(0), "k and v must have the same tokens");
+    require(!q || q->device() == device, "q must be on the cache's GPU");
+    sbvr_rotary_args a = rotary_args(q, k, positions, frequencies, axes, interleaved, inverse, device);
+    Tensor qo;
+    if (q) {
+        qo = rotated(*q, q_out);
+        const HeadsOf h = heads_like(qo, *q, "q_out");
+        a.q_out = h.p;
+        a.q_out_token_stride = h.token_stride;
+        a.q_out_head_stride = h.head_stride;
+    }
+    check(api.rotary_write(&a, &cache, vp, v.stride(0), v.stride(1),
+                           dense<int64_t>(slots, at::kLong, {k.size(0)}, device, "slots"), scope.stream()),
+          "sbvr_rotary_write");
+    return q ? py::cast(qo) : py::none();
+}
+
+// A given workspace, or a new one.
+Tensor workspace_of(const Maybe &given, size_t need, const at::Device &device)
+{
+    if (given) {
+        list<void>(given, at::kByte, device, "workspace");
+        return *given;
+    }
+    return empty({(int64_t)need}, at::kByte, device);
+}
+
+py::tuple beam_select(const Tensor &logits, const Tensor &scores, std::optional<int64_t> n, const Maybe &end_tokens,
+                      const std::optional<std::vector<Tensor>> &out, const Maybe &workspace, const py::object &stream)
+{
+    require(logits.dim() == 2 && logits.is_cuda() && dtype_of(logits) >= 0,
+            "logits must be a GPU tensor [requests * beams][vocabulary] of fp16, bf16 or fp32");
+    require(scores.dim() == 2, "scores must be [requests][beams]");
+    const at::Device device = logits.device();
+    const Scope scope(device, stream);
+    const int64_t R = scores.size(0), B = scores.size(1), V = logits.size(1), N = n.value_or(B);
+    const RowsOf in = rows(logits, logits.scalar_type(), R * B, V, device, "logits");
+    const auto i32 = at::kInt, f32 = at::kFloat;
+    require(N >= 0, "n must not be negative");
+    std::vector<Tensor> o = out ? *out
+                                : std::vector<Tensor>{empty({R, N}, i32, device), empty({R, N}, i32, device),
+                                                      empty({R, N}, f32, device), empty({R, B}, f32, device),
+                                                      empty({R, B}, i32, device)};
+    sbvr_beam_args a = {};
+    a.R = narrow(R, "too many requests");
+    a.B = narrow(B, "too many beams");
+    a.V = narrow(V, "the vocabulary is too large");
+    a.n = narrow(N, "n is too large");
+    a.dtype = dtype_of(logits);
+    a.logits = in.p;
+    a.logits_stride = in.stride;
+    a.scores = dense<float>(scores, f32, {R, B}, device, "scores");
+    a.end_tokens = list<int32_t>(end_tokens, i32, device, "end_tokens");
+    a.n_end = end_tokens ? narrow(end_tokens->size(0), "too many end tokens") : 0;
+    a.tokens = dense<int32_t>(o[0], i32, {R, N}, device, "tokens");
+    a.parents = dense<int32_t>(o[1], i32, {R, N}, device, "parents");
+    a.scores_out = dense<float>(o[2], f32, {R, N}, device, "scores of the output");
+    a.ended = dense<float>(o[3], f32, {R, B}, device, "ended");
+    a.ended_tokens = dense<int32_t>(o[4], i32, {R, B}, device, "ended_tokens");
+    const Tensor ws = workspace_of(workspace, api.beam_workspace_bytes(a.R, a.B, a.V, a.n, a.n_end), device);
+    check(api.beam_select(&a, ws.data_ptr(), (size_t)ws.numel(), scope.stream()), "sbvr_beam_select");
+    return py::make_tuple(o[0], o[1], o[2], o[3], o[4]);
+}
+
+py::tuple page_usage(const Tensor &context_lens, const Tensor &page_table, int64_t page_size, int64_t n_pages,
+                     const std::optional<std::vector<Tensor>> &out, const Maybe &workspace, const py::object &stream)
+{
+    require(context_lens.is_cuda() && context_lens.dim() == 1, "context_lens must be a list on a GPU");
+    const at::Device device = context_lens.device();
+    const Scope scope(device, stream);
+    const int64_t R = context_lens.size(0);
+    const Table table = table_of(page_table, R, device);
+    require(n_pages >= 0, "n_pages must not be negative");
+    const auto i32 = at::kInt;
+    const int r = narrow(R, "too many rows"), pages = narrow(n_pages, "too many pages");
+    std::vector<Tensor> o = out ? *out
+                                : std::vector<Tensor>{empty({n_pages}, i32, device), empty({n_pages}, i32, device),
+                                                      empty({2}, i32, device)};
+    const Tensor ws = workspace_of(workspace, api.usage_workspace_bytes(r, table.pages, pages), device);
+    check(api.page_usage(r, narrow(page_size, "page_size is too large"), pages,
+                         dense<int32_t>(context_lens, i32, {R}, device, "context_lens"), table.p, table.pages,
+                         table.stride, dense<int32_t>(o[0], i32, {n_pages}, device, "refs"),
+                         dense<int32_t>(o[1], i32, {n_pages}, device, "free_pages"),
+                         dense<int32_t>(o[2], i32, {2}, device, "counts"), ws.data_ptr(), (size_t)ws.numel(),
+                         scope.stream()),
+          "sbvr_page_usage");
+    return py::make_tuple(o[0], o[1], o[2]);
+}
+
+py::tuple page_fork(const Tensor &context_lens, const Tensor &page_table, const Tensor &parents, int64_t page_size,
+                    const Tensor &free_pages, const Maybe &taken, const std::optional<std::vector<Tensor>> &out,
+                    const py::object &stream)
+{
+    require(context_lens.is_cuda() && context_lens.dim() == 1, "context_lens must be a list on a GPU");
+    require(parents.dim() == 2, "parents must be [groups][rows of a group]");
+    const at::Device device = context_lens.device();
+    const Scope scope(device, stream);
+    const int64_t G = parents.size(0), N = G * parents.size(1), R = context_lens.size(0);
+    const Table table = table_of(page_table, R, device);
+    const auto i32 = at::kInt;
+    std::vector<Tensor> o = out ? *out
+                                : std::vector<Tensor>{empty({N, table.pages}, i32, device), empty({N}, i32, device),
+                                                      empty({N}, i32, device), empty({N}, i32, device),
+                                                      empty({N}, i32, device), empty({1}, i32, device)};
+    const RowsOf to = rows(o[0], i32, N, table.pages, device, "the new page_table");
+    const int32_t *first = list<int32_t>(taken, i32, device, "taken");
+    require(!taken || taken->size(0) >= 1, "taken must have an element");
+    check(api.page_fork(narrow(G, "too many groups"), narrow(R, "too many rows"), narrow(N, "too many rows"),
+                        narrow(page_size, "page_size is too large"),
+                        dense<int32_t>(context_lens, i32, {R}, device, "context_lens"), table.p, table.pages,
+                        table.stride, dense<int32_t>(parents, i32, parents.sizes(), device, "parents"),
+                        list<int32_t>(free_pages, i32, device, "free_pages"),
+                        narrow(free_pages.size(0), "too many pages"), first, (int32_t *)to.p, whole_rows(o[0], to),
+                        dense<int32_t>(o[1], i32, {N}, device, "the new context_lens"),
+                        dense<int32_t>(o[2], i32, {N}, device, "src"), dense<int32_t>(o[3], i32, {N}, device, "dst"),
+                        dense<int32_t>(o[4], i32, {N}, device, "tokens"), dense<int32_t>(o[5], i32, {1}, device, "used"),
+                        scope.stream()),
+          "sbvr_page_fork");
+    return py::make_tuple(o[0], o[1], o[2], o[3], o[4], o[5]);
+}
+
+py::tuple page_compact(const Tensor &context_lens, const Tensor &page_table, int64_t page_size, int64_t n_pages,
+                       const std::optional<std::vector<Tensor>> &out, const Maybe &workspace, const py::object &stream)
+{
+    require(context_lens.is_cuda() && context_lens.dim() == 1, "context_lens must be a list on a GPU");
+    const at::Device device = context_lens.device();
+    const Scope scope(device, stream);
+    const int64_t R = context_lens.size(0), moves = n_pages / 2;
+    const Table table = table_of(page_table, R, device);
+    require(n_pages >= 0, "n_pages must not be negative");
+    const auto i32 = at::kInt;
+    const int r = narrow(R, "too many rows"), pages = narrow(n_pages, "too many pages");
+    std::vector<Tensor> o = out ? *out
+                                : std::vector<Tensor>{empty({R, table.pages}, i32, device), empty({moves}, i32, device),
+                                                      empty({moves}, i32, device), empty({2}, i32, device)};
+    const RowsOf to = rows(o[0], i32, R, table.pages, device, "the new page_table");
+    const Tensor ws = workspace_of(workspace, api.compact_workspace_bytes(r, table.pages, pages), device);
+    check(api.page_compact(r, narrow(page_size, "page_size is too large"), pages,
+                           dense<int32_t>(context_lens, i32, {R}, device, "context_lens"), table.p, table.pages,
+                           table.stride, (int32_t *)to.p, whole_rows(o[0], to),
+                           dense<int32_t>(o[1], i32, {moves}, device, "src"),
+                           dense<int32_t>(o[2], i32, {moves}, device, "dst"),
+                           dense<int32_t>(o[3], i32, {2}, device, "counts"), ws.data_ptr(), (size_t)ws.numel(),
+                           scope.stream()),
+          "sbvr_page_compact");
+    return py::make_tuple(o[0], o[1], o[2], o[3]);
+}
+
+void page_copy(const std::vector<Tensor> &k_caches, const std::vector<Tensor> &v_caches, const Tensor &src,
+               const Tensor &dst, const Maybe &tokens, const py::object &stream)
+{
+    require(!k_caches.empty() && k_caches.size() == v_caches.size(), "no caches");
+    std::vector<sbvr_kv_cache> caches;
+    for (size_t i = 0; i < k_caches.size(); ++i) {
+        caches.push_back(cache_of(k_caches[i], v_caches[i]));
+        require(k_caches[i].device() == k_caches[0].device(), "the caches must be on one GPU");
+    }
+    const at::Device device = k_caches[0].device();
+    const Scope scope(device, stream);
+    require(src.dim() == 1, "src must be a list");
+    const int64_t n = src.size(0);
+    check(api.page_copy(caches.data(), narrow((int64_t)caches.size(), "too many caches"), narrow(n, "too many copies"),
+                        dense<int32_t>(src, at::kInt, {n}, device, "src"),
+                        dense<int32_t>(dst, at::kInt, {n}, device, "dst"),
+                        dense<int32_t>(tokens, at::kInt, {n}, device, "tokens"), scope.stream()),
+          "sbvr_page_copy");
+}
+
 // The library's functions by name, the class of its errors, torch's query of a
 // device's current stream and its change of the current device.
 void connect(const std::map<std::string, uintptr_t> &address, const py::object &error, const py::object &stream,
@@ -418,6 +704,17 @@ void connect(const std::map<std::string, uintptr_t> &address, const py::object &
         (decltype(api.tree_attention_whole))address.at("sbvr_tree_attention_whole");
     api.residual_norm = (decltype(api.residual_norm))address.at("sbvr_residual_norm");
     api.adjust_logits = (decltype(api.adjust_logits))address.at("sbvr_adjust_logits");
+    api.rotary = (decltype(api.rotary))address.at("sbvr_rotary");
+    api.rotary_write = (decltype(api.rotary_write))address.at("sbvr_rotary_write");
+    api.beam_workspace_bytes = (decltype(api.beam_workspace_bytes))address.at("sbvr_beam_select_workspace_bytes");
+    api.beam_select = (decltype(api.beam_select))address.at("sbvr_beam_select");
+    api.usage_workspace_bytes = (decltype(api.usage_workspace_bytes))address.at("sbvr_page_usage_workspace_bytes");
+    api.page_usage = (decltype(api.page_usage))address.at("sbvr_page_usage");
+    api.page_fork = (decltype(api.page_fork))address.at("sbvr_page_fork");
+    api.compact_workspace_bytes =
+        (decltype(api.compact_workspace_bytes))address.at("sbvr_page_compact_workspace_bytes");
+    api.page_compact = (decltype(api.page_compact))address.at("sbvr_page_compact");
+    api.page_copy = (decltype(api.page_copy))address.at("sbvr_page_copy");
     status_error = error;
     status_error.inc_ref();
     current_stream = stream;
@@ -436,4 +733,11 @@ PYBIND11_MODULE(TORCH_EXTENSION_NAME, m)
     m.def("tree_attention", &tree_attention);
     m.def("residual_norm", &residual_norm);
     m.def("adjust_logits", &adjust_logits);
+    m.def("rotary", &rotary);
+    m.def("rotary_write", &rotary_write);
+    m.def("beam_select", &beam_select);
+    m.def("page_usage", &page_usage);
+    m.def("page_fork", &page_fork);
+    m.def("page_compact", &page_compact);
+    m.def("page_copy", &page_copy);
 }

@@ -1,0 +1,338 @@
+"""The selection of a beam search against the definition in 64 bits, at the
+sizes, masks and ties where it can go wrong."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2509_18172_amd as sb
+
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda"
+F16, BF16, F32 = torch.float16, torch.bfloat16, torch.float32
+INF = math.inf
+
+# How far a score may be off before its own rounding: a lane sums at most 32
+# exponentials in binary32 (31 roundings of 2^-24), each of them within |d| 2^-24 + 2^-23
+# for the exponent's roundings (d = logit - top; beyond |d| = 20 a term adds less than
+# 2^-28 of the sum a piece) and the function's own 2^-23: together below 2^-18.
+OFF = 2.0 ** -18
+
+
+def close(score):
+    return OFF + abs(score) * 2.0 ** -24 if math.isfinite(score) else 0.0
+
+
+def cleaned(row):
+    """Logits as they count: NaN is -infinity, +infinity the largest number."""
+    row = row.astype(np.float64)
+    row[np.isnan(row)] = -INF
+    return np.minimum(row, float(np.finfo(np.float32).max))
+
+
+def candidates(logits, scores, request, beams, most):
+    """(score, beam, token) of each beam's `most` best continuations, best first,
+    and the scores of all [beam][token]."""
+    found, every = [], np.full((beams, logits.shape[1]), -INF)
+    for b in range(beams):
+        base = float(scores[request][b])
+        row = cleaned(logits[request * beams + b])
+        if not math.isfinite(base) or row.max() == -INF:
+            continue
+        # (the largest number and a logarithm do not add up: it is subtracted first)
+        every[b] = base + ((row - row.max()) - math.log(np.exp(row - row.max()).sum()))
+        for v in np.argsort(-row, kind="stable")[:most]:
+            if row[v] > -INF:
+                found.append((-every[b, v], b, int(v)))
+    found.sort()
+    return [(-s, b, v) for s, b, v in found], every
+
+
+def check(logits, scores, n, ends=(), got=None, exact=False):
+    """got (or the operator's choice) against the definition.  Where two scores
+    are nearer than their errors either may be first; exact: none are but equal ones."""
+    R, B = scores.shape
+    if got is None:
+        e = torch.tensor(list(ends), dtype=torch.int32, device=DEV) if ends is not None else None
+        got = sb.beam_select(logits, scores, n=n, end_tokens=e)
+    host = logits.float().cpu().numpy() if logits.dtype != F32 else logits.cpu().numpy()
+    base, ends = scores.cpu().numpy(), set(ends or ())
+    tokens, parents, chosen = got.tokens.tolist(), got.parents.tolist(), got.scores.tolist()
+    ended, ended_tokens = got.ended.tolist(), got.ended_tokens.tolist()
+    for r in range(R):
+        every, value = candidates(host, base, r, B, n + len(ends) + 1)
+        going = [c for c in every if c[2] not in ends]
+        real = min(n, len(going))
+        assert tokens[r][real:] == [-1] * (n - real) and parents[r][real:] == [-1] * (n - real)
+        assert chosen[r][real:] == [-INF] * (n - real)
+        pairs = list(zip(parents[r], tokens[r]))[:real]
+        assert len(set(pairs)) == real and all(value[p] > -INF and p[1] not in ends for p in pairs)
+        for i, p in enumerate(pairs):
+            assert abs(chosen[r][i] - value[p]) <= close(value[p]), (r, i)
+            assert value[p] >= going[i][0] - 2 * OFF, (r, i)  # no better one was passed over
+            if exact:
+                assert p == going[i][1:], (r, i, p, going[i])
+        for i in range(1, real):  # order, and equal logits of a beam by token
+            (b0, v0), (b1, v1) = pairs[i - 1], pairs[i]
+            assert chosen[r][i - 1] >= chosen[r][i]
+            if b0 == b1 and host[r * B + b0][v0] == host[r * B + b1][v1]:
+                assert v0 < v1
+        last = every[min(n, len(every)) - 1][0] if every else -INF
+        for b in range(B):
+            mine = [c for c in every[:n] if c[1] == b and c[2] in ends]
+            if mine and (exact or mine[0][0] > every[n][0] + 2 * OFF if len(every) > n else mine):
+                assert ended_tokens[r][b] == mine[0][2] or abs(value[(b, ended_tokens[r][b])] - mine[0][0]) <= 2 * OFF
+                assert abs(ended[r][b] - mine[0][0]) <= close(mine[0][0])
+            elif ended_tokens[r][b] == -1:
+                assert ended[r][b] == -INF
+            else:  # an end that is as good as the n-th best
+                s = value[(b, ended_tokens[r][b])]
+                assert ended_tokens[r][b] in ends and s >= last - 2 * OFF and abs(ended[r][b] - s) <= close(s)
+                assert not exact
+    return got
+
+
+def make(R, B, V, dtype, seed=0, masked=0.0, scale=3.0):
+    gen = torch.Generator(device=DEV).manual_seed(seed)
+    logits = (scale * torch.randn(R * B, V, generator=gen, device=DEV)).to(dtype)
+    if masked:
+        logits.masked_fill_(torch.rand(R * B, V, generator=gen, device=DEV) < masked, -INF)
+    scores = -3.0 * torch.rand(R, B, generator=gen, device=DEV).cumsum(1)
+    return logits, scores
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16, F32])
+@pytest.mark.parametrize("R,B,V,n", [(1, 1, 1000, 1), (1, 4, 5003, 4), (3, 2, 2048, 5), (2, 5, 8191, 10), (1, 32, 777, 32),
+                                     (9, 8, 3001, 16), (2, 3, 20000, 3), (1, 1, 50001, 64)])
+def test_beam(dtype, R, B, V, n):
+    check(*make(R, B, V, dtype), n)
+
+
+@pytest.mark.parametrize("V", [1, 2, 3, 7, 8, 9, 15, 63, 64, 65, 255, 256, 257, 2047, 2049, 4097])
+@pytest.mark.parametrize("n", [1, 3, 16])
+def test_small_vocabularies(V, n):
+    for dtype in (F16, F32):
+        check(*make(2, 3, V, dtype, seed=V), n, ends=(0, V - 1) if V > 2 else ())
+
+
+@pytest.mark.parametrize("R,B,V,n,ends", [(64, 8, 16385, 8, 1), (128, 4, 9000, 8, 3), (40, 16, 8192, 16, 0), (600, 1, 8193, 5, 2)])
+def test_large_tiles(R, B, V, n, ends):
+    """Enough rows for tiles of 8192 logits."""
+    logits, scores = make(R, B, V, F16, seed=R, masked=0.05)
+    rng = np.random.default_rng(R)
+    check(logits, scores, n, ends=rng.permutation(V)[:ends].tolist())
+
+
+@pytest.mark.parametrize("B,n,V", [(32, 32, 70001), (32, 64, 40000), (16, 64, 100003), (1, 64, 300007)])
+def test_parts_of_several_tiles(B, n, V):
+    """More tiles than a request may have parts."""
+    check(*make(1, B, V, BF16, seed=n), n)
+
+
+def test_large_tiles_in_turn():
+    """Parts of several large tiles: 640 rows that 32 beams and 32 entries leave
+    four parts each."""
+    logits, scores = make(20, 32, 70000, F16, seed=4)
+    check(logits, scores, 30, ends=(5, 69999))
+
+
+@pytest.mark.parametrize("order", ["rising", "falling", "equal", "two"])
+@pytest.mark.parametrize("V", [300, 9000])
+@pytest.mark.parametrize("n", [1, 8, 60])
+def test_ordered_and_equal_logits(order, V, n):
+    """Logits of which many lanes, or one, have all the best: multiples of 1/8, so
+    that equal scores are equal in every form."""
+    row = {"rising": np.arange(V) // 4 / 8.0, "falling": -(np.arange(V) // 4) / 8.0, "equal": np.zeros(V),
+           "two": (np.arange(V) % 2) / 8.0}[order]
+    row = torch.tensor(row, dtype=F32, device=DEV)
+    for B in (1, 3):
+        logits = row.expand(2 * B, V).contiguous()
+        check(logits, torch.full((2, B), -1.0, device=DEV), n, ends=(0, V // 2, V - 1), exact=True)
+
+
+def test_many_rows_of_equal_logits():
+    """The same with large tiles, where a list is longest."""
+    V = 8192 * 2 + 5
+    logits = torch.zeros(260 * 2, V, dtype=F16, device=DEV)
+    logits[::2, 100:2000] = 1.0
+    check(logits, torch.zeros(260, 2, device=DEV), 30, ends=(101, 500), exact=True)
+    rising = (torch.arange(V, device=DEV) // 32 / 8.0).to(F32).expand(520, V).contiguous()
+    check(rising[:6], torch.zeros(3, 2, device=DEV), 30, exact=True)
+    got = sb.beam_select(rising, torch.zeros(260, 2, device=DEV), n=30)
+    few = sb.beam_select(rising[:2], torch.zeros(1, 2, device=DEV), n=30)
+    assert torch.equal(got.tokens, few.tokens.expand(260, 30)) and torch.equal(got.parents, few.parents.expand(260, 30))
+
+
+@pytest.mark.parametrize("V", [100, 2500, 9000])
+def test_masked_rows(V):
+    """Rows and beams that leave nothing, or less than is asked for."""
+    logits, scores = make(4, 3, V, F32, seed=1)
+    logits[0:3] = -INF                      # a request without continuations
+    logits[3] = -INF                        # one beam of three
+    logits[4, 5:] = -INF                    # five tokens
+    logits[5] = -INF
+    logits[5, V - 1] = 2.0                  # one
+    scores[2, 0] = -INF                     # beams that have ended
+    scores[3] = -INF
+    got = check(logits, scores, 8, ends=(4,))
+    assert got.tokens[0].tolist() == [-1] * 8 and got.ended_tokens[3].tolist() == [-1] * 3
+    scores[1, 1], scores[1, 2], scores[2, 1] = math.nan, INF, -INF
+    check(logits, scores, 8, ends=(4,))
+
+
+def test_logits_of_dead_beams_are_not_read():
+    logits, scores = make(2, 2, 3000, F16, seed=2)
+    scores[0, 1] = -INF
+    want = sb.beam_select(logits, scores)
+    logits[1] = math.nan
+    got = sb.beam_select(logits, scores)
+    assert torch.equal(got.tokens, want.tokens) and torch.equal(got.scores, want.scores)
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16, F32])
+def test_nan_and_infinite_logits(dtype):
+    logits, scores = make(3, 2, 4000, dtype, seed=3)
+    logits[0, 10] = math.nan
+    logits[1] = math.nan
+    logits[2, 7], logits[2, 3000] = INF, INF
+    logits[3, ::2] = math.nan
+    logits[4, 100] = INF
+    logits[5, 3999] = -INF
+    check(logits, scores, 4)
+
+
+def test_extreme_logits():
+    """Far apart, all far from 0, and so small that they are denormal."""
+    V = 3000
+    logits = torch.full((4, V), -1e30, dtype=F32, device=DEV)
+    logits[0, 17] = 3e38
+    logits[1] = torch.linspace(-3e38, 3e38, V, device=DEV)
+    logits[2] = 1e30
+    logits[3] = torch.linspace(0, 1e-40, V, device=DEV)
+    check(logits, torch.tensor([[-1.0], [-2.0], [-3.0], [-4.0]], device=DEV), 4)
+
+
+def test_ends_among_the_best():
+    """Ends inside and behind the n best, several of one beam, all of a beam."""
+    V = 1000
+    logits = torch.zeros(4, V, dtype=F32, device=DEV)
+    logits[0, [3, 4, 5]] = torch.tensor([9.0, 8.0, 7.0], device=DEV)
+    logits[1, [3, 4, 900]] = torch.tensor([7.5, 10.0, 9.5], device=DEV)
+    logits[2, :] = -INF
+    logits[2, [3, 4]] = 1.0
+    logits[3, 5] = 5.0
+    scores = torch.tensor([[0.0, -0.25], [-1.0, -2.0]], device=DEV)
+    for n in (1, 2, 3, 4, 6):
+        check(logits, scores, n, ends=(4, 3), exact=True)
+    check(logits, scores, 2, ends=(4, 4, 3, -1, V, 2 ** 31 - 1), exact=True)  # twice, and no tokens
+
+
+@pytest.mark.parametrize("n", [1, 2, 30])
+def test_only_ends(n):
+    V = 50
+    logits, scores = make(2, 2, V, F32, seed=5)
+    check(logits, scores, n, ends=range(0, 34))
+
+
+def test_rows_of_a_larger_matrix():
+    logits, scores = make(3, 2, 4001, F16, seed=6)
+    want = sb.beam_select(logits, scores)
+    room = torch.full((6, 4100), 60000.0, dtype=F16, device=DEV)
+    room[:, 3:4004] = logits
+    got = sb.beam_select(room[:, 3:4004], scores)
+    for name in sb.BeamChoice.__slots__:
+        assert torch.equal(getattr(got, name), getattr(want, name))
+
+
+def test_one_row_for_all_beams():
+    """An expanded prompt's logits (row stride 0): equal beams are told apart by
+    their scores, and then by their number."""
+    logits, _ = make(1, 1, 6000, F32, seed=7)
+    rows = logits.expand(4, 6000)
+    check(rows, torch.tensor([[-1.0, -1.0], [-1.0, -INF]], device=DEV), 4, exact=True)
+
+
+@pytest.mark.parametrize("seed", range(8))
+def test_random(seed):
+    rng = np.random.default_rng(seed)
+    R, B = int(rng.integers(1, 20)), int(rng.integers(1, 17))
+    V, n = int(rng.integers(1, 12000)), int(rng.integers(1, 40))
+    logits, scores = make(R, B, V, [F16, BF16, F32][seed % 3], seed=seed, masked=float(rng.random()) * 0.9)
+    check(logits, scores, n, ends=rng.integers(0, V, int(rng.integers(0, 5))).tolist())
+
+
+def test_the_same_call_gives_the_same_bits():
+    logits, scores = make(16, 8, 30000, F16, seed=8)
+    a = sb.beam_select(logits, scores, n=16)
+    for _ in range(3):
+        b = sb.beam_select(logits, scores, n=16)
+        for name in sb.BeamChoice.__slots__:
+            assert torch.equal(getattr(a, name), getattr(b, name))
+
+
+def test_steps_of_a_search():
+    """Three steps, each on the scores of the one before, as one search: the sums
+    of the steps' exact scores."""
+    R, B, V = 2, 4, 500
+    scores = torch.full((R, B), -INF, device=DEV)
+    scores[:, 0] = 0
+    for step in range(3):
+        logits, _ = make(R, B, V, F32, seed=20 + step)
+        scores = check(logits, scores, B, ends=(1,)).scores
+
+
+def test_in_a_graph():
+    logits, scores = make(2, 4, 9000, F16, seed=9)
+    out, ws = sb.beam_select(logits, scores, n=6, end_tokens=torch.tensor([7], dtype=torch.int32, device=DEV)), None
+    ws = torch.empty(sb.sbvr_beam_select_workspace_bytes(2, 4, 9000, 6, 1), dtype=torch.uint8, device=DEV)
+    ends = torch.tensor([7], dtype=torch.int32, device=DEV)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        sb.beam_select(logits, scores, n=6, end_tokens=ends, out=out, workspace=ws)
+    for step in range(4):
+        l, s = make(2, 4, 9000, F16, seed=30 + step)
+        logits.copy_(l)
+        scores.copy_(s)
+        ws.fill_(255)
+        graph.replay()
+        torch.cuda.synchronize()
+        eager = check(l, s, 6, ends=(7,))
+        for name in sb.BeamChoice.__slots__:
+            assert torch.equal(getattr(out, name), getattr(eager, name))
+
+
+def test_two_at_once():
+    """Two calls on two streams, each with a workspace of its own."""
+    a, b = make(8, 4, 30000, F16, seed=10), make(8, 4, 30000, F16, seed=11)
+    want = [sb.beam_select(*x) for x in (a, b)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    got = [sb.beam_select(*x, stream=s) for x, s in zip((a, b), streams)]
+    torch.cuda.synchronize()
+    for g, w in zip(got, want):
+        assert torch.equal(g.tokens, w.tokens) and torch.equal(g.scores, w.scores)
+
+
+def test_no_requests():
+    got = sb.beam_select(torch.empty(0, 100, dtype=F16, device=DEV), torch.empty(0, 4, device=DEV))
+    assert got.tokens.shape == (0, 4) and got.ended.shape == (0, 4)
+
+
+def test_refusals():
+    logits, scores = make(2, 4, 100, F16)
+    ends = torch.tensor([1], dtype=torch.int32, device=DEV)
+    for bad in (dict(logits=logits[:7]), dict(logits=logits.double()), dict(logits=logits.t()), dict(scores=scores.double()),
+                dict(scores=scores[0]), dict(scores=scores.t()), dict(end_tokens=ends.long()), dict(end_tokens=ends[None]),
+                dict(workspace=torch.empty(4, device=DEV)), dict(n=-1),
+                dict(out=sb.BeamChoice(*[torch.empty(2, 3, device=DEV)] * 5))):
+        with pytest.raises(AssertionError):
+            sb.beam_select(**{**dict(logits=logits, scores=scores, end_tokens=ends), **bad})
+    small = torch.empty(64, dtype=torch.uint8, device=DEV)
+    for bad in (dict(n=0), dict(n=65), dict(n=64, end_tokens=ends), dict(workspace=small),
+                dict(logits=logits.expand(2, 8, 100).reshape(16, 100)[:0], scores=scores[:, :0])):
+        with pytest.raises(sb.SBVRError):
+            sb.beam_select(**{**dict(logits=logits, scores=scores), **bad})
+    with pytest.raises(sb.SBVRError):
+        sb.beam_select(torch.zeros(33, 50, device=DEV), torch.zeros(1, 33, device=DEV))
