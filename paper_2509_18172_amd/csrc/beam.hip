@@ -3,34 +3,34 @@
 //
 // Two launches.  The first reads the logits once: a row is cut into parts, one a
 // workgroup, which goes through its part in tiles held in registers and leaves the
-// part's largest logit, its sum of exponentials, and its `keep` = n + n_end best
-// logits (no beam can have more continuations among the chosen ones, and an end
-// that counts is among the n best).  The second joins a request's parts.
+// part's sum of exponentials and its `keep` = n + n_end best logits (no beam can have
+// more continuations among the chosen ones, and an end that counts is among the n
+// best).  The second joins a request's parts.
 //
-// What a tile adds to the best so far: each four lanes' best logit is a group's, 64
-// groups in all, and the keep-th best of the groups is a value that at least `keep`
+// What a tile adds to the best so far: each four lanes' largest logit is a group's, 64
+// groups in all, and the keep-th largest of these is a value that at least `keep`
 // logits reach, so what is below it cannot be chosen.  What is left -- hardly more
 // than `keep` -- goes into a list, whose entries are ranked by counting the better
-// ones.  A logit is compared with its place: key = (logit, ~token) as one number, so
-// equal logits are ordered, keys are all different, and lists have a bound: the
-// logits of `keep` groups.
+// ones.  Only where so many logits are alike that the list does not hold them, the
+// keep-th best is found bit by bit.  A logit is compared with its place: key =
+// (logit, ~token) as one number, so equal logits are ordered and keys are all
+// different.
 //
-// Sums: exp(l - max) = 2^((l - max) log2 e), with log2 e in two parts, since its
-// rounding would show in every term alike; binary32 within a lane and a tile,
-// binary64 between lanes, tiles and parts.  Two continuations' order may hang on the
-// last bits of these sums.
+// Sums: exp(l - r) = 2^(l log2 e - c), one rounding for the exponent; r = c / log2 e
+// is what the sum refers to, so c's own rounding costs nothing.  (The rounding of
+// log2 e is 1.4e-8 of the exponent; between a request's beams nearly all of that
+// cancels.)  Binary32 within a lane and a tile, binary64 between lanes, tiles and
+// parts: two continuations' order may hang on the last bits.
 #include "step.h"
 
 namespace sbvr {
 
 constexpr int BEAM_THREADS = 256, BEAM_ENTRIES = 4096;  // of a request's parts together
-constexpr float LARGEST = 3.402823466e38f;
-constexpr float LOG2E_HIGH = 1.44269502162933349609375f, LOG2E_LOW = 1.92596299112661746887e-8f;
+constexpr int BEAM_LIST = 256;                          // a tile's logits to be ranked
+constexpr float LOG2E = 1.44269502f, LARGEST = 3.402823466e38f;
 
 struct PartSum {
-    double sum;  // of exp(logit - top)
-    float top;   // -infinity: the part has no logit
-    float unused;
+    double sum, reference;  // of exp(logit - reference); reference -infinity: the part has no logit
 };
 
 struct BeamShape {
@@ -45,198 +45,202 @@ __device__ __forceinline__ uint32_t ordered(float v)
 }
 __device__ __forceinline__ float unordered(uint32_t u) { return __uint_as_float(u & 0x80000000u ? u & 0x7fffffffu : ~u); }
 
-__device__ __forceinline__ uint64_t key_of(float v, int token) { return (uint64_t)ordered(v) << 32 | (uint32_t)~token; }
-
-__device__ __forceinline__ uint64_t shuffle_xor(uint64_t v, int mask)
+// (+infinity as the largest number, and -0 as 0)
+__device__ __forceinline__ uint64_t key_of(float v, int token)
 {
-    return (uint64_t)__shfl_xor((uint32_t)(v >> 32), mask) << 32 | __shfl_xor((uint32_t)v, mask);
-}
-
-// The `keep` largest of the c > keep different numbers in list, to kept, in no order.
-__device__ void largest(const uint64_t *list, int c, int keep, uint64_t *kept, int *counts)
-{
-    const int lane = threadIdx.x & 63;
-    __syncthreads();
-    if (threadIdx.x < 65)
-        counts[threadIdx.x] = 0;
-    __syncthreads();
-    uint64_t least = 0;  // bit by bit the largest number that `keep` of them reach
-    for (int bit = 63; bit >= 0; --bit) {
-        const uint64_t candidate = least | 1ull << bit;
-        int reach = 0;
-        for (int i = threadIdx.x; i < (c + 63) / 64 * 64; i += BEAM_THREADS)
-            reach += __popcll(__ballot(i < c && list[min(i, c - 1)] >= candidate));
-        if (lane == 0 && reach)
-            atomicAdd(&counts[bit], reach);
-        __syncthreads();
-        if (counts[bit] >= keep)
-            least = candidate;
-    }
-    for (int i = threadIdx.x; i < c; i += BEAM_THREADS)
-        if (list[i] >= least)
-            kept[atomicAdd(&counts[64], 1)] = list[i];
-    __syncthreads();
+    return (uint64_t)ordered(fminf(v, LARGEST) + 0.f) << 32 | (uint32_t)~token;
 }
 
 // CH: pieces of eight logits a thread holds of a tile.
 template <typename T, int CH>
 __global__ void __launch_bounds__(BEAM_THREADS) beam_part_kernel(sbvr_beam_args a, BeamShape s, PartSum *sums, uint64_t *entries)
 {
-    constexpr int TILE = 8 * CH * BEAM_THREADS;
-    extern __shared__ uint64_t list[];  // keep entries of the tiles before, and the logits of keep groups
-    __shared__ uint64_t group[64], kept[SBVR_BEAM_KEEP_MAX], least_key;
-    __shared__ int rank[64], count, counts[65];
-    __shared__ float tile_top;
-    __shared__ double lane_sum[BEAM_THREADS / 64];
-    const int tid = threadIdx.x, row = blockIdx.x / s.parts, part = blockIdx.x % s.parts;
+    constexpr int TILE = 8 * CH * BEAM_THREADS, WAVES = BEAM_THREADS / 64;
+    __shared__ uint64_t list[SBVR_BEAM_KEEP_MAX + BEAM_LIST];  // the best so far, and what may be better
+    __shared__ float group[2][64];
+    __shared__ int count, counts[2];
+    __shared__ double wave_sum[WAVES];
+    const int tid = threadIdx.x, lane = tid & 63, row = blockIdx.x / s.parts, part = blockIdx.x % s.parts;
     if (!isfinite(uniform_load(a.scores + row)))
         return;  // the join knows
     const T *in = (const T *)a.logits + row * a.logits_stride;
 
-    float top = -INFINITY;
-    uint64_t floor_key = 1;  // the keep-th best so far
+    double total = 0., reference = -INFINITY;
+    float top = -INFINITY, offset = 0.f;
+    uint32_t floor = ordered(-LARGEST);  // what a logit has to reach: more than the keep-th best so far
     int have = 0;
-    double total = 0.;
     const int first_tile = part * s.tiles;
     for (int tile = first_tile; tile < first_tile + s.tiles && (long long)tile * TILE < a.V; ++tile) {
         float x[CH][8];
-        int at[CH];
+        // a piece that would pass the row's end is moved back to end with it; its
+        // first elements belong to the piece before
+        const int v0 = tile * TILE + tid * 8;
+        auto at = [&](int c) { return max(min(v0 + c * 8 * BEAM_THREADS, a.V - 8), 0); };
+        if (tid == 0)
+            count = have;
+        if (a.V >= 8) {
+            Words<T> w[CH];
 #pragma unroll
-        for (int c = 0; c < CH; ++c) {
-            const int v = tile * TILE + (c * BEAM_THREADS + tid) * 8;
-            Loose<T, 8> l;
-            at[c] = max(min(v, a.V - 8), 0);
-            if (a.V >= 8)
-                l = from_words<T>(load_words(in + at[c]));
-            else
+            for (int c = 0; c < CH; ++c)
+                w[c] = load_words(in + at(c));
+#pragma unroll
+            for (int c = 0; c < CH; ++c) {
+                const Loose<T, 8> l = from_words<T>(w[c]);
 #pragma unroll
                 for (int e = 0; e < 8; ++e)
-                    l.e[e] = in[min(e, a.V - 1)];
+                    x[c][e] = (float)l.e[e];
+            }
+        } else {
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-                x[c][e] = at[c] + e >= v && at[c] + e < a.V ? (float)l.e[e] : -INFINITY;
+            for (int c = 0; c < CH; ++c)
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    x[c][e] = (float)in[min(e, a.V - 1)];
         }
-        float best = -INFINITY;
+        if ((tile + 1ll) * TILE > a.V)  // the row's last tile
 #pragma unroll
-        for (int c = 0; c < CH; ++c)
+            for (int c = 0; c < CH; ++c)
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    x[c][e] = at(c) + e >= v0 + c * 8 * BEAM_THREADS && at(c) + e < a.V ? x[c][e] : -INFINITY;
+        float piece_top[CH], best = -INFINITY;  // (NaN is passed over)
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            piece_top[c] = -INFINITY;
 #pragma unroll
             for (int e = 0; e < 8; ++e)
-                best = fmaxf(best, x[c][e]);
-        int token = 0;
-#pragma unroll
-        for (int c = CH - 1; c >= 0; --c)
-#pragma unroll
-            for (int e = 7; e >= 0; --e)
-                token = x[c][e] == best ? at[c] + e : token;
-        uint64_t mine = best > -INFINITY ? key_of(fminf(best, LARGEST), token) : 0;
-        mine = max(mine, shuffle_xor(mine, 1));
-        mine = max(mine, shuffle_xor(mine, 2));
+                piece_top[c] = fmaxf(piece_top[c], x[c][e]);
+            best = fmaxf(best, piece_top[c]);
+        }
+        float in_group = best;
+        in_group = fmaxf(in_group, __shfl_xor(in_group, 1));
+        in_group = fmaxf(in_group, __shfl_xor(in_group, 2));
+        float *groups = group[tile & 1];
         if ((tid & 3) == 0)
-            group[tid >> 2] = mine;
-        if (tid < 64)
-            rank[tid] = 0;
-        if (tid == 0) {
-            least_key = 1;
-            tile_top = -INFINITY;
-            count = have;
-        }
+            groups[tid >> 2] = in_group;
         __syncthreads();
-        {
-            const uint64_t g = group[tid & 63];
-            int better = 0;
+
+        const float mine = groups[lane];
+        float tile_top = mine;
 #pragma unroll
-            for (int j = 0; j < 16; ++j)
-                better += group[(tid >> 6) * 16 + j] > g;
-            if (better)
-                atomicAdd(&rank[tid & 63], better);
+        for (int m = 32; m; m >>= 1)
+            tile_top = fmaxf(tile_top, __shfl_xor(tile_top, m));
+        // the keep-th largest of the groups' maxima, to its leading 16 bits
+        uint32_t least = 0;
+#pragma unroll
+        for (int bit = 31; bit >= 16; --bit) {
+            const uint32_t candidate = least | 1u << bit;
+            least = __popcll(__ballot(ordered(mine) >= candidate)) >= s.keep ? candidate : least;
         }
-        __syncthreads();
-        if (tid < 64 && group[tid]) {
-            if (rank[tid] == s.keep - 1)
-                least_key = group[tid];
-            if (rank[tid] == 0)
-                tile_top = unordered((uint32_t)(group[tid] >> 32));
-        }
-        __syncthreads();
+        const float least_value = fminf(unordered(max(least, floor)), LARGEST);
         if (tile_top > -INFINITY) {  // the same for all
-            // NaN is passed over by the maxima above and the comparisons below, and
-            // would show in the sum only; +infinity counts as the largest number
-            auto clean = [&] {
+            tile_top = fminf(tile_top, LARGEST);
+            // differences instead where c is so large that 2 to its rounding is (2^-25 of
+            // c: 0.04 at a million)
+            const bool huge = fabsf(tile_top) > 1e6f || (fabsf(top) > 1e6f && top > -INFINITY);
+            if (tile_top > top) {
+                const double now = huge ? (double)tile_top : (double)(tile_top * LOG2E) / (double)LOG2E;
+                total *= reference > -INFINITY ? exp(reference - now) : 0.;
+                reference = now;
+                offset = tile_top * LOG2E;
+                top = tile_top;
+            }
+            float sum = 0.f;
 #pragma unroll
-                for (int c = 0; c < CH; ++c)
+            for (int c = 0; c < CH; ++c)
 #pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        x[c][e] = x[c][e] == x[c][e] ? fminf(x[c][e], LARGEST) : -INFINITY;
-            };
-            if (tile_top >= LARGEST)
-                clean();
-            const float new_top = fmaxf(top, tile_top);
-            total *= top > -INFINITY ? exp((double)top - (double)new_top) : 0.;
-            top = new_top;
-            auto exponentials = [&] {
-                float sum = 0.f;
+                for (int e = 0; e < 8; ++e)
+                    sum += __builtin_amdgcn_exp2f(__builtin_fmaf(x[c][e], LOG2E, -offset));
+            if (huge || sum != sum || sum > LARGEST) {
+                sum = 0.f;
 #pragma unroll
                 for (int c = 0; c < CH; ++c)
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
-                        const float d = x[c][e] - top;
-                        sum += __builtin_amdgcn_exp2f(__builtin_fmaf(d, LOG2E_HIGH, d * LOG2E_LOW));
+                        const float l = x[c][e] == x[c][e] ? fminf(x[c][e], LARGEST) : -INFINITY;
+                        sum += __builtin_amdgcn_exp2f(huge ? (l - top) * LOG2E : __builtin_fmaf(l, LOG2E, -offset));
                     }
-                return sum;
-            };
-            float sum = exponentials();
-            if (sum != sum) {
-                clean();
-                sum = exponentials();
             }
             total += (double)sum;
-            const uint64_t least = max(least_key, floor_key);
-            const float least_value = least > 1 ? unordered((uint32_t)(least >> 32)) : -INFINITY;
-            if (mine >= least)  // something in the four lanes
+
 #pragma unroll
-                for (int c = 0; c < CH; ++c)
+            for (int c = 0; c < CH; ++c)
+                if (piece_top[c] >= least_value)
 #pragma unroll
                     for (int e = 0; e < 8; ++e)
-                        if (x[c][e] > -INFINITY && x[c][e] >= least_value) {
-                            const uint64_t key = key_of(x[c][e], at[c] + e);
-                            if (key >= least)
-                                list[atomicAdd(&count, 1)] = key;
+                        if (x[c][e] >= least_value) {
+                            const int k = atomicAdd(&count, 1);
+                            if (k < SBVR_BEAM_KEEP_MAX + BEAM_LIST)
+                                list[k] = key_of(x[c][e], at(c) + e);
                         }
         }
         __syncthreads();
         int c = count;
-        if (c > have) {
-            const uint64_t *from = list;
-            if (c > BEAM_THREADS) {
-                largest(list, c, s.keep, kept, counts);
-                from = kept;
-                c = s.keep;
+        if (c > BEAM_LIST) {
+            // too many alike: the keep-th best of the tile's and of those before is found
+            // bit by bit, from the logits in memory
+            const uint64_t before = tid < have ? list[tid] : 0;
+            const int first = tile * TILE, n = min(TILE, a.V - first);
+            auto key_at = [&](int i) {
+                const float l = (float)in[first + i];
+                return l > -INFINITY ? key_of(l, first + i) : 0;
+            };
+            uint64_t least_key = 0;
+            for (int bit = 63; bit >= 0; --bit) {
+                const uint64_t candidate = least_key | 1ull << bit;
+                int reach = before >= candidate;
+                for (int i = tid; i < n; i += BEAM_THREADS)
+                    reach += key_at(i) >= candidate;
+                if (tid == 0)
+                    counts[bit & 1] = 0;
+                __syncthreads();
+                atomicAdd(&counts[bit & 1], reach);
+                __syncthreads();
+                least_key = counts[bit & 1] >= s.keep ? candidate : least_key;
             }
-            const uint64_t key = tid < c ? from[tid] : 0;
+            if (tid == 0)
+                count = 0;
+            __syncthreads();
+            if (before && before >= least_key)
+                list[atomicAdd(&count, 1)] = before;
+            for (int i = tid; i < n; i += BEAM_THREADS) {
+                const uint64_t key = key_at(i);
+                if (key && key >= least_key)
+                    list[atomicAdd(&count, 1)] = key;
+            }
+            __syncthreads();
+            c = count;
+            have = 0;
+        }
+        if (c > have) {
+            uint64_t key = 0;
             int better = 0;
-            for (int j = 0; j < c; ++j)
-                better += from[j] > key;
+            if (tid < c) {
+                key = list[tid];
+                for (int j = 0; j < c; ++j)
+                    better += list[j] > key;
+            }
             __syncthreads();
             if (tid < c && better < s.keep)
                 list[better] = key;
             have = min(c, s.keep);
             __syncthreads();
             if (have == s.keep)
-                floor_key = list[s.keep - 1];
+                floor = (uint32_t)(list[s.keep - 1] >> 32) + 1;
         }
     }
 #pragma unroll
     for (int m = 32; m; m >>= 1)
         total += __shfl_xor(total, m);
-    if ((tid & 63) == 0)
-        lane_sum[tid >> 6] = total;
+    if (lane == 0)
+        wave_sum[tid >> 6] = total;
     __syncthreads();
     if (tid == 0) {
         total = 0.;
 #pragma unroll
-        for (int w = 0; w < BEAM_THREADS / 64; ++w)
-            total += lane_sum[w];
-        sums[blockIdx.x] = PartSum{total, top, 0.f};
+        for (int w = 0; w < WAVES; ++w)
+            total += wave_sum[w];
+        sums[blockIdx.x] = PartSum{total, reference};
     }
     if (tid < s.keep)
         entries[(long long)blockIdx.x * s.keep + tid] = tid < have ? list[tid] : 0;
@@ -261,7 +265,7 @@ __global__ void __launch_bounds__(THREADS) beam_join_kernel(sbvr_beam_args a, Be
     constexpr uint32_t END = 1u << 31;
     extern __shared__ double list_score[];  // and behind them, each entry's place, beam and whether it is an end
     __shared__ double add[SBVR_BEAMS_MAX];
-    __shared__ float beam_top[SBVR_BEAMS_MAX];
+    __shared__ double beam_reference[SBVR_BEAMS_MAX];
     __shared__ Candidate group[64], least;
     __shared__ int rank[64], count;
     __shared__ float score_out[SBVR_BEAM_KEEP_MAX], ended[SBVR_BEAMS_MAX];
@@ -272,24 +276,23 @@ __global__ void __launch_bounds__(THREADS) beam_join_kernel(sbvr_beam_args a, Be
     entries += request * all;
     sums += request * a.B * s.parts;
 
-    // what a beam's logits, less the largest, are added to: its score without the
-    // logarithm of its sum
+    // what a beam's logits, less the reference of its sum, are added to: its score
+    // without the sum's logarithm
     for (int b = tid >> 6; b < a.B; b += WAVES) {
         const float base = a.scores[request * a.B + b];
-        double value = -INFINITY;
-        float top = -INFINITY;
+        double value = -INFINITY, reference = -INFINITY;
         if (isfinite(base)) {
             for (int p = lane; p < s.parts; p += 64)
-                top = fmaxf(top, sums[b * s.parts + p].top);
+                reference = fmax(reference, sums[b * s.parts + p].reference);
 #pragma unroll
             for (int m = 32; m; m >>= 1)
-                top = fmaxf(top, __shfl_xor(top, m));
-            if (top > -INFINITY) {
+                reference = fmax(reference, __shfl_xor(reference, m));
+            if (reference > -INFINITY) {
                 double sum = 0.;
                 for (int p = lane; p < s.parts; p += 64) {
                     const PartSum q = sums[b * s.parts + p];
-                    if (q.top > -INFINITY)
-                        sum += q.sum * exp((double)q.top - (double)top);
+                    if (q.reference > -INFINITY)
+                        sum += q.sum * exp(q.reference - reference);
                 }
 #pragma unroll
                 for (int m = 32; m; m >>= 1)
@@ -299,7 +302,7 @@ __global__ void __launch_bounds__(THREADS) beam_join_kernel(sbvr_beam_args a, Be
         }
         if (lane == 0) {
             add[b] = value;
-            beam_top[b] = top;
+            beam_reference[b] = reference;
         }
     }
     if (tid < 64) {
@@ -328,7 +331,7 @@ __global__ void __launch_bounds__(THREADS) beam_join_kernel(sbvr_beam_args a, Be
         score[i] = -INFINITY;
         what[i] = (uint32_t)beam << 16 | place;
         if (key && add[beam] > -INFINITY) {
-            score[i] = add[beam] + ((double)unordered((uint32_t)(key >> 32)) - (double)beam_top[beam]);
+            score[i] = add[beam] + ((double)unordered((uint32_t)(key >> 32)) - beam_reference[beam]);
             const int token = (int)~(uint32_t)key;
             bool end = false;
             for (int e = 0; e < a.n_end; ++e)
@@ -410,17 +413,16 @@ __global__ void __launch_bounds__(THREADS) beam_join_kernel(sbvr_beam_args a, Be
 
 namespace {
 
-// pieces of a thread: large tiles where their workgroups fill the chip, and their
-// lists fit
-int beam_pieces(long long rows, int V, int keep)
+// pieces of a thread: large tiles where their workgroups fill the chip
+int beam_pieces(long long rows, int V)
 {
-    return keep <= 32 && rows * ((V + 8191ll) / 8192) >= 512 ? 4 : 1;
+    return rows * ((V + 8191ll) / 8192) >= 512 ? 4 : 1;
 }
 
 BeamShape beam_shape(int R, int B, int V, int n, int n_end)
 {
     BeamShape s;
-    const int tile = 8 * BEAM_THREADS * beam_pieces((long long)R * B, V, n + n_end);
+    const int tile = 8 * BEAM_THREADS * beam_pieces((long long)R * B, V);
     const int tiles = (V + tile - 1) / tile;
     s.keep = n + n_end;
     // (and no more workgroups than a grid can have)
@@ -442,10 +444,8 @@ int run_parts(const sbvr_beam_args &a, const BeamShape &s, PartSum *sums, uint64
     sbvr_beam_args args = a;
     BeamShape shape = s;
     void *argv[] = {&args, &shape, &sums, &entries};
-    // the entries kept, and all logits of as many groups of four lanes (at most a tile's)
-    const size_t held = (size_t)s.keep * 4 * 8 * CH, list = s.keep + held;
-    return launch_kernel((const void *)beam_part_kernel<T, CH>, dim3((unsigned)(a.R * a.B * s.parts)), dim3(BEAM_THREADS),
-                         list * sizeof(uint64_t), stream, argv);
+    return launch_kernel((const void *)beam_part_kernel<T, CH>, dim3((unsigned)(a.R * a.B * s.parts)), dim3(BEAM_THREADS), 0,
+                         stream, argv);
 }
 
 }  // namespace
@@ -461,7 +461,7 @@ int launch_beam(const sbvr_beam_args &a, void *workspace, hipStream_t stream)
     const BeamShape s = beam_shape(a.R, a.B, a.V, a.n, a.n_end);
     PartSum *sums = (PartSum *)workspace;
     uint64_t *entries = (uint64_t *)((char *)workspace + sums_bytes(a.R, a.B, s));
-    const bool large = beam_pieces((long long)a.R * a.B, a.V, s.keep) == 4;
+    const bool large = beam_pieces((long long)a.R * a.B, a.V) == 4;
     int st;
     switch (a.dtype) {
     case SBVR_F16: st = large ? run_parts<f16_t, 4>(a, s, sums, entries, stream) : run_parts<f16_t, 1>(a, s, sums, entries, stream); break;

@@ -212,6 +212,23 @@ def test_extreme_logits():
     logits[2] = 1e30
     logits[3] = torch.linspace(0, 1e-40, V, device=DEV)
     check(logits, torch.tensor([[-1.0], [-2.0], [-3.0], [-4.0]], device=DEV), 4)
+    for first, second, third in ((-1e38, 5.0, 7.0), (5.0, 1e38, -3e38), (3e38, 1.0, 3.2e38), (-3e38, -2e38, 3.0), (30.0, 2e37, 2.0)):
+        logits = torch.full((1, 3 * 2048), first, dtype=F32, device=DEV)  # by tiles of a part, where there are many rows
+        logits[:, 2048:4096], logits[:, 4096:] = second, third
+        logits += torch.arange(3 * 2048, device=DEV) % 5
+        check(logits, torch.zeros(1, 1, device=DEV), 3)
+        wide = logits.repeat_interleave(4, dim=1).expand(32, -1).contiguous()
+        check(wide, torch.zeros(1, 32, device=DEV), 3)
+
+
+def test_zeros_of_either_sign_are_equal():
+    for V in (300, 9000, 70000):
+        logits = torch.zeros(2, V, dtype=F32, device=DEV)
+        logits[:, ::2] = -0.0
+        logits[:, V // 2:] -= 1
+        check(logits, torch.zeros(1, 2, device=DEV), 10, exact=True)
+        logits[:, V // 3] = 0.25
+        check(logits, torch.zeros(1, 2, device=DEV), 10, exact=True)
 
 
 def test_ends_among_the_best():
