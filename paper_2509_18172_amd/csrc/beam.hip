@@ -45,10 +45,49 @@ __device__ __forceinline__ uint32_t ordered(float v)
 }
 __device__ __forceinline__ float unordered(uint32_t u) { return __uint_as_float(u & 0x80000000u ? u & 0x7fffffffu : ~u); }
 
+constexpr uint64_t END_ENTRY = 1ull << 31;  // cleared in an entry whose token is an end (tokens have 30 bits)
+
 // (+infinity as the largest number, and -0 as 0)
 __device__ __forceinline__ uint64_t key_of(float v, int token)
 {
     return (uint64_t)ordered(fminf(v, LARGEST) + 0.f) << 32 | (uint32_t)~token;
+}
+
+template <int CTRL, int ROWS = 0xf>
+__device__ __forceinline__ float dpp(float v, float out)
+{
+    return __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(out), __float_as_int(v), CTRL, ROWS, 0xf, false));
+}
+template <int CTRL, int ROWS = 0xf>
+__device__ __forceinline__ double dpp(double v, double out)
+{
+    const uint64_t u = __double_as_longlong(v), o = __double_as_longlong(out);
+    const uint32_t low = __builtin_amdgcn_update_dpp((uint32_t)o, (uint32_t)u, CTRL, ROWS, 0xf, false);
+    const uint32_t high = __builtin_amdgcn_update_dpp((uint32_t)(o >> 32), (uint32_t)(u >> 32), CTRL, ROWS, 0xf, false);
+    return __longlong_as_double((uint64_t)high << 32 | low);
+}
+
+// A wavefront's sum, in its last lane, and its maximum, in all.  (Row shifts by 1,
+// 2, 4 and 8, and the rows' last lanes to the rows behind.)
+__device__ __forceinline__ double sum_to_last(double v)
+{
+    v += dpp<0x111>(v, 0.);
+    v += dpp<0x112>(v, 0.);
+    v += dpp<0x114>(v, 0.);
+    v += dpp<0x118>(v, 0.);
+    v += dpp<0x142, 0xa>(v, 0.);
+    v += dpp<0x143, 0xc>(v, 0.);
+    return v;
+}
+__device__ __forceinline__ float max_of_wave(float v)
+{
+    v = fmaxf(v, dpp<0x111>(v, -INFINITY));
+    v = fmaxf(v, dpp<0x112>(v, -INFINITY));
+    v = fmaxf(v, dpp<0x114>(v, -INFINITY));
+    v = fmaxf(v, dpp<0x118>(v, -INFINITY));
+    v = fmaxf(v, dpp<0x142, 0xa>(v, -INFINITY));
+    v = fmaxf(v, dpp<0x143, 0xc>(v, -INFINITY));
+    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
 }
 
 // CH: pieces of eight logits a thread holds of a tile.
@@ -58,13 +97,15 @@ __global__ void __launch_bounds__(BEAM_THREADS) beam_part_kernel(sbvr_beam_args 
     constexpr int TILE = 8 * CH * BEAM_THREADS, WAVES = BEAM_THREADS / 64;
     __shared__ uint64_t list[SBVR_BEAM_KEEP_MAX + BEAM_LIST];  // the best so far, and what may be better
     __shared__ float group[2][64];
-    __shared__ int count, counts[2];
+    __shared__ int count, counts[2], ends[SBVR_BEAM_KEEP_MAX];
     __shared__ double wave_sum[WAVES];
     const int tid = threadIdx.x, lane = tid & 63, row = blockIdx.x / s.parts, part = blockIdx.x % s.parts;
     if (!isfinite(uniform_load(a.scores + row)))
         return;  // the join knows
     const T *in = (const T *)a.logits + row * a.logits_stride;
 
+    if (tid < a.n_end)
+        ends[tid] = a.end_tokens[tid];
     double total = 0., reference = -INFINITY;
     float top = -INFINITY, offset = 0.f;
     uint32_t floor = ordered(-LARGEST);  // what a logit has to reach: more than the keep-th best so far
@@ -112,19 +153,15 @@ __global__ void __launch_bounds__(BEAM_THREADS) beam_part_kernel(sbvr_beam_args 
                 piece_top[c] = fmaxf(piece_top[c], x[c][e]);
             best = fmaxf(best, piece_top[c]);
         }
-        float in_group = best;
-        in_group = fmaxf(in_group, __shfl_xor(in_group, 1));
-        in_group = fmaxf(in_group, __shfl_xor(in_group, 2));
+        float in_group = fmaxf(best, dpp<0xb1>(best, best));         // lanes 1 0 3 2
+        in_group = fmaxf(in_group, dpp<0x4e>(in_group, in_group));  // lanes 2 3 0 1
         float *groups = group[tile & 1];
         if ((tid & 3) == 0)
             groups[tid >> 2] = in_group;
         __syncthreads();
 
         const float mine = groups[lane];
-        float tile_top = mine;
-#pragma unroll
-        for (int m = 32; m; m >>= 1)
-            tile_top = fmaxf(tile_top, __shfl_xor(tile_top, m));
+        float tile_top = max_of_wave(mine);
         // the keep-th largest of the groups' maxima, to its leading 16 bits
         uint32_t least = 0;
 #pragma unroll
@@ -229,10 +266,15 @@ __global__ void __launch_bounds__(BEAM_THREADS) beam_part_kernel(sbvr_beam_args 
                 floor = (uint32_t)(list[s.keep - 1] >> 32) + 1;
         }
     }
-#pragma unroll
-    for (int m = 32; m; m >>= 1)
-        total += __shfl_xor(total, m);
-    if (lane == 0)
+    if (tid < s.keep) {
+        uint64_t entry = tid < have ? list[tid] : 0;
+        for (int e = 0; e < a.n_end; ++e)
+            if (entry && ends[e] == (int)~(uint32_t)entry)
+                entry &= ~END_ENTRY;  // (once: then the token is another)
+        entries[(long long)blockIdx.x * s.keep + tid] = entry;
+    }
+    total = sum_to_last(total);
+    if (lane == 63)
         wave_sum[tid >> 6] = total;
     __syncthreads();
     if (tid == 0) {
@@ -242,8 +284,6 @@ __global__ void __launch_bounds__(BEAM_THREADS) beam_part_kernel(sbvr_beam_args 
             total += wave_sum[w];
         sums[blockIdx.x] = PartSum{total, reference};
     }
-    if (tid < s.keep)
-        entries[(long long)blockIdx.x * s.keep + tid] = tid < have ? list[tid] : 0;
 }
 
 struct Candidate {
@@ -254,9 +294,18 @@ __device__ __forceinline__ bool better_than(const Candidate &a, const Candidate 
 {
     return a.score > b.score || (a.score == b.score && a.place < b.place);
 }
+template <int CTRL>
+__device__ __forceinline__ void take_better(Candidate &c)
+{
+    const Candidate other = {dpp<CTRL>(c.score, c.score),
+                             __builtin_amdgcn_update_dpp(c.place, c.place, CTRL, 0xf, 0xf, false)};
+    if (better_than(other, c))
+        c = other;
+}
 
 // One request.  Entries are in the order of beam, part and rank, so of those with
-// equal scores the lower place has the lower beam, or token.
+// equal scores the lower place has the lower beam, or token.  A chain of latencies:
+// the entries are loaded beside the sums.
 template <int THREADS>
 __global__ void __launch_bounds__(THREADS) beam_join_kernel(sbvr_beam_args a, BeamShape s, const PartSum *sums,
                                                             const uint64_t *entries)
@@ -264,8 +313,7 @@ __global__ void __launch_bounds__(THREADS) beam_join_kernel(sbvr_beam_args a, Be
     constexpr int PER = THREADS == 1024 ? BEAM_ENTRIES / 1024 : 4, WAVES = THREADS / 64;
     constexpr uint32_t END = 1u << 31;
     extern __shared__ double list_score[];  // and behind them, each entry's place, beam and whether it is an end
-    __shared__ double add[SBVR_BEAMS_MAX];
-    __shared__ double beam_reference[SBVR_BEAMS_MAX];
+    __shared__ double add[SBVR_BEAMS_MAX], beam_reference[SBVR_BEAMS_MAX];
     __shared__ Candidate group[64], least;
     __shared__ int rank[64], count;
     __shared__ float score_out[SBVR_BEAM_KEEP_MAX], ended[SBVR_BEAMS_MAX];
@@ -276,31 +324,34 @@ __global__ void __launch_bounds__(THREADS) beam_join_kernel(sbvr_beam_args a, Be
     entries += request * all;
     sums += request * a.B * s.parts;
 
+    uint64_t key[PER];
+#pragma unroll
+    for (int i = 0; i < PER; ++i)
+        key[i] = entries[min(i * THREADS + tid, all - 1)];
     // what a beam's logits, less the reference of its sum, are added to: its score
     // without the sum's logarithm
     for (int b = tid >> 6; b < a.B; b += WAVES) {
         const float base = a.scores[request * a.B + b];
+        PartSum first = {0., -INFINITY};
+        if (lane < s.parts)
+            first = sums[b * s.parts + lane];  // (of a beam that is none not written, and not used)
         double value = -INFINITY, reference = -INFINITY;
         if (isfinite(base)) {
-            for (int p = lane; p < s.parts; p += 64)
-                reference = fmax(reference, sums[b * s.parts + p].reference);
-#pragma unroll
-            for (int m = 32; m; m >>= 1)
-                reference = fmax(reference, __shfl_xor(reference, m));
-            if (reference > -INFINITY) {
-                double sum = 0.;
-                for (int p = lane; p < s.parts; p += 64) {
+            float top = (float)first.reference;
+            for (int p = lane + 64; p < s.parts; p += 64)
+                top = fmaxf(top, (float)sums[b * s.parts + p].reference);
+            top = max_of_wave(top);
+            if (top > -INFINITY) {
+                reference = top;
+                double sum = first.sum * exp(first.reference - reference);  // (0 for a part without logits)
+                for (int p = lane + 64; p < s.parts; p += 64) {
                     const PartSum q = sums[b * s.parts + p];
-                    if (q.reference > -INFINITY)
-                        sum += q.sum * exp(q.reference - reference);
+                    sum += q.sum * exp(q.reference - reference);
                 }
-#pragma unroll
-                for (int m = 32; m; m >>= 1)
-                    sum += __shfl_xor(sum, m);
-                value = (double)base - log(sum);
+                value = (double)base - log(sum_to_last(sum));
             }
         }
-        if (lane == 0) {
+        if (lane == 63) {
             add[b] = value;
             beam_reference[b] = reference;
         }
@@ -322,32 +373,24 @@ __global__ void __launch_bounds__(THREADS) beam_join_kernel(sbvr_beam_args a, Be
 
     Candidate mine = {-INFINITY, BEAM_ENTRIES};  // the thread's best that goes on
     double score[PER];
-    uint32_t what[PER];
+    int beam[PER];
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
         const int place = i * THREADS + tid;
-        const uint64_t key = place < all ? entries[place] : 0;
-        const int beam = place < all ? place / per_beam : 0;
+        beam[i] = min(place, all - 1) / per_beam;
         score[i] = -INFINITY;
-        what[i] = (uint32_t)beam << 16 | place;
-        if (key && add[beam] > -INFINITY) {
-            score[i] = add[beam] + ((double)unordered((uint32_t)(key >> 32)) - beam_reference[beam]);
-            const int token = (int)~(uint32_t)key;
-            bool end = false;
-            for (int e = 0; e < a.n_end; ++e)
-                end |= uniform_load(a.end_tokens + e) == token;
+        if (place < all && key[i] && add[beam[i]] > -INFINITY) {
+            score[i] = add[beam[i]] + ((double)unordered((uint32_t)(key[i] >> 32)) - beam_reference[beam[i]]);
             const Candidate c = {score[i], place};
-            if (end)
-                what[i] |= END;
-            else if (better_than(c, mine))
+            if ((key[i] & END_ENTRY) && better_than(c, mine))
                 mine = c;
         }
     }
-#pragma unroll
-    for (int m = 1; m < WAVES; m <<= 1) {
-        const Candidate other = {__shfl_xor(mine.score, m), __shfl_xor(mine.place, m)};
-        if (better_than(other, mine))
-            mine = other;
+    take_better<0xb1>(mine);  // lanes 1 0 3 2, 2 3 0 1 of four
+    take_better<0x4e>(mine);
+    if (WAVES == 16) {
+        take_better<0x124>(mine);  // rotations by 4 and 8 of sixteen
+        take_better<0x128>(mine);
     }
     if (tid % WAVES == 0)
         group[tid / WAVES] = mine;
@@ -366,39 +409,42 @@ __global__ void __launch_bounds__(THREADS) beam_join_kernel(sbvr_beam_args a, Be
     if (tid < 64 && group[tid].score > -INFINITY && rank[tid] == a.n - 1)
         least = group[tid];
     __syncthreads();
+    int listed[PER];
 #pragma unroll
-    for (int i = 0; i < PER; ++i)
-        if (score[i] > -INFINITY && !better_than(least, Candidate{score[i], (int)(what[i] & 0xffff)})) {
+    for (int i = 0; i < PER; ++i) {
+        const int place = i * THREADS + tid;
+        listed[i] = score[i] > -INFINITY && !better_than(least, Candidate{score[i], place});
+        if (listed[i]) {
             const int k = atomicAdd(&count, 1);
             list_score[k] = score[i];
-            list_what[k] = what[i];
-        }
-    __syncthreads();
-    const int c = count;
-    for (int i = tid; i < c; i += THREADS) {
-        const uint32_t w = list_what[i];
-        const Candidate me = {list_score[i], (int)(w & 0xffff)};
-        const int beam = (w >> 16) & 0x7fff;
-        int better = 0, going = 0, same = 0;  // all, those that go on, and ends of the beam
-        for (int j = 0; j < c; ++j) {
-            const uint32_t u = list_what[j];
-            const bool b = better_than(Candidate{list_score[j], (int)(u & 0xffff)}, me);
-            better += b;
-            going += b && !(u & END);
-            same += b && (u & END) && ((u >> 16) & 0x7fff) == beam;
-        }
-        const int token = (int)~(uint32_t)entries[me.place];
-        if (!(w & END)) {
-            if (going < a.n) {
-                token_out[going] = token;
-                parent_out[going] = beam;
-                score_out[going] = (float)me.score;
-            }
-        } else if (better < a.n && same == 0) {
-            ended[beam] = (float)me.score;
-            ended_token[beam] = token;
+            list_what[k] = (uint32_t)beam[i] << 16 | place | (key[i] & END_ENTRY ? 0 : END);
         }
     }
+    __syncthreads();
+    const int c = count;
+#pragma unroll
+    for (int i = 0; i < PER; ++i)
+        if (listed[i]) {
+            const Candidate me = {score[i], i * THREADS + tid};
+            int better = 0, going = 0, same = 0;  // all, those that go on, and ends of the beam
+            for (int j = 0; j < c; ++j) {
+                const uint32_t u = list_what[j];
+                const bool b = better_than(Candidate{list_score[j], (int)(u & 0xffff)}, me);
+                better += b;
+                going += b && !(u & END);
+                same += b && (u & END) && (int)((u >> 16) & 0x7fff) == beam[i];
+            }
+            if (key[i] & END_ENTRY) {
+                if (going < a.n) {
+                    token_out[going] = (int)~(uint32_t)key[i];
+                    parent_out[going] = beam[i];
+                    score_out[going] = (float)me.score;
+                }
+            } else if (better < a.n && same == 0) {
+                ended[beam[i]] = (float)me.score;
+                ended_token[beam[i]] = (int)~(uint32_t)(key[i] | END_ENTRY);
+            }
+        }
     __syncthreads();
     if (tid < a.n) {
         a.tokens[request * a.n + tid] = token_out[tid];
