@@ -25,7 +25,7 @@
 
 namespace sbvr {
 
-constexpr int BEAM_THREADS = 256, BEAM_ENTRIES = 4096;  // of a request's parts together
+constexpr int BEAM_THREADS = 256, BEAM_ENTRIES = 3072;  // of a request's parts together
 constexpr int BEAM_LIST = 256;                          // a tile's logits to be ranked
 constexpr float LOG2E = 1.44269502f, LARGEST = 3.402823466e38f;
 
@@ -88,6 +88,48 @@ __device__ __forceinline__ float max_of_wave(float v)
     v = fmaxf(v, dpp<0x142, 0xa>(v, -INFINITY));
     v = fmaxf(v, dpp<0x143, 0xc>(v, -INFINITY));
     return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
+}
+
+// exp(x) for x <= 0 and log(x) for a normal x, to 2^-36: the join is a chain of such
+// steps, and the sums are no better.  (Taylor's series to the 9th power behind the
+// powers of 2: the next term is 7e-12; log m = 2 artanh((m - 1) / (m + 1)) for m
+// between the roots of 1/2 and 2, to the 13th power: 5e-13.)
+__device__ __forceinline__ double exp_of(double x)
+{
+    x = fmax(x, -700.);
+    const double k = rint(x * 1.4426950408889634), r = fma(-k, 0.6931471805599453, x);
+    double p = 1. / 362880;
+    p = fma(p, r, 1. / 40320);
+    p = fma(p, r, 1. / 5040);
+    p = fma(p, r, 1. / 720);
+    p = fma(p, r, 1. / 120);
+    p = fma(p, r, 1. / 24);
+    p = fma(p, r, 1. / 6);
+    p = fma(p, r, 1. / 2);
+    p = fma(p, r, 1.);
+    p = fma(p, r, 1.);
+    return ldexp(p, (int)k);
+}
+__device__ __forceinline__ double log_of(double x)
+{
+    int e = __builtin_amdgcn_frexp_exp(x);
+    double m = __builtin_amdgcn_frexp_mant(x);
+    const bool low = m < 0.7071067811865476;
+    m = low ? 2. * m : m;
+    e -= low;
+    const double d = m + 1.;
+    double inverse = __builtin_amdgcn_rcp(d);
+    inverse = fma(fma(-d, inverse, 1.), inverse, inverse);
+    inverse = fma(fma(-d, inverse, 1.), inverse, inverse);
+    const double z = (m - 1.) * inverse, q = z * z;
+    double p = 2. / 13;
+    p = fma(p, q, 2. / 11);
+    p = fma(p, q, 2. / 9);
+    p = fma(p, q, 2. / 7);
+    p = fma(p, q, 2. / 5);
+    p = fma(p, q, 2. / 3);
+    p = fma(p, q, 2.);
+    return fma((double)e, 0.6931471805599453, p * z);
 }
 
 // CH: pieces of eight logits a thread holds of a tile.
@@ -177,7 +219,7 @@ __global__ void __launch_bounds__(BEAM_THREADS) beam_part_kernel(sbvr_beam_args 
             const bool huge = fabsf(tile_top) > 1e6f || (fabsf(top) > 1e6f && top > -INFINITY);
             if (tile_top > top) {
                 const double now = huge ? (double)tile_top : (double)(tile_top * LOG2E) / (double)LOG2E;
-                total *= reference > -INFINITY ? exp(reference - now) : 0.;
+                total *= exp_of(reference - now);  // (0 before the first)
                 reference = now;
                 offset = tile_top * LOG2E;
                 top = tile_top;
@@ -254,6 +296,7 @@ __global__ void __launch_bounds__(BEAM_THREADS) beam_part_kernel(sbvr_beam_args 
             int better = 0;
             if (tid < c) {
                 key = list[tid];
+#pragma unroll 8
                 for (int j = 0; j < c; ++j)
                     better += list[j] > key;
             }
@@ -292,17 +335,8 @@ struct Candidate {
 };
 __device__ __forceinline__ bool better_than(const Candidate &a, const Candidate &b)
 {
-    return a.score > b.score || (a.score == b.score && a.place < b.place);
+    return (a.score > b.score) | ((a.score == b.score) & (a.place < b.place));  // (no branch: LDS reads stay in flight)
 }
-template <int CTRL>
-__device__ __forceinline__ void take_better(Candidate &c)
-{
-    const Candidate other = {dpp<CTRL>(c.score, c.score),
-                             __builtin_amdgcn_update_dpp(c.place, c.place, CTRL, 0xf, 0xf, false)};
-    if (better_than(other, c))
-        c = other;
-}
-
 // One request.  Entries are in the order of beam, part and rank, so of those with
 // equal scores the lower place has the lower beam, or token.  A chain of latencies:
 // the entries are loaded beside the sums.
@@ -312,15 +346,15 @@ __global__ void __launch_bounds__(THREADS) beam_join_kernel(sbvr_beam_args a, Be
 {
     constexpr int PER = THREADS == 1024 ? BEAM_ENTRIES / 1024 : 4, WAVES = THREADS / 64;
     constexpr uint32_t END = 1u << 31;
-    extern __shared__ double list_score[];  // and behind them, each entry's place, beam and whether it is an end
+    extern __shared__ double list_score[];  // and behind them, each entry's place, beam and whether it is an end, and its token
     __shared__ double add[SBVR_BEAMS_MAX], beam_reference[SBVR_BEAMS_MAX];
-    __shared__ Candidate group[64], least;
+    __shared__ float group[64];
     __shared__ int rank[64], count;
     __shared__ float score_out[SBVR_BEAM_KEEP_MAX], ended[SBVR_BEAMS_MAX];
     __shared__ int token_out[SBVR_BEAM_KEEP_MAX], parent_out[SBVR_BEAM_KEEP_MAX], ended_token[SBVR_BEAMS_MAX];
     const int tid = threadIdx.x, lane = tid & 63, per_beam = s.parts * s.keep, all = a.B * per_beam;
     const long long request = blockIdx.x;
-    uint32_t *list_what = (uint32_t *)(list_score + all);
+    uint32_t *list_what = (uint32_t *)(list_score + all), *list_token = list_what + all;
     entries += request * all;
     sums += request * a.B * s.parts;
 
@@ -343,12 +377,12 @@ __global__ void __launch_bounds__(THREADS) beam_join_kernel(sbvr_beam_args a, Be
             top = max_of_wave(top);
             if (top > -INFINITY) {
                 reference = top;
-                double sum = first.sum * exp(first.reference - reference);  // (0 for a part without logits)
+                double sum = first.sum * exp_of(first.reference - reference);  // (0 for a part without logits)
                 for (int p = lane + 64; p < s.parts; p += 64) {
                     const PartSum q = sums[b * s.parts + p];
-                    sum += q.sum * exp(q.reference - reference);
+                    sum += q.sum * exp_of(q.reference - reference);
                 }
-                value = (double)base - log(sum_to_last(sum));
+                value = (double)base - log_of(sum_to_last(sum));
             }
         }
         if (lane == 63) {
@@ -365,86 +399,84 @@ __global__ void __launch_bounds__(THREADS) beam_join_kernel(sbvr_beam_args a, Be
         ended[tid] = -INFINITY;
         ended_token[tid] = -1;
     }
-    if (tid == 0) {
-        least = {-INFINITY, 0};
+    if (tid == 0)
         count = 0;
-    }
     __syncthreads();
 
-    Candidate mine = {-INFINITY, BEAM_ENTRIES};  // the thread's best that goes on
+    // As in a tile: the n-th largest of 64 groups' best scores that go on, here
+    // rounded to binary32, which keeps their order, leaves hardly more than the n best.
+    float mine = -INFINITY;
     double score[PER];
     int beam[PER];
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
         const int place = i * THREADS + tid;
-        beam[i] = min(place, all - 1) / per_beam;
-        score[i] = -INFINITY;
-        if (place < all && key[i] && add[beam[i]] > -INFINITY) {
-            score[i] = add[beam[i]] + ((double)unordered((uint32_t)(key[i] >> 32)) - beam_reference[beam[i]]);
-            const Candidate c = {score[i], place};
-            if ((key[i] & END_ENTRY) && better_than(c, mine))
-                mine = c;
-        }
+        beam[i] = small_div(min(place, all - 1), per_beam, 1.f / (float)per_beam);
+        // (the score of a beam that is none is -infinity)
+        const double value = add[beam[i]] + ((double)unordered((uint32_t)(key[i] >> 32)) - beam_reference[beam[i]]);
+        score[i] = (place < all) & (key[i] != 0) & (add[beam[i]] > -INFINITY) ? value : -INFINITY;
+        mine = fmaxf(mine, key[i] & END_ENTRY ? (float)score[i] : -INFINITY);
     }
-    take_better<0xb1>(mine);  // lanes 1 0 3 2, 2 3 0 1 of four
-    take_better<0x4e>(mine);
+    mine = fmaxf(mine, dpp<0xb1>(mine, mine));  // lanes 1 0 3 2, 2 3 0 1 of four
+    mine = fmaxf(mine, dpp<0x4e>(mine, mine));
     if (WAVES == 16) {
-        take_better<0x124>(mine);  // rotations by 4 and 8 of sixteen
-        take_better<0x128>(mine);
+        mine = fmaxf(mine, dpp<0x124>(mine, mine));  // rotations by 4 and 8 of sixteen
+        mine = fmaxf(mine, dpp<0x128>(mine, mine));
     }
     if (tid % WAVES == 0)
         group[tid / WAVES] = mine;
     __syncthreads();
-    {
-        const Candidate g = group[lane];
-        int better = 0;
+    mine = group[lane];
+    int above = 0;
 #pragma unroll
-        for (int j = 0; j < 64 / WAVES; ++j)
-            better += better_than(group[(tid >> 6) * (64 / WAVES) + j], g);
-        if (better)
-            atomicAdd(&rank[lane], better);
-    }
+    for (int j = 0; j < 64 / WAVES; ++j)
+        above += group[(tid >> 6) * (64 / WAVES) + j] > mine;
+    if (above)
+        atomicAdd(&rank[lane], above);
     __syncthreads();
-    // what is worse than the n-th best group has n better ones that go on
-    if (tid < 64 && group[tid].score > -INFINITY && rank[tid] == a.n - 1)
-        least = group[tid];
-    __syncthreads();
-    int listed[PER];
+    const float least = -max_of_wave(rank[lane] < a.n ? -mine : -INFINITY);
+    int listed[PER], mine_listed = 0;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-        const int place = i * THREADS + tid;
-        listed[i] = score[i] > -INFINITY && !better_than(least, Candidate{score[i], place});
-        if (listed[i]) {
-            const int k = atomicAdd(&count, 1);
-            list_score[k] = score[i];
-            list_what[k] = (uint32_t)beam[i] << 16 | place | (key[i] & END_ENTRY ? 0 : END);
-        }
+        listed[i] = (score[i] > -INFINITY) & ((float)score[i] >= least);
+        mine_listed += listed[i];
+    }
+    if (mine_listed) {
+        int k = atomicAdd(&count, mine_listed);
+#pragma unroll
+        for (int i = 0; i < PER; ++i)
+            if (listed[i]) {
+                list_score[k] = score[i];
+                list_what[k] = (uint32_t)beam[i] << 16 | (i * THREADS + tid) | (key[i] & END_ENTRY ? 0 : END);
+                list_token[k++] = ~(uint32_t)(key[i] | END_ENTRY);
+            }
     }
     __syncthreads();
     const int c = count;
-#pragma unroll
-    for (int i = 0; i < PER; ++i)
-        if (listed[i]) {
-            const Candidate me = {score[i], i * THREADS + tid};
-            int better = 0, going = 0, same = 0;  // all, those that go on, and ends of the beam
-            for (int j = 0; j < c; ++j) {
-                const uint32_t u = list_what[j];
-                const bool b = better_than(Candidate{list_score[j], (int)(u & 0xffff)}, me);
-                better += b;
-                going += b && !(u & END);
-                same += b && (u & END) && (int)((u >> 16) & 0x7fff) == beam[i];
-            }
-            if (key[i] & END_ENTRY) {
-                if (going < a.n) {
-                    token_out[going] = (int)~(uint32_t)key[i];
-                    parent_out[going] = beam[i];
-                    score_out[going] = (float)me.score;
-                }
-            } else if (better < a.n && same == 0) {
-                ended[beam[i]] = (float)me.score;
-                ended_token[beam[i]] = (int)~(uint32_t)(key[i] | END_ENTRY);
-            }
+    for (int i = tid; i < c; i += THREADS) {
+        const uint32_t w = list_what[i];
+        const Candidate me = {list_score[i], (int)(w & 0xffff)};
+        const uint32_t beam = (w >> 16) & 0x7fff;
+        int better = 0, going = 0, same = 0;  // all, those that go on, and ends of the beam
+#pragma unroll 4
+        for (int j = 0; j < c; ++j) {
+            const uint32_t u = list_what[j];
+            const int b = better_than(Candidate{list_score[j], (int)(u & 0xffff)}, me), end = u >> 31;
+            better += b;
+            going += b & ~end;
+            same += b & end & (int)(((u >> 16) & 0x7fff) == beam);
         }
+        if (!(w & END)) {
+            if (going < a.n) {
+                token_out[going] = (int)list_token[i];
+                parent_out[going] = beam;
+                score_out[going] = (float)me.score;
+            }
+        } else if (better < a.n && same == 0) {
+            ended[beam] = (float)me.score;
+            ended_token[beam] = (int)list_token[i];
+        }
+    }
     __syncthreads();
     if (tid < a.n) {
         a.tokens[request * a.n + tid] = token_out[tid];
@@ -522,7 +554,7 @@ int launch_beam(const sbvr_beam_args &a, void *workspace, hipStream_t stream)
     const uint64_t *entries_in = entries;
     void *argv[] = {&args, &shape, &sums_in, &entries_in};
     const int all = a.B * s.parts * s.keep;
-    const size_t lds = (size_t)all * (sizeof(double) + sizeof(uint32_t));
+    const size_t lds = (size_t)all * (sizeof(double) + 2 * sizeof(uint32_t));
     return all <= 1024 ? launch_kernel((const void *)beam_join_kernel<256>, dim3(a.R), dim3(256), lds, stream, argv)
                        : launch_kernel((const void *)beam_join_kernel<1024>, dim3(a.R), dim3(1024), lds, stream, argv);
 }

@@ -24,15 +24,6 @@ struct RotaryShape {
     int width;                   // pairs rounded up to pieces
 };
 
-// i / d for 0 <= i < 2^24
-__device__ __forceinline__ int small_div(int i, int d, float inverse)
-{
-    int q = (int)((float)i * inverse);
-    q -= q * d > i;
-    q += (q + 1) * d <= i;
-    return q;
-}
-
 // T: element type; EVEN: every piece is whole (pairs a multiple of 8); WRITE: keys
 // and values go into the cache.
 template <typename T, bool EVEN, bool WRITE>

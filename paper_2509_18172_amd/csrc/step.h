@@ -171,6 +171,15 @@ int launch_compact(const CompactArgs &a, hipStream_t stream);
 int launch_page_copy(const sbvr_kv_cache *caches, int n_caches, int n, const int32_t *src, const int32_t *dst,
                      const int32_t *tokens, hipStream_t stream);
 
+// i / d for 0 <= i < 2^24
+__device__ __forceinline__ int small_div(int i, int d, float inverse)
+{
+    int q = (int)((float)i * inverse);
+    q -= q * d > i;
+    q += (q + 1) * d <= i;
+    return q;
+}
+
 // The last index i of the ascending start[0 .. n] with start[i] <= v, for
 // start[0] <= v < start[n]: the owner of item v, empty owners skipped.
 template <typename I>
