@@ -392,7 +392,7 @@ int sbvr_page_usage(int R, int page_size, int n_pages, const int32_t *context_le
         !aligned(counts, 4) || !aligned(workspace, 16))
         return SBVR_E_ALIGNMENT;
     const PageTable t{R, __builtin_ctz(page_size), max_pages, context_lens, page_table, table_stride};
-    return launch_usage(UsageArgs{t, n_pages, refs, free_pages, counts, (uint32_t *)workspace}, stream);
+    return launch_usage(UsageArgs{t, n_pages, refs, free_pages, counts, (int32_t *)workspace}, stream);
 }
 
 int sbvr_page_fork(int groups, int rows_in, int rows_out, int page_size, const int32_t *context_lens,
@@ -448,9 +448,8 @@ int sbvr_page_compact(int R, int page_size, int n_pages, const int32_t *context_
     if (!aligned(workspace, 16))
         return SBVR_E_ALIGNMENT;
     const PageTable t{R, __builtin_ctz(page_size), max_pages, context_lens, page_table, table_stride};
-    const CompactArgs a{t, n_pages, out_table, out_stride, src, dst, counts, (uint32_t *)workspace,
-                        (int32_t *)((char *)workspace + usage_workspace_bytes(n_pages))};
-    return launch_compact(a, stream);
+    return launch_compact(CompactArgs{t, n_pages, out_table, out_stride, src, dst, counts, (uint32_t *)workspace, nullptr},
+                          stream);
 }
 
 int sbvr_page_copy(const sbvr_kv_cache *caches, int n_caches, int n, const int32_t *src, const int32_t *dst,

@@ -45,113 +45,164 @@ __device__ __forceinline__ int sum_before(int v, int &all, int *scratch)
 // use of pages
 // ---------------------------------------------------------------------------
 
-constexpr int PAGE_THREADS = 1024;
+constexpr int PAGE_THREADS = 1024, PAGE_WAVES = PAGE_THREADS / 64;
 
-// Words of marks, a bit per page; the launches below read whole ones.
-__host__ __device__ constexpr int mark_words(int n_pages) { return (n_pages + 31) / 32; }
-
-__global__ void __launch_bounds__(256) clear_kernel(uint32_t *p, int n, uint32_t *q, int m)
+__device__ __forceinline__ int lanes_before(uint64_t mask)
 {
-    const int i = blockIdx.x * 256 + threadIdx.x;
-    if (i < n)
-        p[i] = 0;
-    if (i < m)
-        q[i] = 0;
+    return __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0));
 }
 
-// A wavefront per 256 entries of a row: marks their pages, and counts them where
-// refs is given.
-__global__ void __launch_bounds__(256) mark_kernel(PageTable t, int n_pages, uint32_t *marks, int32_t *refs, int pieces)
+// Calls f(page) for every entry in use, and f(-1) beside, by a workgroup of
+// PAGE_THREADS: a wavefront takes eight rows at a time, 128 entries of each in flight.
+template <typename F>
+__device__ __forceinline__ void each_page(const PageTable &t, F f)
 {
-    const long long items = (long long)t.R * pieces;
-    for (long long item = (long long)blockIdx.x * 4 + (threadIdx.x >> 6); item < items; item += (long long)gridDim.x * 4) {
-        const int r = (int)(item / pieces), e0 = (int)(item % pieces) * 256 + (threadIdx.x & 63);
-        const int used = entries_in_use(t.context_lens[r], t);
+    constexpr int ROWS = 8, LOADS = 2;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    for (int r0 = wave * ROWS; r0 < t.R; r0 += PAGE_THREADS) {
+        // the lengths of the wavefront's next 64 rows
+        const int row = r0 + lane / ROWS * (PAGE_WAVES * ROWS) + lane % ROWS;
+        const int used_by = row < t.R ? entries_in_use(t.context_lens[row], t) : 0;
+        for (int i = 0; i < 64; i += ROWS) {
+            int used[ROWS], most = 0;
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            const int e = e0 + 64 * u;
-            const int page = e < used ? t.page_table[r * t.table_stride + e] : -1;
-            if (page >= 0 && page < n_pages) {
-                if (!refs || atomicAdd(&refs[page], 1) == 0)
-                    atomicOr(&marks[page >> 5], 1u << (page & 31));
+            for (int u = 0; u < ROWS; ++u) {
+                used[u] = __builtin_amdgcn_readlane(used_by, i + u);
+                most = max(most, used[u]);
+            }
+            const int32_t *table = t.page_table + (long long)(r0 + i * PAGE_WAVES) * t.table_stride;
+            for (int e0 = lane; e0 - lane < most; e0 += 64 * LOADS) {
+                int page[ROWS][LOADS];
+#pragma unroll
+                for (int u = 0; u < ROWS; ++u)
+#pragma unroll
+                    for (int k = 0; k < LOADS; ++k) {
+                        const int e = e0 + 64 * k;
+                        page[u][k] = e < used[u] ? table[u * t.table_stride + e] : -1;
+                    }
+#pragma unroll
+                for (int u = 0; u < ROWS; ++u)
+#pragma unroll
+                    for (int k = 0; k < LOADS; ++k)
+                        f(page[u][k]);
             }
         }
     }
 }
 
-// Pages marked before `page`, by the whole workgroup.
-__device__ __forceinline__ int marked_before(const uint32_t *marks, int page, int *scratch)
+// A workgroup owns USAGE_PAGES pages, whose counts it holds in LDS: it goes through
+// all entries in use and counts its own.  (Counting in memory, by atomic additions
+// that cross the chip's L2s, took 40 us for 262144 entries.)  With one workgroup that
+// is all; else a second launch makes the list of free pages, where each workgroup
+// adds up the used pages before its own.
+constexpr int USAGE_PAGES = 12288;
+
+// The list of free pages from counts in LDS or memory, by a workgroup with the pages
+// first .. first + n, `before` of the lower ones used and `total` of all.
+__device__ __forceinline__ void list_free(const UsageArgs &a, const int *count, int first, int n, int before, int total,
+                                          int *used_by_wave)
 {
-    int n = 0, all;
-    for (int w = threadIdx.x; w < page / 32; w += PAGE_THREADS)
-        n += __popc(marks[w]);
-    if (threadIdx.x == 0 && (page & 31))
-        n += __popc(marks[page / 32] & ((1u << (page & 31)) - 1));
-    sum_before<PAGE_THREADS>(n, all, scratch);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int share = (n + PAGE_THREADS - 1) / PAGE_THREADS * 64, i0 = wave * share, i1 = min(i0 + share, n);
+    int used = before;
+    for (int w = 0; w < wave; ++w)
+        used += used_by_wave[w];
+    for (int i = i0; i < i1; i += 64) {
+        const bool in = i + lane < i1;
+        const bool here = in && count[i + lane] > 0;
+        const uint64_t marks = __ballot(here);
+        const int p = first + i + lane;
+        if (in && !here)
+            a.free_pages[p - (used + lanes_before(marks))] = p;
+        if (in && p >= a.n_pages - total)
+            a.free_pages[p] = -1;
+        used += __popcll(marks);
+    }
+}
+
+// Used pages of each wavefront's share of counts, to used_by_wave; returns their sum.
+__device__ __forceinline__ int count_used(const int *count, int n, int *used_by_wave)
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int share = (n + PAGE_THREADS - 1) / PAGE_THREADS * 64, i0 = wave * share, i1 = min(i0 + share, n);
+    int used = 0;
+    for (int i = i0; i < i1; i += 64)
+        used += __popcll(__ballot(i + lane < i1 && count[min(i + lane, i1 - 1)] > 0));
+    if (lane == 0)
+        used_by_wave[wave] = used;
+    __syncthreads();
+    int all = 0;
+#pragma unroll
+    for (int w = 0; w < PAGE_WAVES; ++w)
+        all += used_by_wave[w];
     return all;
 }
 
-// The free pages in order, a word of marks a thread.
-__global__ void __launch_bounds__(PAGE_THREADS) free_kernel(UsageArgs a)
+__global__ void __launch_bounds__(PAGE_THREADS) usage_kernel(UsageArgs a)
 {
-    __shared__ int scratch[PAGE_THREADS / 64];
-    const int words = mark_words(a.n_pages), first = blockIdx.x * PAGE_THREADS;
-    const int before = marked_before(a.marks, min(first * 32, a.n_pages), scratch);
-    const int total = marked_before(a.marks, a.n_pages, scratch);
-    const int w = first + (int)threadIdx.x, p0 = w * 32;
-    const uint32_t mark = w < words ? a.marks[w] : ~0u;
-    int here;
-    int used = before + sum_before<PAGE_THREADS>(w < words ? __popc(mark) : 0, here, scratch);
-    for (int i = 0; i < 32 && p0 + i < a.n_pages; ++i) {
-        const int p = p0 + i;
-        if ((mark >> i) & 1)
-            ++used;
-        else
-            a.free_pages[p - used] = p;
-        if (p >= a.n_pages - total)
-            a.free_pages[p] = -1;
-    }
-    if (blockIdx.x == 0 && threadIdx.x == 0) {
-        a.counts[0] = a.n_pages - total;
-        a.counts[1] = total;
+    __shared__ int count[USAGE_PAGES], used_by_wave[PAGE_WAVES];
+    const int first = blockIdx.x * USAGE_PAGES, n = min(USAGE_PAGES, a.n_pages - first);
+    for (int i = threadIdx.x; i < n; i += PAGE_THREADS)
+        count[i] = 0;
+    __syncthreads();
+    each_page(a.t, [&](int page) {
+        const uint32_t own = (uint32_t)page - (uint32_t)first;
+        if (own < (uint32_t)n)
+            atomicAdd(&count[own], 1);
+    });
+    __syncthreads();
+    for (int i = threadIdx.x; i < n; i += PAGE_THREADS)
+        a.refs[first + i] = count[i];
+    const int used = count_used(count, n, used_by_wave);
+    if (gridDim.x == 1) {
+        list_free(a, count, first, n, 0, used, used_by_wave);
+        if (threadIdx.x == 0) {
+            a.counts[0] = a.n_pages - used;
+            a.counts[1] = used;
+        }
+    } else if (threadIdx.x == 0) {
+        a.used[blockIdx.x] = used;
     }
 }
 
-size_t usage_workspace_bytes(int n_pages) { return ((size_t)mark_words(n_pages) * 4 + 15) / 16 * 16; }
+__global__ void __launch_bounds__(PAGE_THREADS) free_kernel(UsageArgs a)
+{
+    __shared__ int used_by_wave[PAGE_WAVES], scratch[PAGE_WAVES];
+    const int first = blockIdx.x * USAGE_PAGES, n = min(USAGE_PAGES, a.n_pages - first), groups = gridDim.x;
+    int before = 0, all = 0, sum;
+    for (int w = threadIdx.x; w < groups; w += PAGE_THREADS) {
+        all += a.used[w];
+        before += w < (int)blockIdx.x ? a.used[w] : 0;
+    }
+    sum_before<PAGE_THREADS>(all, sum, scratch);
+    all = sum;
+    sum_before<PAGE_THREADS>(before, sum, scratch);
+    before = sum;
+    count_used(a.refs + first, n, used_by_wave);
+    list_free(a, a.refs + first, first, n, before, all, used_by_wave);
+    if (blockIdx.x == 0 && threadIdx.x == 0) {
+        a.counts[0] = a.n_pages - all;
+        a.counts[1] = all;
+    }
+}
 
 namespace {
 
-// workgroups of a launch whose items may be more than a grid can be
-unsigned capped(long long n) { return (unsigned)(n < (1 << 20) ? n : 1 << 20); }
-
-int run_mark(const PageTable &t, int n_pages, uint32_t *marks, int32_t *refs, hipStream_t stream)
-{
-    int words = mark_words(n_pages), n = refs ? n_pages : 0;
-    uint32_t *counts = (uint32_t *)refs;
-    void *clear[] = {&marks, &words, &counts, &n};
-    const int most = n > words ? n : words;
-    int st = launch_kernel((const void *)clear_kernel, dim3((most + 255) / 256), dim3(256), 0, stream, clear);
-    if (st != SBVR_OK || t.R == 0)
-        return st;
-    PageTable table = t;
-    int pieces = (t.max_pages + 255) / 256;
-    const long long items = (long long)t.R * pieces;
-    void *mark[] = {&table, &n_pages, &marks, &refs, &pieces};
-    return launch_kernel((const void *)mark_kernel, dim3(capped((items + 3) / 4)), dim3(256), 0, stream, mark);
-}
-
-int mark_groups(int n_pages) { return (mark_words(n_pages) + PAGE_THREADS - 1) / PAGE_THREADS; }
+int usage_groups(int n_pages) { return (n_pages + USAGE_PAGES - 1) / USAGE_PAGES; }
 
 }  // namespace
 
+size_t usage_workspace_bytes(int n_pages) { return ((size_t)usage_groups(n_pages) * sizeof(int32_t) + 15) / 16 * 16; }
+
 int launch_usage(const UsageArgs &a, hipStream_t stream)
 {
-    const int st = run_mark(a.t, a.n_pages, a.marks, a.refs, stream);
-    if (st != SBVR_OK)
-        return st;
     UsageArgs args = a;
     void *argv[] = {&args};
-    return launch_kernel((const void *)free_kernel, dim3(mark_groups(a.n_pages)), dim3(PAGE_THREADS), 0, stream, argv);
+    const dim3 grid(usage_groups(a.n_pages));
+    const int st = launch_kernel((const void *)usage_kernel, grid, dim3(PAGE_THREADS), 0, stream, argv);
+    if (st != SBVR_OK || grid.x == 1)
+        return st;
+    return launch_kernel((const void *)free_kernel, grid, dim3(PAGE_THREADS), 0, stream, argv);
 }
 
 // ---------------------------------------------------------------------------
@@ -252,11 +303,141 @@ int launch_fork(const ForkArgs &a, hipStream_t stream)
 // compaction
 // ---------------------------------------------------------------------------
 
-// The k-th free page below the number of used ones is dst[k], the k-th used page from
-// there on src[k]; number[p] = k for the latter.
+// Words of marks, a bit per page.
+__host__ __device__ constexpr int mark_words(int n_pages) { return (n_pages + 31) / 32; }
+
+// The new number of an entry's page: the used pages that stay keep theirs.
+__device__ __forceinline__ int renumbered(const CompactArgs &a, int page, int used)
+{
+    if (page < 0 || page >= a.n_pages)
+        return -1;
+    return page < used ? page : a.dst[a.number[page]];
+}
+
+// (A wavefront per 64 entries of a row; at most 4096 rows of 2^22.)
+__device__ __forceinline__ void renumber_entries(const CompactArgs &a, int used, int first, int step)
+{
+    const PageTable &t = a.t;
+    const int pieces = (t.max_pages + 63) / 64, items = t.R * pieces;
+    for (int item = first; item < items; item += step) {
+        const int r = item / pieces, e = (item - r * pieces) * 64 + (threadIdx.x & 63);
+        if (e >= t.max_pages)
+            continue;
+        const int page = e < entries_in_use(t.context_lens[r], t) ? t.page_table[r * t.table_stride + e] : -1;
+        a.out_table[r * a.out_stride + e] = renumbered(a, page, used);
+    }
+}
+
+// Few pages and entries: one workgroup marks the used pages in LDS, finds the moves
+// -- the k-th free page below the number of used ones is dst[k], the k-th used page
+// from there on src[k], and number[p] = k for that -- and, if `whole`, rewrites the
+// tables too.
+#ifndef COMPACT_ENTRIES
+#define COMPACT_ENTRIES 262144
+#endif
+#ifndef COMPACT_WHOLE
+#define COMPACT_WHOLE 16384
+#endif
+constexpr int COMPACT_PAGES = 131072;
+
+__global__ void __launch_bounds__(PAGE_THREADS) compact_kernel(CompactArgs a, int whole)
+{
+    __shared__ uint32_t marks[COMPACT_PAGES / 32];
+    __shared__ int used_before[COMPACT_PAGES / 32];  // of each word
+    __shared__ int scratch[PAGE_WAVES], stays;
+    const int tid = threadIdx.x, words = mark_words(a.n_pages), lists = a.n_pages / 2;
+    for (int w = tid; w < words; w += PAGE_THREADS)
+        marks[w] = 0;
+    __syncthreads();
+    each_page(a.t, [&](int page) {
+        if ((uint32_t)page < (uint32_t)a.n_pages)
+            atomicOr(&marks[page >> 5], 1u << (page & 31));
+    });
+    __syncthreads();
+    constexpr int PER = COMPACT_PAGES / 32 / PAGE_THREADS;
+    int own = 0, total;
+#pragma unroll
+    for (int i = 0; i < PER; ++i)
+        own += tid * PER + i < words ? __popc(marks[tid * PER + i]) : 0;
+    int before = sum_before<PAGE_THREADS>(own, total, scratch);
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const int w = tid * PER + i;
+        if (w < words) {
+            used_before[w] = before;
+            if (w == total >> 5)
+                stays = before + __popc(marks[w] & ((1u << (total & 31)) - 1));
+            before += __popc(marks[w]);
+        }
+    }
+    if (tid == 0 && total == 32 * words)
+        stays = total;
+    __syncthreads();
+    const int moved = total - stays;
+    for (int p = tid; p < a.n_pages; p += PAGE_THREADS) {
+        const uint32_t mark = marks[p >> 5];
+        const int used = used_before[p >> 5] + __popc(mark & ((1u << (p & 31)) - 1));
+        const bool in_use = (mark >> (p & 31)) & 1;
+        if (in_use && p >= total) {
+            a.number[p] = used - stays;
+            a.src[used - stays] = p;
+        } else if (!in_use && p < total) {
+            a.dst[p - used] = p;
+        }
+        if (p >= moved && p < lists)
+            a.src[p] = a.dst[p] = -1;
+    }
+    if (tid == 0) {
+        a.counts[0] = total;
+        a.counts[1] = moved;
+    }
+    if (whole) {
+        __syncthreads();
+        renumber_entries(a, total, tid >> 6, PAGE_WAVES);
+    }
+}
+
+// Many: the same in launches of many workgroups, with the marks in memory.
+__global__ void __launch_bounds__(256) clear_kernel(uint32_t *marks, int words)
+{
+    const int i = blockIdx.x * 256 + threadIdx.x;
+    if (i < words)
+        marks[i] = 0;
+}
+
+__global__ void __launch_bounds__(256) mark_kernel(CompactArgs a)
+{
+    const PageTable &t = a.t;
+    const int pieces = (t.max_pages + 255) / 256;
+    const long long items = (long long)t.R * pieces;
+    for (long long item = (long long)blockIdx.x * 4 + (threadIdx.x >> 6); item < items; item += (long long)gridDim.x * 4) {
+        const int r = (int)(item / pieces), e0 = (int)(item % pieces) * 256 + (threadIdx.x & 63);
+        const int used = entries_in_use(t.context_lens[r], t);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int e = e0 + 64 * u;
+            const int page = e < used ? t.page_table[r * t.table_stride + e] : -1;
+            if (page >= 0 && page < a.n_pages)
+                atomicOr(&a.marks[page >> 5], 1u << (page & 31));
+        }
+    }
+}
+
+// Pages marked before `page`, by the whole workgroup.
+__device__ __forceinline__ int marked_before(const uint32_t *marks, int page, int *scratch)
+{
+    int n = 0, all;
+    for (int w = threadIdx.x; w < page / 32; w += PAGE_THREADS)
+        n += __popc(marks[w]);
+    if (threadIdx.x == 0 && (page & 31))
+        n += __popc(marks[page / 32] & ((1u << (page & 31)) - 1));
+    sum_before<PAGE_THREADS>(n, all, scratch);
+    return all;
+}
+
 __global__ void __launch_bounds__(PAGE_THREADS) moves_kernel(CompactArgs a)
 {
-    __shared__ int scratch[PAGE_THREADS / 64];
+    __shared__ int scratch[PAGE_WAVES];
     const int words = mark_words(a.n_pages), first = blockIdx.x * PAGE_THREADS;
     const int total = marked_before(a.marks, a.n_pages, scratch);
     const int low = marked_before(a.marks, total, scratch);  // those that stay
@@ -285,39 +466,51 @@ __global__ void __launch_bounds__(PAGE_THREADS) moves_kernel(CompactArgs a)
     }
 }
 
-__global__ void __launch_bounds__(256) renumber_kernel(CompactArgs a, int pieces)
+__global__ void __launch_bounds__(256) renumber_kernel(CompactArgs a)
 {
-    const PageTable &t = a.t;
-    const long long items = (long long)t.R * pieces;
-    for (long long item = blockIdx.x; item < items; item += gridDim.x) {
-        const int r = (int)(item / pieces), e = (int)(item % pieces) * 256 + threadIdx.x;
-        if (e >= t.max_pages)
-            continue;
-        int page = e < entries_in_use(t.context_lens[r], t) ? t.page_table[r * t.table_stride + e] : -1;
-        if (page < 0 || page >= a.n_pages)
-            page = -1;
-        else if (page >= a.counts[0])
-            page = a.dst[a.number[page]];
-        a.out_table[r * a.out_stride + e] = page;
-    }
+    renumber_entries(a, a.counts[0], blockIdx.x * 4 + (threadIdx.x >> 6), gridDim.x * 4);
 }
 
-size_t compact_workspace_bytes(int n_pages) { return usage_workspace_bytes(n_pages) + (size_t)n_pages * sizeof(int32_t); }
+size_t compact_workspace_bytes(int n_pages)
+{
+    return ((size_t)mark_words(n_pages) * sizeof(uint32_t) + 15) / 16 * 16 + (size_t)n_pages * sizeof(int32_t);
+}
+
+namespace {
+
+// workgroups of a launch whose items may be more than a grid can be
+unsigned capped(long long n) { return (unsigned)(n < (1 << 20) ? n : 1 << 20); }
+
+}  // namespace
 
 int launch_compact(const CompactArgs &a, hipStream_t stream)
 {
-    int st = run_mark(a.t, a.n_pages, a.marks, nullptr, stream);
-    if (st != SBVR_OK)
-        return st;
     CompactArgs args = a;
-    void *moves[] = {&args};
-    st = launch_kernel((const void *)moves_kernel, dim3(mark_groups(a.n_pages)), dim3(PAGE_THREADS), 0, stream, moves);
-    if (st != SBVR_OK || a.t.R == 0)
-        return st;
-    int pieces = (a.t.max_pages + 255) / 256;
-    void *renumber[] = {&args, &pieces};
-    return launch_kernel((const void *)renumber_kernel, dim3(capped((long long)a.t.R * pieces)), dim3(256), 0, stream,
-                         renumber);
+    args.number = (int32_t *)((char *)a.marks + ((size_t)mark_words(a.n_pages) * sizeof(uint32_t) + 15) / 16 * 16);
+    void *argv[] = {&args};
+    const long long entries = (long long)a.t.R * a.t.max_pages;
+    int st;
+    if (a.n_pages <= COMPACT_PAGES && entries <= COMPACT_ENTRIES) {
+        int whole = entries <= COMPACT_WHOLE;
+        void *one[] = {&args, &whole};
+        st = launch_kernel((const void *)compact_kernel, dim3(1), dim3(PAGE_THREADS), 0, stream, one);
+        if (st != SBVR_OK || whole)
+            return st;
+    } else {
+        int words = mark_words(a.n_pages);
+        void *clear[] = {&args.marks, &words};
+        st = launch_kernel((const void *)clear_kernel, dim3((words + 255) / 256), dim3(256), 0, stream, clear);
+        if (st == SBVR_OK && a.t.R)
+            st = launch_kernel((const void *)mark_kernel, dim3(capped(((long long)a.t.R * ((a.t.max_pages + 255) / 256) + 3) / 4)),
+                               dim3(256), 0, stream, argv);
+        if (st == SBVR_OK)
+            st = launch_kernel((const void *)moves_kernel, dim3((words + PAGE_THREADS - 1) / PAGE_THREADS),
+                               dim3(PAGE_THREADS), 0, stream, argv);
+        if (st != SBVR_OK || a.t.R == 0)
+            return st;
+    }
+    return launch_kernel((const void *)renumber_kernel, dim3(capped(((long long)a.t.R * ((a.t.max_pages + 63) / 64) + 3) / 4)),
+                         dim3(256), 0, stream, argv);
 }
 
 // ---------------------------------------------------------------------------

@@ -130,7 +130,7 @@ struct UsageArgs {
     PageTable t;
     int n_pages;
     int32_t *refs, *free_pages, *counts;
-    uint32_t *marks;  // the workspace: a bit per page
+    int32_t *used;  // the workspace: used pages of each workgroup's
 };
 
 struct ForkArgs {
@@ -148,8 +148,8 @@ struct CompactArgs {
     int32_t *out_table;
     int64_t out_stride;
     int32_t *src, *dst, *counts;
-    uint32_t *marks;  // the workspace: a bit per page, and behind them
-    int32_t *number;  // the number of the move of a page that moves
+    uint32_t *marks;  // the workspace: a bit per page, and behind them, set by the
+    int32_t *number;  // launcher, the number of the move of a page that moves
 };
 
 int launch_plan(const PlanArgs &a, hipStream_t stream);
