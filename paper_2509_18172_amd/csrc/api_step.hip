@@ -373,7 +373,7 @@ int sbvr_beam_select(const sbvr_beam_args *a, void *workspace, size_t ws_bytes, 
 size_t sbvr_page_usage_workspace_bytes(int R, int max_pages, int n_pages)
 {
     return check_table_shape(R, max_pages, max_pages, 16) == SBVR_OK && check_pool(n_pages) == SBVR_OK
-               ? usage_workspace_bytes(n_pages)
+               ? usage_workspace_bytes(R, max_pages, n_pages)
                : 0;
 }
 
@@ -386,13 +386,13 @@ int sbvr_page_usage(int R, int page_size, int n_pages, const int32_t *context_le
         return st;
     if ((R && (!context_lens || !page_table)) || !refs || !free_pages || !counts)
         return SBVR_E_INVALID_ARG;
-    if (ws_bytes < usage_workspace_bytes(n_pages) || !workspace)
+    if (ws_bytes < usage_workspace_bytes(R, max_pages, n_pages) || !workspace)
         return SBVR_E_WORKSPACE;
     if (!aligned(context_lens, 4) || !aligned(page_table, 4) || !aligned(refs, 4) || !aligned(free_pages, 4) ||
         !aligned(counts, 4) || !aligned(workspace, 16))
         return SBVR_E_ALIGNMENT;
     const PageTable t{R, __builtin_ctz(page_size), max_pages, context_lens, page_table, table_stride};
-    return launch_usage(UsageArgs{t, n_pages, refs, free_pages, counts, (int32_t *)workspace}, stream);
+    return launch_usage(UsageArgs{t, n_pages, refs, free_pages, counts, (int32_t *)workspace, nullptr}, stream);
 }
 
 int sbvr_page_fork(int groups, int rows_in, int rows_out, int page_size, const int32_t *context_lens,

@@ -16,17 +16,24 @@ __device__ __forceinline__ int entries_in_use(int length, const PageTable &t)
     return (int)min(n, (long long)t.max_pages);
 }
 
+// Inclusive scan over a wavefront's lanes: row shifts by 1, 2, 4 and 8, and the rows'
+// last lanes to the rows behind.
+__device__ __forceinline__ int scan_of_wave(int v)
+{
+    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);
+    return v;
+}
+
 // Sum of v over the workgroup's threads before this one, and over all of them.
 template <int THREADS>
 __device__ __forceinline__ int sum_before(int v, int &all, int *scratch)
 {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    int up = v;
-#pragma unroll
-    for (int m = 1; m < 64; m <<= 1) {
-        const int other = __shfl_up(up, m);
-        up += lane >= m ? other : 0;
-    }
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, up = scan_of_wave(v);
     __syncthreads();
     if (lane == 63)
         scratch[wave] = up;
@@ -52,64 +59,93 @@ __device__ __forceinline__ int lanes_before(uint64_t mask)
     return __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0));
 }
 
-// Calls f(page) for every entry in use, and f(-1) beside, by a workgroup of
-// PAGE_THREADS: a wavefront takes eight rows at a time, 128 entries of each in flight.
-template <typename F>
-__device__ __forceinline__ void each_page(const PageTable &t, F f)
+// Calls f(page) for every entry in use, and f(-1) beside, of one of `splits` parts, by
+// a workgroup of PAGE_THREADS.  The rows' entries are chunks of 64, numbered over all
+// rows, and shared out evenly: sixteen a wavefront are in flight, whose rows its lanes
+// find together.  start: R + 1 numbers of LDS; meanwhile(): what is done while the
+// lengths are loaded, ready for f behind a barrier.
+template <typename M, typename F>
+__device__ __forceinline__ void each_page(const PageTable &t, int split, int splits, int *start, int *scratch, M meanwhile, F f)
 {
-    constexpr int ROWS = 8, LOADS = 2;
+    constexpr int PER = SBVR_REQUESTS_MAX / PAGE_THREADS, FLIGHT = 16;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    for (int r0 = wave * ROWS; r0 < t.R; r0 += PAGE_THREADS) {
-        // the lengths of the wavefront's next 64 rows
-        const int row = r0 + lane / ROWS * (PAGE_WAVES * ROWS) + lane % ROWS;
-        const int used_by = row < t.R ? entries_in_use(t.context_lens[row], t) : 0;
-        for (int i = 0; i < 64; i += ROWS) {
-            int used[ROWS], most = 0;
+    int chunks[PER], own = 0, all;
 #pragma unroll
-            for (int u = 0; u < ROWS; ++u) {
-                used[u] = __builtin_amdgcn_readlane(used_by, i + u);
-                most = max(most, used[u]);
-            }
-            const int32_t *table = t.page_table + (long long)(r0 + i * PAGE_WAVES) * t.table_stride;
-            for (int e0 = lane; e0 - lane < most; e0 += 64 * LOADS) {
-                int page[ROWS][LOADS];
+    for (int i = 0; i < PER; ++i) {
+        const int r = threadIdx.x * PER + i;
+        chunks[i] = r < t.R ? (entries_in_use(t.context_lens[r], t) + 63) >> 6 : 0;
+    }
+    meanwhile();
 #pragma unroll
-                for (int u = 0; u < ROWS; ++u)
+    for (int i = 0; i < PER; ++i)
+        own += chunks[i];
+    int before = sum_before<PAGE_THREADS>(own, all, scratch);
 #pragma unroll
-                    for (int k = 0; k < LOADS; ++k) {
-                        const int e = e0 + 64 * k;
-                        page[u][k] = e < used[u] ? table[u * t.table_stride + e] : -1;
-                    }
+    for (int i = 0; i < PER; ++i) {
+        const int r = threadIdx.x * PER + i;
+        if (r < t.R)
+            start[r] = before;
+        before += chunks[i];
+    }
+    if (threadIdx.x == 0)
+        start[t.R] = all;
+    __syncthreads();
+    // while one batch is used the next one is on its way
+    const int step = splits * PAGE_WAVES * FLIGHT;
+    int a[FLIGHT], b[FLIGHT];
+    auto fetch = [&](int c0, int (&page)[FLIGHT]) {
+        const int c = c0 + lane % FLIGHT, row = owner_of(start, t.R, min(c, all - 1)), entry = (c - start[row]) * 64;
+        const int left = c < all ? entries_in_use(t.context_lens[row], t) - entry : 0;
+        const uint64_t at = (uint64_t)(t.page_table + row * t.table_stride + entry);
 #pragma unroll
-                for (int u = 0; u < ROWS; ++u)
-#pragma unroll
-                    for (int k = 0; k < LOADS; ++k)
-                        f(page[u][k]);
-            }
+        for (int u = 0; u < FLIGHT; ++u) {
+            const int n = __builtin_amdgcn_readlane(left, u);
+            const uint32_t low = __builtin_amdgcn_readlane((uint32_t)at, u);
+            const uint32_t high = __builtin_amdgcn_readlane((uint32_t)(at >> 32), u);
+            const int32_t *entries = (const int32_t *)((uint64_t)high << 32 | low);
+            page[u] = lane < n ? entries[lane] : -1;
         }
+    };
+    auto use = [&](const int (&page)[FLIGHT]) {
+#pragma unroll
+        for (int u = 0; u < FLIGHT; ++u)
+            f(page[u]);
+    };
+    int c0 = (split * PAGE_WAVES + wave) * FLIGHT;
+    if (c0 < all)
+        fetch(c0, a);
+    for (; c0 < all; c0 += 2 * step) {
+        if (c0 + step < all)
+            fetch(c0 + step, b);
+        use(a);
+        if (c0 + 2 * step < all)
+            fetch(c0 + 2 * step, a);
+        if (c0 + step < all)
+            use(b);
     }
 }
 
 // A workgroup owns USAGE_PAGES pages, whose counts it holds in LDS: it goes through
-// all entries in use and counts its own.  (Counting in memory, by atomic additions
-// that cross the chip's L2s, took 40 us for 262144 entries.)  With one workgroup that
-// is all; else a second launch makes the list of free pages, where each workgroup
-// adds up the used pages before its own.
-constexpr int USAGE_PAGES = 12288;
+// the entries in use and counts its own.  (Counting in memory, by atomic additions
+// that cross the chip's L2s, took 40 us for 262144 entries.)  Few pages and entries:
+// that is all, and the workgroup makes the list of free pages too.  Many entries are
+// split over several workgroups, whose counts a second launch adds up; the list of
+// many pages is made by a last launch, where each workgroup adds up the used pages
+// before its own.
+constexpr int USAGE_PAGES = 11264, SHARE = USAGE_PAGES / PAGE_WAVES;  // SHARE: pages of a wavefront, or of a later launch's workgroup
+#ifndef USAGE_CHUNKS
+#define USAGE_CHUNKS 256
+#endif
+constexpr int USAGE_SPLITS = 16, USAGE_GROUPS = 256;
 
-// The list of free pages from counts in LDS or memory, by a workgroup with the pages
-// first .. first + n, `before` of the lower ones used and `total` of all.
-__device__ __forceinline__ void list_free(const UsageArgs &a, const int *count, int first, int n, int before, int total,
-                                          int *used_by_wave)
+// The list of free pages for the pages first .. first + n, by one wavefront; `used`
+// of the lower ones are, and `total` of all.
+__device__ __forceinline__ void list_free(const UsageArgs &a, const int *count, int first, int n, int used, int total)
 {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int share = (n + PAGE_THREADS - 1) / PAGE_THREADS * 64, i0 = wave * share, i1 = min(i0 + share, n);
-    int used = before;
-    for (int w = 0; w < wave; ++w)
-        used += used_by_wave[w];
-    for (int i = i0; i < i1; i += 64) {
-        const bool in = i + lane < i1;
-        const bool here = in && count[i + lane] > 0;
+    const int lane = threadIdx.x & 63;
+    for (int i = 0; i < n; i += 64) {
+        const bool in = i + lane < n;
+        const bool here = in && count[min(i + lane, n - 1)] > 0;
         const uint64_t marks = __ballot(here);
         const int p = first + i + lane;
         if (in && !here)
@@ -120,66 +156,109 @@ __device__ __forceinline__ void list_free(const UsageArgs &a, const int *count, 
     }
 }
 
-// Used pages of each wavefront's share of counts, to used_by_wave; returns their sum.
-__device__ __forceinline__ int count_used(const int *count, int n, int *used_by_wave)
+__device__ __forceinline__ int count_used(const int *count, int n)
 {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int share = (n + PAGE_THREADS - 1) / PAGE_THREADS * 64, i0 = wave * share, i1 = min(i0 + share, n);
+    const int lane = threadIdx.x & 63;
     int used = 0;
-    for (int i = i0; i < i1; i += 64)
-        used += __popcll(__ballot(i + lane < i1 && count[min(i + lane, i1 - 1)] > 0));
-    if (lane == 0)
-        used_by_wave[wave] = used;
-    __syncthreads();
-    int all = 0;
-#pragma unroll
-    for (int w = 0; w < PAGE_WAVES; ++w)
-        all += used_by_wave[w];
-    return all;
+    for (int i = 0; i < n; i += 64)
+        used += __popcll(__ballot(i + lane < n && count[min(i + lane, n - 1)] > 0));
+    return used;
 }
 
 __global__ void __launch_bounds__(PAGE_THREADS) usage_kernel(UsageArgs a)
 {
-    __shared__ int count[USAGE_PAGES], used_by_wave[PAGE_WAVES];
+    __shared__ int count[USAGE_PAGES], start[SBVR_REQUESTS_MAX + 1], used_by_wave[PAGE_WAVES];
     const int first = blockIdx.x * USAGE_PAGES, n = min(USAGE_PAGES, a.n_pages - first);
-    for (int i = threadIdx.x; i < n; i += PAGE_THREADS)
-        count[i] = 0;
-    __syncthreads();
-    each_page(a.t, [&](int page) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const bool alone = gridDim.x == 1 && gridDim.y == 1;
+    auto clear = [&] {
+        for (int i = threadIdx.x; i < n; i += PAGE_THREADS)
+            count[i] = 0;
+    };
+    each_page(a.t, blockIdx.y, gridDim.y, start, used_by_wave, clear, [&](int page) {
         const uint32_t own = (uint32_t)page - (uint32_t)first;
         if (own < (uint32_t)n)
             atomicAdd(&count[own], 1);
     });
     __syncthreads();
+    int32_t *out = (gridDim.y > 1 ? a.partial + (long long)blockIdx.y * a.n_pages : a.refs) + first;
     for (int i = threadIdx.x; i < n; i += PAGE_THREADS)
-        a.refs[first + i] = count[i];
-    const int used = count_used(count, n, used_by_wave);
-    if (gridDim.x == 1) {
-        list_free(a, count, first, n, 0, used, used_by_wave);
-        if (threadIdx.x == 0) {
-            a.counts[0] = a.n_pages - used;
-            a.counts[1] = used;
-        }
-    } else if (threadIdx.x == 0) {
-        a.used[blockIdx.x] = used;
+        out[i] = count[i];
+    if (gridDim.y > 1)
+        return;
+    // alone: the wavefronts share the pages evenly
+    const int share = alone ? (n + PAGE_THREADS - 1) / PAGE_THREADS * 64 : SHARE;
+    const int i0 = min(wave * share, n), m = min(share, n - i0);
+    const int used = count_used(count + i0, m);
+    if (!alone) {
+        if (lane == 0 && m > 0)
+            a.used[blockIdx.x * PAGE_WAVES + wave] = used;
+        return;
+    }
+    if (lane == 0)
+        used_by_wave[wave] = used;
+    __syncthreads();
+    int before = 0, all = 0;
+#pragma unroll
+    for (int w = 0; w < PAGE_WAVES; ++w) {
+        before += w < wave ? used_by_wave[w] : 0;
+        all += used_by_wave[w];
+    }
+    list_free(a, count + i0, i0, m, before, all);
+    if (threadIdx.x == 0) {
+        a.counts[0] = a.n_pages - all;
+        a.counts[1] = all;
     }
 }
 
-__global__ void __launch_bounds__(PAGE_THREADS) free_kernel(UsageArgs a)
+// A share's counts added up over the splits.
+__global__ void __launch_bounds__(256) add_kernel(UsageArgs a, int splits)
 {
-    __shared__ int used_by_wave[PAGE_WAVES], scratch[PAGE_WAVES];
-    const int first = blockIdx.x * USAGE_PAGES, n = min(USAGE_PAGES, a.n_pages - first), groups = gridDim.x;
-    int before = 0, all = 0, sum;
-    for (int w = threadIdx.x; w < groups; w += PAGE_THREADS) {
-        all += a.used[w];
-        before += w < (int)blockIdx.x ? a.used[w] : 0;
+    __shared__ int scratch[4];
+    const int first = blockIdx.x * SHARE, n = min(SHARE, a.n_pages - first);
+    int used = 0, all;
+#pragma unroll
+    for (int k = 0; k < (SHARE + 255) / 256; ++k) {
+        const int i = k * 256 + threadIdx.x;
+        int sum = 0, part[USAGE_SPLITS];
+#pragma unroll
+        for (int s = 0; s < USAGE_SPLITS; ++s)
+            part[s] = i < n && s < splits ? a.partial[(long long)s * a.n_pages + first + i] : 0;
+#pragma unroll
+        for (int s = 0; s < USAGE_SPLITS; ++s)
+            sum += part[s];
+        if (i < n)
+            a.refs[first + i] = sum;
+        used += sum > 0;
     }
-    sum_before<PAGE_THREADS>(all, sum, scratch);
+    sum_before<256>(used, all, scratch);
+    if (threadIdx.x == 0)
+        a.used[blockIdx.x] = all;
+}
+
+// The free pages of a share.
+__global__ void __launch_bounds__(256) free_kernel(UsageArgs a)
+{
+    __shared__ int scratch[4], used_by_wave[4];
+    const int first = blockIdx.x * SHARE, n = min(SHARE, a.n_pages - first), shares = gridDim.x;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int i0 = min(wave * (SHARE / 4), n), m = min(SHARE / 4, n - i0);
+    const int used = count_used(a.refs + first + i0, m);
+    if (lane == 0)
+        used_by_wave[wave] = used;
+    int before = 0, all = 0, sum;
+    for (int w = threadIdx.x; w < shares; w += 256) {
+        const int u = a.used[w];
+        all += u;
+        before += w < (int)blockIdx.x ? u : 0;
+    }
+    sum_before<256>(all, sum, scratch);
     all = sum;
-    sum_before<PAGE_THREADS>(before, sum, scratch);
+    sum_before<256>(before, sum, scratch);
     before = sum;
-    count_used(a.refs + first, n, used_by_wave);
-    list_free(a, a.refs + first, first, n, before, all, used_by_wave);
+    for (int w = 0; w < wave; ++w)
+        before += used_by_wave[w];
+    list_free(a, a.refs + first + i0, first + i0, m, before, all);
     if (blockIdx.x == 0 && threadIdx.x == 0) {
         a.counts[0] = a.n_pages - all;
         a.counts[1] = all;
@@ -188,21 +267,46 @@ __global__ void __launch_bounds__(PAGE_THREADS) free_kernel(UsageArgs a)
 
 namespace {
 
-int usage_groups(int n_pages) { return (n_pages + USAGE_PAGES - 1) / USAGE_PAGES; }
+struct UsageShape {
+    int owners, splits, shares;
+};
+
+UsageShape usage_shape(int R, int max_pages, int n_pages)
+{
+    UsageShape s;
+    s.owners = (n_pages + USAGE_PAGES - 1) / USAGE_PAGES;
+    s.shares = (n_pages + SHARE - 1) / SHARE;
+    const long long chunks = (long long)R * ((max_pages + 63) / 64);
+    s.splits = chunks < 2 * USAGE_CHUNKS ? 1 : chunks < USAGE_SPLITS * USAGE_CHUNKS ? (int)(chunks / USAGE_CHUNKS) : USAGE_SPLITS;
+    if (s.splits * s.owners > USAGE_GROUPS)
+        s.splits = USAGE_GROUPS / s.owners > 1 ? USAGE_GROUPS / s.owners : 1;
+    return s;
+}
+
+size_t used_bytes(const UsageShape &s) { return ((size_t)s.shares * sizeof(int32_t) + 15) / 16 * 16; }
 
 }  // namespace
 
-size_t usage_workspace_bytes(int n_pages) { return ((size_t)usage_groups(n_pages) * sizeof(int32_t) + 15) / 16 * 16; }
+size_t usage_workspace_bytes(int R, int max_pages, int n_pages)
+{
+    const UsageShape s = usage_shape(R, max_pages, n_pages);
+    return used_bytes(s) + (s.splits > 1 ? (size_t)s.splits * n_pages * sizeof(int32_t) : 0);
+}
 
 int launch_usage(const UsageArgs &a, hipStream_t stream)
 {
+    const UsageShape s = usage_shape(a.t.R, a.t.max_pages, a.n_pages);
     UsageArgs args = a;
-    void *argv[] = {&args};
-    const dim3 grid(usage_groups(a.n_pages));
-    const int st = launch_kernel((const void *)usage_kernel, grid, dim3(PAGE_THREADS), 0, stream, argv);
-    if (st != SBVR_OK || grid.x == 1)
+    args.partial = (int32_t *)((char *)a.used + used_bytes(s));
+    int splits = s.splits;
+    void *argv[] = {&args, &splits};
+    int st = launch_kernel((const void *)usage_kernel, dim3(s.owners, s.splits), dim3(PAGE_THREADS), 0, stream, argv);
+    if (st != SBVR_OK || (s.owners == 1 && s.splits == 1))
         return st;
-    return launch_kernel((const void *)free_kernel, grid, dim3(PAGE_THREADS), 0, stream, argv);
+    if (s.splits > 1 &&
+        (st = launch_kernel((const void *)add_kernel, dim3(s.shares), dim3(256), 0, stream, argv)) != SBVR_OK)
+        return st;
+    return launch_kernel((const void *)free_kernel, dim3(s.shares), dim3(256), 0, stream, argv);
 }
 
 // ---------------------------------------------------------------------------
@@ -344,12 +448,14 @@ __global__ void __launch_bounds__(PAGE_THREADS) compact_kernel(CompactArgs a, in
 {
     __shared__ uint32_t marks[COMPACT_PAGES / 32];
     __shared__ int used_before[COMPACT_PAGES / 32];  // of each word
+    __shared__ int start[SBVR_REQUESTS_MAX + 1];
     __shared__ int scratch[PAGE_WAVES], stays;
     const int tid = threadIdx.x, words = mark_words(a.n_pages), lists = a.n_pages / 2;
-    for (int w = tid; w < words; w += PAGE_THREADS)
-        marks[w] = 0;
-    __syncthreads();
-    each_page(a.t, [&](int page) {
+    auto clear = [&] {
+        for (int w = tid; w < words; w += PAGE_THREADS)
+            marks[w] = 0;
+    };
+    each_page(a.t, 0, 1, start, scratch, clear, [&](int page) {
         if ((uint32_t)page < (uint32_t)a.n_pages)
             atomicOr(&marks[page >> 5], 1u << (page & 31));
     });

@@ -130,7 +130,8 @@ struct UsageArgs {
     PageTable t;
     int n_pages;
     int32_t *refs, *free_pages, *counts;
-    int32_t *used;  // the workspace: used pages of each workgroup's
+    int32_t *used;     // the workspace: used pages of each share of the pages, and behind
+    int32_t *partial;  // them, set by the launcher, counts by splits of the rows
 };
 
 struct ForkArgs {
@@ -163,7 +164,7 @@ int launch_logits(const sbvr_logits_args &a, hipStream_t stream);
 int launch_rotary(const RotaryArgs &a, hipStream_t stream);
 size_t beam_workspace_bytes(int R, int B, int V, int n, int n_end);
 int launch_beam(const sbvr_beam_args &a, void *workspace, hipStream_t stream);
-size_t usage_workspace_bytes(int n_pages);
+size_t usage_workspace_bytes(int R, int max_pages, int n_pages);
 int launch_usage(const UsageArgs &a, hipStream_t stream);
 int launch_fork(const ForkArgs &a, hipStream_t stream);
 size_t compact_workspace_bytes(int n_pages);

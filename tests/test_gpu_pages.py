@@ -81,6 +81,16 @@ def test_usage_of_most_rows():
     check_usage(rng.integers(0, 70 * 16, 4096).tolist(), table, 16, 9000)
 
 
+@pytest.mark.parametrize("R,width,pages", [(1000, 300, 30000), (130, 513, 12289), (4096, 150, 9000), (2000, 100, 4), (700, 50, 400001)])
+def test_usage_of_many_rows_and_pages(R, width, pages):
+    """Rows that are split over workgroups, with one owner of pages and several."""
+    rng = np.random.default_rng(R)
+    table = rng.integers(-1, pages + 1, (R, width)).tolist()
+    lens = rng.integers(0, width * 16 + 40, R)
+    lens[::3] //= 10
+    check_usage(lens.tolist(), table, 16, pages, stride=width + 1)
+
+
 def test_usage_of_one_page_by_all():
     check_usage([160] * 500, [[5] * 10] * 500, 16, 9)
 
