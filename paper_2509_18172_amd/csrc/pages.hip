@@ -662,7 +662,7 @@ __global__ void __launch_bounds__(COPY_THREADS) page_copy_kernel(CopyArgs a)
 #pragma unroll
                 for (int u = 0; u < COPY_UNROLL; ++u)
                     if (t0 + u * Y < last)
-                        *(v4u *)(to + (t0 + u * Y) * token_stride) = v[u];
+                        __builtin_nontemporal_store(v[u], (v4u *)(to + (t0 + u * Y) * token_stride));
             }
         }
     }
