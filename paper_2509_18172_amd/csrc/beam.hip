@@ -11,10 +11,11 @@
 // groups in all, and the keep-th largest of these is a value that at least `keep`
 // logits reach, so what is below it cannot be chosen.  What is left -- hardly more
 // than `keep` -- goes into a list, whose entries are ranked by counting the better
-// ones.  Only where so many logits are alike that the list does not hold them, the
-// keep-th best is found bit by bit.  A logit is compared with its place: key =
-// (logit, ~token) as one number, so equal logits are ordered and keys are all
-// different.
+// ones; a longer list, as of a tile that is hardly filled, is first cut to its `keep`
+// best bit by bit.  A logit is compared with its place: key = (logit, ~token) as one
+// number, so equal logits are ordered and keys are all different.  Where so many are
+// alike that the list does not hold them, those above the value go into it and of the
+// equal ones the `keep` first.
 //
 // Sums: exp(l - r) = 2^(l log2 e - c), one rounding for the exponent; r = c / log2 e
 // is what the sum refers to, so c's own rounding costs nothing.  (The rounding of
@@ -26,7 +27,7 @@
 namespace sbvr {
 
 constexpr int BEAM_THREADS = 256, BEAM_ENTRIES = 3072;  // of a request's parts together
-constexpr int BEAM_LIST = 256;                          // a tile's logits to be ranked
+constexpr int BEAM_RANKED = 256, BEAM_LIST = 2048 + SBVR_BEAM_KEEP_MAX;  // logits to be ranked, and to be cut before
 constexpr float LOG2E = 1.44269502f, LARGEST = 3.402823466e38f;
 
 struct PartSum {
@@ -132,14 +133,46 @@ __device__ __forceinline__ double log_of(double x)
     return fma((double)e, 0.6931471805599453, p * z);
 }
 
+// The `keep` largest of the c > keep different numbers in list, to kept, in no order:
+// bit by bit the largest number that `keep` of them reach.  counts: 65 numbers.
+template <typename F>
+__device__ __forceinline__ void largest(F number, int c, int keep, uint64_t *kept, int *counts)
+{
+    const int lane = threadIdx.x & 63;
+    __syncthreads();
+    if (threadIdx.x < 65)
+        counts[threadIdx.x] = 0;
+    __syncthreads();
+    uint64_t least = 0;
+    for (int bit = 63; bit >= 0; --bit) {
+        const uint64_t candidate = least | 1ull << bit;
+        int reach = 0;
+        for (int i = threadIdx.x; i < (c + 63) / 64 * 64; i += BEAM_THREADS)
+            reach += __popcll(__ballot(i < c && number(min(i, c - 1)) >= candidate));
+        if (lane == 0 && reach)
+            atomicAdd(&counts[bit], reach);
+        __syncthreads();
+        if (counts[bit] >= keep)
+            least = candidate;
+        if (counts[bit] == keep)
+            break;
+    }
+    for (int i = threadIdx.x; i < c; i += BEAM_THREADS) {
+        const uint64_t v = number(i);
+        if (v && v >= least)
+            kept[atomicAdd(&counts[64], 1)] = v;
+    }
+    __syncthreads();
+}
+
 // CH: pieces of eight logits a thread holds of a tile.
 template <typename T, int CH>
 __global__ void __launch_bounds__(BEAM_THREADS) beam_part_kernel(sbvr_beam_args a, BeamShape s, PartSum *sums, uint64_t *entries)
 {
     constexpr int TILE = 8 * CH * BEAM_THREADS, WAVES = BEAM_THREADS / 64;
-    __shared__ uint64_t list[SBVR_BEAM_KEEP_MAX + BEAM_LIST];  // the best so far, and what may be better
+    __shared__ uint64_t list[BEAM_LIST], kept[SBVR_BEAM_KEEP_MAX];  // the best so far, and what may be better
     __shared__ float group[2][64];
-    __shared__ int count, counts[2], ends[SBVR_BEAM_KEEP_MAX];
+    __shared__ int count, counts[65], ends[SBVR_BEAM_KEEP_MAX], equal_before[WAVES];
     __shared__ double wave_sum[WAVES];
     const int tid = threadIdx.x, lane = tid & 63, row = blockIdx.x / s.parts, part = blockIdx.x % s.parts;
     if (!isfinite(uniform_load(a.scores + row)))
@@ -211,14 +244,14 @@ __global__ void __launch_bounds__(BEAM_THREADS) beam_part_kernel(sbvr_beam_args 
             const uint32_t candidate = least | 1u << bit;
             least = __popcll(__ballot(ordered(mine) >= candidate)) >= s.keep ? candidate : least;
         }
-        const float least_value = fminf(unordered(max(least, floor)), LARGEST);
+        float least_value = fminf(unordered(max(least, floor)), LARGEST);
         if (tile_top > -INFINITY) {  // the same for all
             tile_top = fminf(tile_top, LARGEST);
             // differences instead where c is so large that 2 to its rounding is (2^-25 of
             // c: 0.04 at a million)
             const bool huge = fabsf(tile_top) > 1e6f || (fabsf(top) > 1e6f && top > -INFINITY);
             if (tile_top > top) {
-                const double now = huge ? (double)tile_top : (double)(tile_top * LOG2E) / (double)LOG2E;
+                const double now = huge ? (double)tile_top : (double)(tile_top * LOG2E) * (1. / (double)LOG2E);
                 total *= exp_of(reference - now);  // (0 before the first)
                 reference = now;
                 offset = tile_top * LOG2E;
@@ -249,56 +282,92 @@ __global__ void __launch_bounds__(BEAM_THREADS) beam_part_kernel(sbvr_beam_args 
                     for (int e = 0; e < 8; ++e)
                         if (x[c][e] >= least_value) {
                             const int k = atomicAdd(&count, 1);
-                            if (k < SBVR_BEAM_KEEP_MAX + BEAM_LIST)
+                            if (k < BEAM_LIST)
                                 list[k] = key_of(x[c][e], at(c) + e);
                         }
         }
         __syncthreads();
         int c = count;
+        const uint64_t *from = list;
         if (c > BEAM_LIST) {
-            // too many alike: the keep-th best of the tile's and of those before is found
-            // bit by bit, from the logits in memory
-            const uint64_t before = tid < have ? list[tid] : 0;
-            const int first = tile * TILE, n = min(TILE, a.V - first);
-            auto key_at = [&](int i) {
-                const float l = (float)in[first + i];
-                return l > -INFINITY ? key_of(l, first + i) : 0;
-            };
-            uint64_t least_key = 0;
-            for (int bit = 63; bit >= 0; --bit) {
-                const uint64_t candidate = least_key | 1ull << bit;
-                int reach = before >= candidate;
-                for (int i = tid; i < n; i += BEAM_THREADS)
-                    reach += key_at(i) >= candidate;
-                if (tid == 0)
-                    counts[bit & 1] = 0;
-                __syncthreads();
-                atomicAdd(&counts[bit & 1], reach);
-                __syncthreads();
-                least_key = counts[bit & 1] >= s.keep ? candidate : least_key;
+            // too many alike: the value to the last bit, those above it, and the first
+            // of those that have it
+            least = 0;
+#pragma unroll
+            for (int bit = 31; bit >= 0; --bit) {
+                const uint32_t candidate = least | 1u << bit;
+                least = __popcll(__ballot(ordered(mine) >= candidate)) >= s.keep ? candidate : least;
             }
-            if (tid == 0)
-                count = 0;
+            least_value = fminf(unordered(max(least, floor)), LARGEST);
             __syncthreads();
-            if (before && before >= least_key)
-                list[atomicAdd(&count, 1)] = before;
-            for (int i = tid; i < n; i += BEAM_THREADS) {
-                const uint64_t key = key_at(i);
-                if (key && key >= least_key)
-                    list[atomicAdd(&count, 1)] = key;
+            if (tid == 0)
+                count = have;
+            __syncthreads();
+            int equal = 0;  // of the pieces before, in all threads
+#pragma unroll
+            for (int c = 0; c < CH; ++c) {
+                int own = 0;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float l = fminf(x[c][e], LARGEST);
+                    own += x[c][e] == x[c][e] && l == least_value;
+                    if (x[c][e] == x[c][e] && l > least_value) {
+                        const int k = atomicAdd(&count, 1);
+                        if (k < BEAM_LIST)
+                            list[k] = key_of(l, at(c) + e);
+                    }
+                }
+                int up = own;  // with the lanes before
+#pragma unroll
+                for (int m = 1; m < 64; m <<= 1) {
+                    const int other = __shfl_up(up, m);
+                    up += lane >= m ? other : 0;
+                }
+                __syncthreads();
+                if (lane == 63)
+                    equal_before[tid >> 6] = up;
+                __syncthreads();
+                int place = equal + up - own;
+#pragma unroll
+                for (int w = 0; w < WAVES; ++w) {
+                    place += w < tid >> 6 ? equal_before[w] : 0;
+                    equal += equal_before[w];
+                }
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (x[c][e] == x[c][e] && fminf(x[c][e], LARGEST) == least_value && place++ < s.keep) {
+                        const int k = atomicAdd(&count, 1);
+                        if (k < BEAM_LIST)
+                            list[k] = key_of(x[c][e], at(c) + e);
+                    }
             }
             __syncthreads();
             c = count;
-            have = 0;
         }
-        if (c > have) {
+        if (c > BEAM_LIST) {
+            // even so, as in a tile whose best lie together: from the logits in memory
+            const int first = tile * TILE, n = min(TILE, a.V - first);
+            largest([&](int i) -> uint64_t {
+                if (i < have)
+                    return list[i];
+                const float l = (float)in[first + i - have];
+                return l > -INFINITY ? key_of(l, first + i - have) : 0;
+            }, n + have, s.keep, kept, counts);
+            from = kept;
+            c = s.keep;
+        } else if (c > BEAM_RANKED) {
+            largest([&](int i) { return list[i]; }, c, s.keep, kept, counts);
+            from = kept;
+            c = s.keep;
+        }
+        if (c > have || from == kept) {
             uint64_t key = 0;
             int better = 0;
             if (tid < c) {
-                key = list[tid];
+                key = from[tid];
 #pragma unroll 8
                 for (int j = 0; j < c; ++j)
-                    better += list[j] > key;
+                    better += from[j] > key;
             }
             __syncthreads();
             if (tid < c && better < s.keep)
@@ -348,7 +417,7 @@ __global__ void __launch_bounds__(THREADS) beam_join_kernel(sbvr_beam_args a, Be
     constexpr uint32_t END = 1u << 31;
     extern __shared__ double list_score[];  // and behind them, each entry's place, beam and whether it is an end, and its token
     __shared__ double add[SBVR_BEAMS_MAX], beam_reference[SBVR_BEAMS_MAX];
-    __shared__ float group[64];
+    __shared__ uint32_t group[64];
     __shared__ int rank[64], count;
     __shared__ float score_out[SBVR_BEAM_KEEP_MAX], ended[SBVR_BEAMS_MAX];
     __shared__ int token_out[SBVR_BEAM_KEEP_MAX], parent_out[SBVR_BEAM_KEEP_MAX], ended_token[SBVR_BEAMS_MAX];
@@ -391,7 +460,7 @@ __global__ void __launch_bounds__(THREADS) beam_join_kernel(sbvr_beam_args a, Be
         }
     }
     if (tid < 64) {
-        rank[tid] = 0;
+        rank[tid] = group[tid] = 0;
         score_out[tid] = -INFINITY;
         token_out[tid] = parent_out[tid] = -1;
     }
@@ -417,24 +486,19 @@ __global__ void __launch_bounds__(THREADS) beam_join_kernel(sbvr_beam_args a, Be
         score[i] = (place < all) & (key[i] != 0) & (add[beam[i]] > -INFINITY) ? value : -INFINITY;
         mine = fmaxf(mine, key[i] & END_ENTRY ? (float)score[i] : -INFINITY);
     }
-    mine = fmaxf(mine, dpp<0xb1>(mine, mine));  // lanes 1 0 3 2, 2 3 0 1 of four
-    mine = fmaxf(mine, dpp<0x4e>(mine, mine));
-    if (WAVES == 16) {
-        mine = fmaxf(mine, dpp<0x124>(mine, mine));  // rotations by 4 and 8 of sixteen
-        mine = fmaxf(mine, dpp<0x128>(mine, mine));
-    }
-    if (tid % WAVES == 0)
-        group[tid / WAVES] = mine;
+    // (a group is a lane of all wavefronts: neighbours are of one list, in order)
+    if (mine > -INFINITY)
+        atomicMax(&group[lane], ordered(mine));
     __syncthreads();
-    mine = group[lane];
+    const uint32_t number = group[lane];
     int above = 0;
 #pragma unroll
     for (int j = 0; j < 64 / WAVES; ++j)
-        above += group[(tid >> 6) * (64 / WAVES) + j] > mine;
+        above += group[(tid >> 6) * (64 / WAVES) + j] > number;
     if (above)
         atomicAdd(&rank[lane], above);
     __syncthreads();
-    const float least = -max_of_wave(rank[lane] < a.n ? -mine : -INFINITY);
+    const float least = -max_of_wave(rank[lane] >= a.n ? -INFINITY : number ? -unordered(number) : INFINITY);
     int listed[PER], mine_listed = 0;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
