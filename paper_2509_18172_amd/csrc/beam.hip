@@ -11,8 +11,8 @@
 // groups in all, and the keep-th largest of these is a value that at least `keep`
 // logits reach, so what is below it cannot be chosen.  What is left -- hardly more
 // than `keep` -- goes into a list, whose entries are ranked by counting the better
-// ones; a longer list, as of a tile that is hardly filled, is first cut to its `keep`
-// best bit by bit.  A logit is compared with its place: key = (logit, ~token) as one
+// ones; a longer list, as of a tile that is hardly filled, is first thinned out the
+// same way.  A logit is compared with its place: key = (logit, ~token) as one
 // number, so equal logits are ordered and keys are all different.  Where so many are
 // alike that the list does not hold them, those above the value go into it and of the
 // equal ones the `keep` first.
@@ -26,8 +26,8 @@
 
 namespace sbvr {
 
-constexpr int BEAM_THREADS = 256, BEAM_ENTRIES = 3072;  // of a request's parts together
-constexpr int BEAM_RANKED = 256, BEAM_LIST = 2048 + SBVR_BEAM_KEEP_MAX;  // logits to be ranked, and to be cut before
+constexpr int BEAM_THREADS = 256, BEAM_WAVES = BEAM_THREADS / 64, BEAM_ENTRIES = 3072;  // of a request's parts together
+constexpr int BEAM_RANKED = 2 * BEAM_THREADS, BEAM_LIST = 2048 + SBVR_BEAM_KEEP_MAX;  // logits to be ranked, and to be thinned out before
 constexpr float LOG2E = 1.44269502f, LARGEST = 3.402823466e38f;
 
 struct PartSum {
@@ -165,14 +165,58 @@ __device__ __forceinline__ void largest(F number, int c, int keep, uint64_t *kep
     __syncthreads();
 }
 
-// CH: pieces of eight logits a thread holds of a tile.
-template <typename T, int CH>
-__global__ void __launch_bounds__(BEAM_THREADS) beam_part_kernel(sbvr_beam_args a, BeamShape s, PartSum *sums, uint64_t *entries)
+// The keep-th largest of the lanes' numbers, to the bits from `last` up.
+__device__ __forceinline__ uint32_t reached_by(uint32_t number, int keep, int last)
 {
-    constexpr int TILE = 8 * CH * BEAM_THREADS, WAVES = BEAM_THREADS / 64;
+    uint32_t least = 0;
+#pragma unroll
+    for (int bit = 31; bit >= last; --bit) {
+        const uint32_t candidate = least | 1u << bit;
+        least = __popcll(__ballot(number >= candidate)) >= keep ? candidate : least;
+    }
+    return least;
+}
+
+// Thins out the c different keys of list to those whose value a quarter of `keep`
+// threads of each wavefront reach, and returns how many are left.
+__device__ __forceinline__ int thin_out(uint64_t *list, int c, int keep, uint32_t *least_of, int *count)
+{
+    const int tid = threadIdx.x;
+    uint32_t mine = 0, least = ~0u;
+    for (int i = tid; i < c; i += BEAM_THREADS)
+        mine = max(mine, (uint32_t)(list[i] >> 32));
+    mine = reached_by(mine, (keep + BEAM_WAVES - 1) / BEAM_WAVES, 0);
+    __syncthreads();
+    if ((tid & 63) == 0)
+        least_of[tid >> 6] = mine;
+    if (tid == 0)
+        *count = 0;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < BEAM_WAVES; ++w)
+        least = min(least, least_of[w]);
+    // (what is written lies in what all threads have read)
+    for (int i0 = 0; i0 < c; i0 += BEAM_THREADS) {
+        const uint64_t key = i0 + tid < c ? list[i0 + tid] : 0;
+        __syncthreads();
+        if (key && (uint32_t)(key >> 32) >= least)
+            list[atomicAdd(count, 1)] = key;
+        __syncthreads();
+    }
+    return *count;
+}
+
+// CH: pieces of eight logits a thread holds of a tile.
+// Six wavefronts a SIMD: 256 rows of 131072 in binary16 take 26.2 us with the 80
+// registers that this leaves, 27.5 with five and 82 (seven: 42, with spills).
+template <typename T, int CH>
+__global__ void __launch_bounds__(BEAM_THREADS, 6) beam_part_kernel(sbvr_beam_args a, BeamShape s, PartSum *sums, uint64_t *entries)
+{
+    constexpr int TILE = 8 * CH * BEAM_THREADS, WAVES = BEAM_WAVES;
     __shared__ uint64_t list[BEAM_LIST], kept[SBVR_BEAM_KEEP_MAX];  // the best so far, and what may be better
     __shared__ float group[2][64];
     __shared__ int count, counts[65], ends[SBVR_BEAM_KEEP_MAX], equal_before[WAVES];
+    __shared__ uint32_t least_of[BEAM_WAVES];
     __shared__ double wave_sum[WAVES];
     const int tid = threadIdx.x, lane = tid & 63, row = blockIdx.x / s.parts, part = blockIdx.x % s.parts;
     if (!isfinite(uniform_load(a.scores + row)))
@@ -192,8 +236,6 @@ __global__ void __launch_bounds__(BEAM_THREADS) beam_part_kernel(sbvr_beam_args 
         // first elements belong to the piece before
         const int v0 = tile * TILE + tid * 8;
         auto at = [&](int c) { return max(min(v0 + c * 8 * BEAM_THREADS, a.V - 8), 0); };
-        if (tid == 0)
-            count = have;
         if (a.V >= 8) {
             Words<T> w[CH];
 #pragma unroll
@@ -233,17 +275,27 @@ __global__ void __launch_bounds__(BEAM_THREADS) beam_part_kernel(sbvr_beam_args 
         float *groups = group[tile & 1];
         if ((tid & 3) == 0)
             groups[tid >> 2] = in_group;
+        // many to keep: the 64 groups' maxima are no close bound, the lanes' of each
+        // wavefront are
+        const bool many = s.keep > 32;
+        if (many) {
+            const uint32_t reached = reached_by(ordered(best), (s.keep + WAVES - 1) / WAVES, 16);
+            if (lane == 0)
+                least_of[tid >> 6] = reached;
+        }
+        if (tid == 0)
+            count = have;
         __syncthreads();
 
         const float mine = groups[lane];
         float tile_top = max_of_wave(mine);
-        // the keep-th largest of the groups' maxima, to its leading 16 bits
-        uint32_t least = 0;
+        uint32_t least = ~0u;
+        if (many)
 #pragma unroll
-        for (int bit = 31; bit >= 16; --bit) {
-            const uint32_t candidate = least | 1u << bit;
-            least = __popcll(__ballot(ordered(mine) >= candidate)) >= s.keep ? candidate : least;
-        }
+            for (int w = 0; w < WAVES; ++w)
+                least = min(least, least_of[w]);
+        else
+            least = reached_by(ordered(mine), s.keep, 16);
         float least_value = fminf(unordered(max(least, floor)), LARGEST);
         if (tile_top > -INFINITY) {  // the same for all
             tile_top = fminf(tile_top, LARGEST);
@@ -292,29 +344,28 @@ __global__ void __launch_bounds__(BEAM_THREADS) beam_part_kernel(sbvr_beam_args 
         if (c > BEAM_LIST) {
             // too many alike: the value to the last bit, those above it, and the first
             // of those that have it
-            least = 0;
-#pragma unroll
-            for (int bit = 31; bit >= 0; --bit) {
-                const uint32_t candidate = least | 1u << bit;
-                least = __popcll(__ballot(ordered(mine) >= candidate)) >= s.keep ? candidate : least;
-            }
+            least = reached_by(ordered(mine), s.keep, 0);
             least_value = fminf(unordered(max(least, floor)), LARGEST);
             __syncthreads();
             if (tid == 0)
                 count = have;
             __syncthreads();
             int equal = 0;  // of the pieces before, in all threads
-#pragma unroll
-            for (int c = 0; c < CH; ++c) {
+#pragma unroll 1
+            for (int i = 0; i < CH; ++i) {
+                // (read again: held until here, they cost every tile registers)
+                const int v = tile * TILE + (i * BEAM_THREADS + tid) * 8;
+                float l[8];
                 int own = 0;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    const float l = fminf(x[c][e], LARGEST);
-                    own += x[c][e] == x[c][e] && l == least_value;
-                    if (x[c][e] == x[c][e] && l > least_value) {
+                    l[e] = v + e < a.V ? (float)in[min(v + e, a.V - 1)] : -INFINITY;
+                    l[e] = l[e] == l[e] ? fminf(l[e], LARGEST) : -INFINITY;
+                    own += l[e] == least_value;
+                    if (l[e] > least_value) {
                         const int k = atomicAdd(&count, 1);
                         if (k < BEAM_LIST)
-                            list[k] = key_of(l, at(c) + e);
+                            list[k] = key_of(l[e], v + e);
                     }
                 }
                 int up = own;  // with the lanes before
@@ -335,10 +386,10 @@ __global__ void __launch_bounds__(BEAM_THREADS) beam_part_kernel(sbvr_beam_args 
                 }
 #pragma unroll
                 for (int e = 0; e < 8; ++e)
-                    if (x[c][e] == x[c][e] && fminf(x[c][e], LARGEST) == least_value && place++ < s.keep) {
+                    if (l[e] == least_value && place++ < s.keep) {
                         const int k = atomicAdd(&count, 1);
                         if (k < BEAM_LIST)
-                            list[k] = key_of(x[c][e], at(c) + e);
+                            list[k] = key_of(l[e], v + e);
                     }
             }
             __syncthreads();
@@ -355,23 +406,32 @@ __global__ void __launch_bounds__(BEAM_THREADS) beam_part_kernel(sbvr_beam_args 
             }, n + have, s.keep, kept, counts);
             from = kept;
             c = s.keep;
-        } else if (c > BEAM_RANKED) {
+        } else if (c > BEAM_THREADS) {
+            c = thin_out(list, c, s.keep, least_of, &count);
+        }
+        if (from == list && c > BEAM_RANKED) {
             largest([&](int i) { return list[i]; }, c, s.keep, kept, counts);
             from = kept;
             c = s.keep;
         }
         if (c > have || from == kept) {
-            uint64_t key = 0;
-            int better = 0;
-            if (tid < c) {
-                key = from[tid];
+            uint64_t key[BEAM_RANKED / BEAM_THREADS];
+            int better[BEAM_RANKED / BEAM_THREADS] = {};
+#pragma unroll
+            for (int i = 0; i < BEAM_RANKED / BEAM_THREADS; ++i) {
+                key[i] = 0;
+                if (i * BEAM_THREADS + tid < c) {
+                    key[i] = from[i * BEAM_THREADS + tid];
 #pragma unroll 8
-                for (int j = 0; j < c; ++j)
-                    better += from[j] > key;
+                    for (int j = 0; j < c; ++j)
+                        better[i] += from[j] > key[i];
+                }
             }
             __syncthreads();
-            if (tid < c && better < s.keep)
-                list[better] = key;
+#pragma unroll
+            for (int i = 0; i < BEAM_RANKED / BEAM_THREADS; ++i)
+                if (key[i] && better[i] < s.keep)
+                    list[better[i]] = key[i];
             have = min(c, s.keep);
             __syncthreads();
             if (have == s.keep)
@@ -417,8 +477,8 @@ __global__ void __launch_bounds__(THREADS) beam_join_kernel(sbvr_beam_args a, Be
     constexpr uint32_t END = 1u << 31;
     extern __shared__ double list_score[];  // and behind them, each entry's place, beam and whether it is an end, and its token
     __shared__ double add[SBVR_BEAMS_MAX], beam_reference[SBVR_BEAMS_MAX];
-    __shared__ uint32_t group[64];
-    __shared__ int rank[64], count;
+    __shared__ __attribute__((aligned(16))) uint32_t group[256];
+    __shared__ int rank[256], count;
     __shared__ float score_out[SBVR_BEAM_KEEP_MAX], ended[SBVR_BEAMS_MAX];
     __shared__ int token_out[SBVR_BEAM_KEEP_MAX], parent_out[SBVR_BEAM_KEEP_MAX], ended_token[SBVR_BEAMS_MAX];
     const int tid = threadIdx.x, lane = tid & 63, per_beam = s.parts * s.keep, all = a.B * per_beam;
@@ -459,8 +519,9 @@ __global__ void __launch_bounds__(THREADS) beam_join_kernel(sbvr_beam_args a, Be
             beam_reference[b] = reference;
         }
     }
-    if (tid < 64) {
+    if (tid < 256)
         rank[tid] = group[tid] = 0;
+    if (tid < 64) {
         score_out[tid] = -INFINITY;
         token_out[tid] = parent_out[tid] = -1;
     }
@@ -472,8 +533,9 @@ __global__ void __launch_bounds__(THREADS) beam_join_kernel(sbvr_beam_args a, Be
         count = 0;
     __syncthreads();
 
-    // As in a tile: the n-th largest of 64 groups' best scores that go on, here
-    // rounded to binary32, which keeps their order, leaves hardly more than the n best.
+    // As in a tile: the n-th largest of 64 groups' best scores that go on (256 where n
+    // is large), here rounded to binary32, which keeps their order, leaves hardly more
+    // than the n best.
     float mine = -INFINITY;
     double score[PER];
     int beam[PER];
@@ -486,19 +548,26 @@ __global__ void __launch_bounds__(THREADS) beam_join_kernel(sbvr_beam_args a, Be
         score[i] = (place < all) & (key[i] != 0) & (add[beam[i]] > -INFINITY) ? value : -INFINITY;
         mine = fmaxf(mine, key[i] & END_ENTRY ? (float)score[i] : -INFINITY);
     }
-    // (a group is a lane of all wavefronts: neighbours are of one list, in order)
+    // (a group is every 64th or 256th thread: neighbours are of one list, in order)
+    const int groups = a.n > 16 ? 256 : 64, slot = tid & (groups - 1), share = groups * groups / THREADS;
     if (mine > -INFINITY)
-        atomicMax(&group[lane], ordered(mine));
+        atomicMax(&group[slot], ordered(mine));
     __syncthreads();
-    const uint32_t number = group[lane];
+    const uint32_t number = group[slot];
     int above = 0;
-#pragma unroll
-    for (int j = 0; j < 64 / WAVES; ++j)
-        above += group[(tid >> 6) * (64 / WAVES) + j] > number;
+#pragma unroll 4
+    for (int j = tid / groups * share; j < (tid / groups + 1) * share; j += 4) {
+        const uint4 g = *(const uint4 *)&group[j];
+        above += (g.x > number) + (g.y > number) + (g.z > number) + (g.w > number);
+    }
     if (above)
-        atomicAdd(&rank[lane], above);
+        atomicAdd(&rank[slot], above);
     __syncthreads();
-    const float least = -max_of_wave(rank[lane] >= a.n ? -INFINITY : number ? -unordered(number) : INFINITY);
+    float least = INFINITY;
+    for (int g = lane; g < groups; g += 64)
+        if (rank[g] < a.n)
+            least = fminf(least, group[g] ? unordered(group[g]) : -INFINITY);
+    least = -max_of_wave(-least);
     int listed[PER], mine_listed = 0;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {

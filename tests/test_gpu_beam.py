@@ -138,6 +138,32 @@ def test_large_tiles_in_turn():
     check(logits, scores, 30, ends=(5, 69999))
 
 
+@pytest.mark.parametrize("B,n,V", [(2, 33, 900), (2, 62, 900), (1, 60, 8192 + 300), (3, 40, 2048 + 100), (2, 64, 200)])
+def test_hardly_filled_tiles(B, n, V):
+    """Tiles with fewer groups than there are entries to keep."""
+    for R in (1, 300):
+        logits, scores = make(R, B, V, F32, seed=n)
+        check(logits[:4 * B], scores[:4], n)
+        got, few = sb.beam_select(logits, scores, n=n), sb.beam_select(logits[:4 * B], scores[:4], n=n)
+        assert torch.equal(got.tokens[:4], few.tokens) and torch.equal(got.parents[:4], few.parents)
+
+
+@pytest.mark.parametrize("allowed", [0, 1, 5, 30])
+def test_finite_masks(allowed):
+    """Rows in which all but a few tokens have one low, finite logit, as some masks
+    leave them: the lowest tokens among equal ones follow."""
+    for R, B, V in ((1, 2, 3000), (150, 4, 9000)):
+        logits, scores = make(R, B, V, F32, seed=allowed)
+        keep = torch.randperm(V, device=DEV)[:allowed]
+        masked = torch.full_like(logits, -10000.0)
+        masked[:, keep] = logits[:, keep]
+        scores[:] = -1.0
+        masked[:] = masked[:1].clone()  # (the beams alike: equal scores are equal in every form)
+        check(masked[:2 * B], scores[:2], 20, ends=(0, 7), exact=True)
+        got = sb.beam_select(masked, scores, n=20)
+        assert bool((got.tokens == got.tokens[:1]).all()) and bool((got.parents == got.parents[:1]).all())
+
+
 @pytest.mark.parametrize("order", ["rising", "falling", "equal", "two"])
 @pytest.mark.parametrize("V", [300, 9000])
 @pytest.mark.parametrize("n", [1, 8, 60])
