@@ -3,14 +3,17 @@
 //
 // Memory-bound for many tokens, a latency for few.  A workgroup takes the work of
 // some tokens, or a part of one's: pieces of eight pairs of a head (two loads and
-// two stores of 16 bytes), and pieces of eight elements that are only copied (what
+// two stores of 16 bytes), and pieces of sixteen elements that are only copied (what
 // lies behind the pairs, and the values).  The sine and cosine of a pair are the
 // same in all heads, so they are computed once a workgroup, into LDS.  The angle's
 // turn is taken in binary64: a binary32 product of position 100000 and a frequency
 // is off by 4e-3, and one in 64 bits costs a few instructions a pair.
 //
-// A piece that the pairs do not fill is moved by elements.  No piece is loaded by
-// a lane that another lane stores, so the outputs may be the inputs.
+// Where the last piece would not be whole it is moved back to end with the pairs (or
+// the head), and some elements are computed and written twice, alike.  In place that
+// would turn them twice, so it is done by elements there (8192 tokens of 40 heads
+// with 37 pairs: PLACEHOLDER).  No piece is loaded by a lane that another lane stores,
+// so the outputs may be the inputs.
 #include "step.h"
 
 namespace sbvr {
@@ -18,11 +21,28 @@ namespace sbvr {
 constexpr int ROTARY_THREADS = 256;
 
 struct RotaryShape {
-    int turned, copied, valued;  // pieces of a head that are turned, only copied, and of its values
+    int turned, copied, valued;  // pieces of a head that are turned, copied, and of its values
     int units;                   // pieces of a token
     int split, tokens;           // pieces and tokens of a workgroup (split < units: one token)
     int width;                   // pairs rounded up to pieces
 };
+
+// The two elements of a pair turned: spelt out and in binary32, so that they are
+// rounded alike however a piece is taken (the compiler would round some of them
+// straight to 16 bits).
+__device__ __forceinline__ float in_binary32(float v)
+{
+    asm("" : "+v"(v));
+    return v;
+}
+__device__ __forceinline__ float turned_first(float a, float b, float c, float s)
+{
+    return in_binary32(__builtin_fmaf(a, c, -(b * s)));
+}
+__device__ __forceinline__ float turned_second(float a, float b, float c, float s)
+{
+    return in_binary32(__builtin_fmaf(b, c, a * s));
+}
 
 // T: element type; EVEN: every piece is whole (pairs a multiple of 8); WRITE: keys
 // and values go into the cache.
@@ -81,19 +101,28 @@ __global__ void __launch_bounds__(ROTARY_THREADS) rotary_kernel(RotaryArgs args,
                 out = key ? (T *)a.k_out + t * a.k_out_token_stride + head * a.k_out_head_stride
                           : (T *)a.q_out + t * a.q_out_token_stride + head * a.q_out_head_stride;
             }
+            const bool in_place = out == in;
             if (!turns) {
-                const int at = (value ? 0 : 2 * n) + 8 * piece;
-                if (!keep)
+                const int base = value ? 0 : 2 * n;
+                int at = base + 16 * piece;
+                if (!keep || in_place)
                     continue;
-                if (EVEN || value || at + 8 <= a.head_dim)
-                    store_words(out + at, load_words(in + at));
-                else
-                    for (int e = at; e < a.head_dim; ++e)
-                        out[e] = in[e];
+                if (at + 16 > a.head_dim && a.head_dim - base >= 16)
+                    at = a.head_dim - 16;
+                if (at + 16 <= a.head_dim) {
+                    const Words<T> w0 = load_words(in + at), w1 = load_words(in + at + 8);
+                    store_words(out + at, w0);
+                    store_words(out + at + 8, w1);
+                } else {
+                    for (; at + 8 <= a.head_dim; at += 8)
+                        store_words(out + at, load_words(in + at));
+                    for (; at < a.head_dim; ++at)
+                        out[at] = in[at];
+                }
                 continue;
             }
-            const float *c = cosine + dt * s.width + 8 * piece, *sn = sine + dt * s.width + 8 * piece;
-            const int p0 = 8 * piece;
+            const int p0 = EVEN || 8 * piece + 8 <= n || n < 8 || in_place ? 8 * piece : n - 8;
+            const float *c = cosine + dt * s.width + p0, *sn = sine + dt * s.width + p0;
             if (EVEN || p0 + 8 <= n) {
                 const int a0 = a.interleaved ? 2 * p0 : p0, b0 = a.interleaved ? 2 * p0 + 8 : n + p0;
                 const Loose<T, 8> x = from_words<T>(load_words(in + a0)), y = from_words<T>(load_words(in + b0));
@@ -102,18 +131,18 @@ __global__ void __launch_bounds__(ROTARY_THREADS) rotary_kernel(RotaryArgs args,
     #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         const float u = (float)x.e[2 * e], v = (float)x.e[2 * e + 1];
-                        xo.e[2 * e] = (T)(u * c[e] - v * sn[e]);
-                        xo.e[2 * e + 1] = (T)(v * c[e] + u * sn[e]);
+                        xo.e[2 * e] = (T)turned_first(u, v, c[e], sn[e]);
+                        xo.e[2 * e + 1] = (T)turned_second(u, v, c[e], sn[e]);
                         const float w = (float)y.e[2 * e], z = (float)y.e[2 * e + 1];
-                        yo.e[2 * e] = (T)(w * c[e + 4] - z * sn[e + 4]);
-                        yo.e[2 * e + 1] = (T)(z * c[e + 4] + w * sn[e + 4]);
+                        yo.e[2 * e] = (T)turned_first(w, z, c[e + 4], sn[e + 4]);
+                        yo.e[2 * e + 1] = (T)turned_second(w, z, c[e + 4], sn[e + 4]);
                     }
                 } else {
     #pragma unroll
                     for (int e = 0; e < 8; ++e) {
                         const float u = (float)x.e[e], v = (float)y.e[e];
-                        xo.e[e] = (T)(u * c[e] - v * sn[e]);
-                        yo.e[e] = (T)(v * c[e] + u * sn[e]);
+                        xo.e[e] = (T)turned_first(u, v, c[e], sn[e]);
+                        yo.e[e] = (T)turned_second(u, v, c[e], sn[e]);
                     }
                 }
                 if (keep) {
@@ -124,8 +153,8 @@ __global__ void __launch_bounds__(ROTARY_THREADS) rotary_kernel(RotaryArgs args,
                 for (int p = p0; p < n; ++p) {
                     const int ia = a.interleaved ? 2 * p : p, ib = a.interleaved ? 2 * p + 1 : n + p;
                     const float u = (float)in[ia], v = (float)in[ib];
-                    out[ia] = (T)(u * c[p - p0] - v * sn[p - p0]);
-                    out[ib] = (T)(v * c[p - p0] + u * sn[p - p0]);
+                    out[ia] = (T)turned_first(u, v, c[p - p0], sn[p - p0]);
+                    out[ib] = (T)turned_second(u, v, c[p - p0], sn[p - p0]);
                 }
             }
         }
@@ -138,8 +167,8 @@ int run_rotary(const RotaryArgs &a, hipStream_t stream)
     const sbvr_rotary_args &r = a.r;
     RotaryShape s;
     s.turned = (r.pairs + 7) / 8;
-    s.copied = (r.head_dim - 2 * r.pairs + 7) / 8;
-    s.valued = r.head_dim / 8;
+    s.copied = (r.head_dim - 2 * r.pairs + 15) / 16;
+    s.valued = (r.head_dim + 15) / 16;
     s.width = 8 * s.turned;
     s.units = (r.heads + r.kv_heads) * (s.turned + s.copied) + (WRITE ? r.kv_heads * s.valued : 0);
     // four pieces a thread where there are many tokens, one where there are few
