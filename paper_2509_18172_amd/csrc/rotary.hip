@@ -21,7 +21,7 @@ namespace sbvr {
 constexpr int ROTARY_THREADS = 256;
 
 struct RotaryShape {
-    int turned, copied, valued;  // pieces of a head that are turned, copied, and of its values
+    int turned, per_head, valued;  // pieces of a head that are turned, all of it, and of its values
     int units;                   // pieces of a token
     int split, tokens;           // pieces and tokens of a workgroup (split < units: one token)
     int width;                   // pairs rounded up to pieces
@@ -72,17 +72,17 @@ __global__ void __launch_bounds__(ROTARY_THREADS) rotary_kernel(RotaryArgs args,
         __syncthreads();
 
         const int first = blockIdx.y * s.split, last = min(first + s.split, tokens * s.units);
-        const int turned = heads * s.turned, copied = heads * s.copied;
         for (int i = first + (int)threadIdx.x; i < last; i += ROTARY_THREADS) {
             const int dt = small_div(i, s.units, 1.f / (float)s.units);
             const long long t = t0 + dt;
             int j = i - dt * s.units;
-            // which head, and which piece of it
-            const bool turns = j < turned, value = WRITE && j >= turned + copied;
-            const int per = turns ? s.turned : value ? s.valued : s.copied;
-            j -= turns ? 0 : value ? turned + copied : turned;
-            int head = small_div(j, per, 1.f / (float)per);
-            const int piece = j - head * per;
+            // which head, and which piece of it: the pieces of a head lie together
+            const bool value = WRITE && j >= heads * s.per_head;
+            j -= value ? heads * s.per_head : 0;
+            const int per = value ? s.valued : s.per_head;
+            int head = small_div(j, per, 1.f / (float)per), piece = j - head * per;
+            const bool turns = !value && piece < s.turned;
+            piece -= turns || value ? 0 : s.turned;
             const bool key = value || head >= a.heads;
             head -= !value && key ? a.heads : 0;
             const T *in = value ? (const T *)args.v + t * args.v_token_stride + head * args.v_head_stride
@@ -102,33 +102,21 @@ __global__ void __launch_bounds__(ROTARY_THREADS) rotary_kernel(RotaryArgs args,
                           : (T *)a.q_out + t * a.q_out_token_stride + head * a.q_out_head_stride;
             }
             const bool in_place = out == in;
-            if (!turns) {
-                const int base = value ? 0 : 2 * n;
-                int at = base + 16 * piece;
-                if (!keep || in_place)
-                    continue;
-                if (at + 16 > a.head_dim && a.head_dim - base >= 16)
-                    at = a.head_dim - 16;
-                if (at + 16 <= a.head_dim) {
-                    const Words<T> w0 = load_words(in + at), w1 = load_words(in + at + 8);
-                    store_words(out + at, w0);
-                    store_words(out + at + 8, w1);
-                } else {
-                    for (; at + 8 <= a.head_dim; at += 8)
-                        store_words(out + at, load_words(in + at));
-                    for (; at < a.head_dim; ++at)
-                        out[at] = in[at];
-                }
+            // what is copied in place stays; both kinds load and store two pieces
+            if (!keep || (in_place && !turns))
                 continue;
-            }
-            const int p0 = EVEN || 8 * piece + 8 <= n || n < 8 || in_place ? 8 * piece : n - 8;
+            const int base = value ? 0 : 2 * n, end = a.head_dim;
+            const int p0 = !turns ? 0 : EVEN || 8 * piece + 8 <= n || n < 8 || in_place ? 8 * piece : n - 8;
+            const int at = base + 16 * piece + 16 > end && end - base >= 16 ? end - 16 : base + 16 * piece;
             const float *c = cosine + dt * s.width + p0, *sn = sine + dt * s.width + p0;
-            if (EVEN || p0 + 8 <= n) {
-                const int a0 = a.interleaved ? 2 * p0 : p0, b0 = a.interleaved ? 2 * p0 + 8 : n + p0;
-                const Loose<T, 8> x = from_words<T>(load_words(in + a0)), y = from_words<T>(load_words(in + b0));
+            if (turns ? EVEN || p0 + 8 <= n : at + 16 <= end) {
+                const int a0 = !turns ? at : a.interleaved ? 2 * p0 : p0;
+                const int b0 = !turns ? at + 8 : a.interleaved ? 2 * p0 + 8 : n + p0;
+                const Words<T> wx = load_words(in + a0), wy = load_words(in + b0);
+                const Loose<T, 8> x = from_words<T>(wx), y = from_words<T>(wy);
                 Loose<T, 8> xo, yo;
                 if (a.interleaved) {
-    #pragma unroll
+#pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         const float u = (float)x.e[2 * e], v = (float)x.e[2 * e + 1];
                         xo.e[2 * e] = (T)turned_first(u, v, c[e], sn[e]);
@@ -138,24 +126,28 @@ __global__ void __launch_bounds__(ROTARY_THREADS) rotary_kernel(RotaryArgs args,
                         yo.e[2 * e + 1] = (T)turned_second(w, z, c[e + 4], sn[e + 4]);
                     }
                 } else {
-    #pragma unroll
+#pragma unroll
                     for (int e = 0; e < 8; ++e) {
                         const float u = (float)x.e[e], v = (float)y.e[e];
                         xo.e[e] = (T)turned_first(u, v, c[e], sn[e]);
                         yo.e[e] = (T)turned_second(u, v, c[e], sn[e]);
                     }
                 }
-                if (keep) {
-                    store_words(out + a0, to_words(xo));
-                    store_words(out + b0, to_words(yo));
-                }
-            } else if (keep) {
-                for (int p = p0; p < n; ++p) {
+                store_words(out + a0, turns ? to_words(xo) : wx);
+                store_words(out + b0, turns ? to_words(yo) : wy);
+            } else if (turns) {
+                for (int p = p0; p < min(p0 + 8, n); ++p) {
                     const int ia = a.interleaved ? 2 * p : p, ib = a.interleaved ? 2 * p + 1 : n + p;
                     const float u = (float)in[ia], v = (float)in[ib];
                     out[ia] = (T)turned_first(u, v, c[p - p0], sn[p - p0]);
                     out[ib] = (T)turned_second(u, v, c[p - p0], sn[p - p0]);
                 }
+            } else {
+                int e = at;
+                for (; e + 8 <= end; e += 8)
+                    store_words(out + e, load_words(in + e));
+                for (; e < end; ++e)
+                    out[e] = in[e];
             }
         }
     }
@@ -167,10 +159,10 @@ int run_rotary(const RotaryArgs &a, hipStream_t stream)
     const sbvr_rotary_args &r = a.r;
     RotaryShape s;
     s.turned = (r.pairs + 7) / 8;
-    s.copied = (r.head_dim - 2 * r.pairs + 15) / 16;
+    s.per_head = s.turned + (r.head_dim - 2 * r.pairs + 15) / 16;
     s.valued = (r.head_dim + 15) / 16;
     s.width = 8 * s.turned;
-    s.units = (r.heads + r.kv_heads) * (s.turned + s.copied) + (WRITE ? r.kv_heads * s.valued : 0);
+    s.units = (r.heads + r.kv_heads) * s.per_head + (WRITE ? r.kv_heads * s.valued : 0);
     // four pieces a thread where there are many tokens, one where there are few
     const int target = (long long)r.T * s.units > 1024ll * ROTARY_THREADS ? 4 * ROTARY_THREADS : ROTARY_THREADS;
     s.tokens = s.units > target ? 1 : target / s.units;
