@@ -340,6 +340,7 @@ __global__ void __launch_bounds__(BEAM_THREADS, 6) beam_part_kernel(sbvr_beam_ar
         }
         __syncthreads();
         int c = count;
+        const bool more = c > have;
         const uint64_t *from = list;
         if (c > BEAM_LIST) {
             // too many alike: the value to the last bit, those above it, and the first
@@ -414,7 +415,7 @@ __global__ void __launch_bounds__(BEAM_THREADS, 6) beam_part_kernel(sbvr_beam_ar
             from = kept;
             c = s.keep;
         }
-        if (c > have || from == kept) {
+        if (more) {
             uint64_t key[BEAM_RANKED / BEAM_THREADS];
             int better[BEAM_RANKED / BEAM_THREADS] = {};
 #pragma unroll

@@ -306,6 +306,36 @@ def test_random(seed):
     check(logits, scores, n, ends=rng.integers(0, V, int(rng.integers(0, 5))).tolist())
 
 
+def test_equal_best_among_many_close_ones():
+    """Each tile better than those before, its four best equal, all others so close that
+    they are listed first: of equal ones the lower token is the better."""
+    V, B = 8192 * 15, 32
+    rng = np.random.default_rng(0)
+    scores = torch.full((1, B), -100.0, device=DEV)
+    scores[0, 5] = 0
+    for trial in range(100):
+        # tile t from 1 + 1000 t 2^-23 on: all of them 1 to 7 bits behind the point
+        base = np.arange(V) // 2048 * 1000 + rng.integers(0, 999, V)
+        best = V - 2048 + rng.permutation(2048)[:4]
+        base[best] = 60 * 1000
+        row = torch.from_numpy((1 + base * 2.0 ** -23).astype(np.float32))
+        got = sb.beam_select(row.to(DEV).expand(B, V).contiguous(), scores, n=4)
+        assert got.tokens[0].tolist() == sorted(best.tolist()), trial
+        assert got.parents[0].tolist() == [5] * 4
+
+
+def test_offsets_past_32_bits():
+    """More than 2^31 logits: the last rows are as if they were alone."""
+    V, rows = 60_000_001, 37
+    logits = torch.empty(rows, V, dtype=F16, device=DEV).normal_(generator=torch.Generator(device=DEV).manual_seed(0))
+    logits[-1, [3, V - 1, 77]] = torch.tensor([20.0, 19.0, 18.0], dtype=F16, device=DEV)
+    scores = torch.zeros(rows, 1, device=DEV)
+    got, alone = sb.beam_select(logits, scores, n=5), sb.beam_select(logits[-2:].contiguous(), scores[-2:], n=5)
+    assert got.tokens[-1, :3].tolist() == [3, V - 1, 77]
+    assert torch.equal(got.tokens[-2:], alone.tokens)
+    assert float((got.scores[-2:] - alone.scores).abs().max()) <= 2 * close(20.0)
+
+
 def test_the_same_call_gives_the_same_bits():
     logits, scores = make(16, 8, 30000, F16, seed=8)
     a = sb.beam_select(logits, scores, n=16)
