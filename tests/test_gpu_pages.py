@@ -258,6 +258,14 @@ def test_compact_of_most_rows():
     check_compact(rng.integers(0, 300, 4096).tolist(), rng.integers(0, 40000, (4096, 20)).tolist(), 16, 40000)
 
 
+@pytest.mark.parametrize("R,width,pages", [(4096, 70, 5000), (4096, 65, 131072), (10, 5, 131073), (300, 1000, 70000)])
+def test_compact_many_entries(R, width, pages):
+    rng = np.random.default_rng(R)
+    lens = rng.integers(0, width * 16 + 30, R)
+    lens[rng.random(R) < 0.7] //= 20
+    check_compact(lens.tolist(), rng.integers(-1, pages + 1, (R, width)).tolist(), 16, pages, stride=width + 2)
+
+
 def test_compact_without_rows():
     c = sb.page_compact(i32([]), torch.empty(0, 4, dtype=torch.int32, device=DEV), 16, 10)
     assert c.src.tolist() == [-1] * 5 and c.dst.tolist() == [-1] * 5 and c.counts.tolist() == [0, 0]
@@ -312,6 +320,27 @@ def test_copy_of_one_cache_and_of_nothing():
     want[3] = want[1]
     sb.page_copy(made[0], i32([1]), i32([3]))
     assert torch.equal(made[0].k, want)
+
+
+def test_copy_between_layouts():
+    """Keys head by head, values token by token."""
+    made = caches(2, 9, 32, 4, 64, layout="head")
+    other = caches(2, 9, 32, 4, 64, layout="token", seed=1)
+    check_copy([sb.KVCache(a.k, b.v) for a, b in zip(made, other)], [0, 5], [3, 1], [32, 7])
+    check_copy([sb.KVCache(b.k, a.v) for a, b in zip(made, other)], [0, 5], [3, 1], [9, 32])
+
+
+def test_copy_past_32_bits():
+    """Pages whose elements' numbers pass 2^31."""
+    P, heads, dim, pages = 64, 8, 128, 2 ** 31 // (64 * 8 * 128) + 3
+    cache = sb.KVCache.alloc(pages, P, heads, dim)
+    for t in (cache.k, cache.v):
+        t[pages - 2:].normal_()
+        t[:2].normal_()
+    want = [(t[pages - 1].clone(), t[1].clone()) for t in (cache.k, cache.v)]
+    sb.page_copy(cache, i32([pages - 1, 1]), i32([0, pages - 2]))
+    for t, (high, low) in zip((cache.k, cache.v), want):
+        assert torch.equal(t[0], high) and torch.equal(t[pages - 2], low) and torch.equal(t[pages - 1], high)
 
 
 def test_copy_of_many():

@@ -233,6 +233,19 @@ def test_rotary_write(T, H, K, D, n, P, dtype, layout, interleaved):
     assert torch.equal(q, want_q)
 
 
+def test_rotary_write_past_32_bits():
+    """Slots whose elements' numbers pass 2^31."""
+    P, K, D = 64, 8, 128
+    pages = 2 ** 31 // (P * K * D) + 3
+    q, k, v = qkv(3, 8, K, D, F16)
+    cache = sb.KVCache.alloc(pages, P, K, D)
+    slots, pos = torch.tensor([pages * P - 1, 5, (pages - 1) * P], device=DEV), i32([9, 100, 70000])
+    _, want = sb.rotary(q, k, pos, frequencies(64))
+    sb.rotary_write(q, cache, k, v, slots, pos, frequencies(64))
+    for t, w in ((cache.k, want), (cache.v, v)):
+        assert torch.equal(torch.stack([t[s // P, s % P] for s in slots.tolist()]), w)
+
+
 def test_rotary_write_axes_and_inverse():
     T, K, D, n, P = 20, 2, 64, 32, 16
     q, k, v = qkv(T, 4, K, D, F16)
