@@ -26,7 +26,7 @@
 
 namespace sbvr {
 
-constexpr int BEAM_THREADS = 256, BEAM_WAVES = BEAM_THREADS / 64, BEAM_ENTRIES = 3072;  // of a request's parts together
+constexpr int BEAM_THREADS = 256, BEAM_WAVES = BEAM_THREADS / 64, BEAM_ENTRIES = 2816;  // of a request's parts together
 constexpr int BEAM_RANKED = 2 * BEAM_THREADS, BEAM_LIST = 2048 + SBVR_BEAM_KEEP_MAX;  // logits to be ranked, and to be thinned out before
 constexpr float LOG2E = 1.44269502f, LARGEST = 3.402823466e38f;
 
@@ -474,7 +474,7 @@ template <int THREADS>
 __global__ void __launch_bounds__(THREADS) beam_join_kernel(sbvr_beam_args a, BeamShape s, const PartSum *sums,
                                                             const uint64_t *entries)
 {
-    constexpr int PER = THREADS == 1024 ? BEAM_ENTRIES / 1024 : 4, WAVES = THREADS / 64;
+    constexpr int PER = THREADS == 1024 ? (BEAM_ENTRIES + 1023) / 1024 : 4, WAVES = THREADS / 64;
     constexpr uint32_t END = 1u << 31;
     extern __shared__ double list_score[];  // and behind them, each entry's place, beam and whether it is an end, and its token
     __shared__ double add[SBVR_BEAMS_MAX], beam_reference[SBVR_BEAMS_MAX];
