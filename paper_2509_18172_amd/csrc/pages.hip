@@ -133,10 +133,11 @@ __device__ __forceinline__ void each_page(const PageTable &t, int split, int spl
 // many pages is made by a last launch, where each workgroup adds up the used pages
 // before its own.
 constexpr int USAGE_PAGES = 11264, SHARE = USAGE_PAGES / PAGE_WAVES;  // SHARE: pages of a wavefront, or of a later launch's workgroup
-#ifndef USAGE_CHUNKS
-#define USAGE_CHUNKS 256
-#endif
-constexpr int USAGE_SPLITS = 16, USAGE_GROUPS = 256;
+// A part has USAGE_CHUNKS chunks or more: splitting pays from 32768 entries on (of
+// 11264 pages, 12.0 us either way; 16384 entries 9.8 us whole, 11.9 in two parts;
+// 65536 of 65536 pages 17.9 whole, 12.6 in four).  1024 rows of 8192 tokens (524288
+// entries): 16.9 us, 77.9 whole, of which the table's 2 MB are the least.
+constexpr int USAGE_CHUNKS = 256, USAGE_SPLITS = 16, USAGE_GROUPS = 256;
 
 // The list of free pages for the pages first .. first + n, by one wavefront; `used`
 // of the lower ones are, and `total` of all.
@@ -435,14 +436,11 @@ __device__ __forceinline__ void renumber_entries(const CompactArgs &a, int used,
 // Few pages and entries: one workgroup marks the used pages in LDS, finds the moves
 // -- the k-th free page below the number of used ones is dst[k], the k-th used page
 // from there on src[k], and number[p] = k for that -- and, if `whole`, rewrites the
-// tables too.
-#ifndef COMPACT_ENTRIES
-#define COMPACT_ENTRIES 262144
-#endif
-#ifndef COMPACT_WHOLE
-#define COMPACT_WHOLE 16384
-#endif
-constexpr int COMPACT_PAGES = 131072;
+// tables too.  Measured: 1024 entries 6.2 us whole, 7.5 with a second launch for the
+// tables; 4096 9.9 and 9.5; 16384 25.3 and 16.4.  131072 entries 55 us in two launches,
+// 58 with the marks in memory; 262144 73 and 64; 1048576 193 and 115.
+constexpr int COMPACT_WHOLE = 2048, COMPACT_ENTRIES = 131072;
+constexpr int COMPACT_PAGES = 131072;  // whose marks, and their sums, LDS holds
 
 __global__ void __launch_bounds__(PAGE_THREADS) compact_kernel(CompactArgs a, int whole)
 {
