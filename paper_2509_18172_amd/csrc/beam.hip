@@ -22,11 +22,18 @@
 // log2 e is 1.4e-8 of the exponent; between a request's beams nearly all of that
 // cancels.)  Binary32 within a lane and a tile, binary64 between lanes, tiles and
 // parts: two continuations' order may hang on the last bits.
+//
+// Memory-bound for many rows: 245 rows of 131072 in binary32 (128 MB, 20 to 21 us of a
+// plain read) take 31 us, in binary16 26; of that 3 to 5 are the join, the rest above
+// the read the beginning of the workgroups and, in binary16, the exponentials.  Few
+// rows are a chain of latencies: four rows of 50001 8.8 us, an empty launch 2.1.
 #include "step.h"
 
 namespace sbvr {
 
-constexpr int BEAM_THREADS = 256, BEAM_WAVES = BEAM_THREADS / 64, BEAM_ENTRIES = 2816;  // of a request's parts together
+// BEAM_ENTRIES: of a request's parts together, which the join holds in registers and,
+// if need be, in LDS
+constexpr int BEAM_THREADS = 256, BEAM_WAVES = BEAM_THREADS / 64, BEAM_ENTRIES = 2816;
 constexpr int BEAM_RANKED = 2 * BEAM_THREADS, BEAM_LIST = 2048 + SBVR_BEAM_KEEP_MAX;  // logits to be ranked, and to be thinned out before
 constexpr float LOG2E = 1.44269502f, LARGEST = 3.402823466e38f;
 
@@ -276,7 +283,8 @@ __global__ void __launch_bounds__(BEAM_THREADS, 6) beam_part_kernel(sbvr_beam_ar
         if ((tid & 3) == 0)
             groups[tid >> 2] = in_group;
         // many to keep: the 64 groups' maxima are no close bound, the lanes' of each
-        // wavefront are
+        // wavefront are (128 rows of 131072 in binary16: 64 kept 57.7 us, by the groups
+        // 59.9; 48 alike; 32 29.3 by the groups, 30.4)
         const bool many = s.keep > 32;
         if (many) {
             const uint32_t reached = reached_by(ordered(best), (s.keep + WAVES - 1) / WAVES, 16);
@@ -549,8 +557,10 @@ __global__ void __launch_bounds__(THREADS) beam_join_kernel(sbvr_beam_args a, Be
         score[i] = (place < all) & (key[i] != 0) & (add[beam[i]] > -INFINITY) ? value : -INFINITY;
         mine = fmaxf(mine, key[i] & END_ENTRY ? (float)score[i] : -INFINITY);
     }
-    // (a group is every 64th or 256th thread: neighbours are of one list, in order)
-    const int groups = a.n > 16 ? 256 : 64, slot = tid & (groups - 1), share = groups * groups / THREADS;
+    // A group is every 64th or 256th thread: neighbours are of one list, in order.
+    // (16 requests of 8 beams of 131072: n = 8 takes 18.5 us, with 256 groups 20.6; 14
+    // 19.0 and 20.2; 16 21.2 so, with 64 groups 26.6.)
+    const int groups = a.n >= 16 ? 256 : 64, slot = tid & (groups - 1), share = groups * groups / THREADS;
     if (mine > -INFINITY)
         atomicMax(&group[slot], ordered(mine));
     __syncthreads();
@@ -625,10 +635,12 @@ __global__ void __launch_bounds__(THREADS) beam_join_kernel(sbvr_beam_args a, Be
 
 namespace {
 
-// pieces of a thread: large tiles where their workgroups fill the chip
+// pieces of a thread: large tiles unless that leaves half of the chip empty (binary16,
+// 8 beams: 8 rows of 131072 take 10.5 us with four, 12.2 with one; 256 rows 26 and 47;
+// 16 of 32000 10.7 and 10.1)
 int beam_pieces(long long rows, int V)
 {
-    return rows * ((V + 8191ll) / 8192) >= 512 ? 4 : 1;
+    return rows * ((V + 8191ll) / 8192) >= 128 ? 4 : 1;
 }
 
 BeamShape beam_shape(int R, int B, int V, int n, int n_end)

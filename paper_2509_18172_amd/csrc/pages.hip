@@ -315,7 +315,9 @@ int launch_usage(const UsageArgs &a, hipStream_t stream)
 // ---------------------------------------------------------------------------
 
 // Every workgroup finds which rows need a page, and how many do before each; then
-// it writes its share of the rows.
+// it writes its share of the rows.  A chain of latencies -- parents and free pages,
+// lengths, table, scan, table again: 4 rows of 63 pages with their copies 5.6 us in
+// two launches of which an empty one is 2.1.
 template <int THREADS, int PER>
 __global__ void __launch_bounds__(THREADS) fork_kernel(ForkArgs a)
 {
@@ -633,7 +635,10 @@ struct CopyArgs {
 };
 
 // A workgroup takes `chunk` tokens of a page, in one cache's keys or values: X lanes
-// for a token's pieces by Y tokens, as in the cache write.
+// for a token's pieces by Y tokens, as in the cache write.  Stores go past the caches
+// (484 MB of forked pages in 8 layers: 129 us, 133 through them); loads do not (copies
+// that fit in the caches 12.8 us, 13.8 past them).  256 rows of 4096 tokens compacted in
+// two layers, 3.0 GB: 606 us together, 4.95 TB/s -- what a plain copy reaches.
 __global__ void __launch_bounds__(COPY_THREADS) page_copy_kernel(CopyArgs a)
 {
     const int layer = blockIdx.z >> 1, is_v = blockIdx.z & 1, first = blockIdx.y * a.chunk;
