@@ -191,9 +191,9 @@ def beam_select(logits, scores, n=None, end_tokens=None, out=None, workspace=Non
     """The n (default: as many as beams) best continuations of each request's
     beams: logits [R * B][V] (fp16, bf16 or fp32), scores fp32 [R][B] the
     beams' log probabilities (-infinity: no such beam), end_tokens int32 [E]:
-    tokens that end a beam.  out: a BeamChoice of the same sizes to fill;
-    workspace: a uint8 tensor of sbvr_beam_select_workspace_bytes, by default a
-    new one."""
+    tokens that end a beam.  out: a BeamChoice of the same sizes to fill, whose
+    scores may be the old ones where n is their number; workspace: a uint8
+    tensor of sbvr_beam_select_workspace_bytes, by default a new one."""
     given = None if out is None else [getattr(out, name) for name in BeamChoice.__slots__]
     made = _native.beam_select(logits, scores, n, end_tokens, given, workspace, stream)
     return BeamChoice(*made) if out is None else out

@@ -324,6 +324,18 @@ def test_equal_best_among_many_close_ones():
         assert got.parents[0].tolist() == [5] * 4
 
 
+@pytest.mark.parametrize("R,B,V", [(1, 4, 1000), (40, 8, 5001), (2047, 32, 100), (3, 32, 60000)])
+def test_scores_in_place(R, B, V):
+    logits = torch.randn(R * B, V, device=DEV, generator=torch.Generator(device=DEV).manual_seed(R))
+    scores = torch.randn(R, B, device=DEV, generator=torch.Generator(device=DEV).manual_seed(V))
+    want = sb.beam_select(logits, scores)
+    out = sb.BeamChoice(*(torch.empty_like(getattr(want, n)) for n in sb.BeamChoice.__slots__))
+    out.scores = scores
+    sb.beam_select(logits, scores, out=out)
+    for n in sb.BeamChoice.__slots__:
+        assert torch.equal(getattr(out, n), getattr(want, n)), n
+
+
 def test_offsets_past_32_bits():
     """More than 2^31 logits: the last rows are as if they were alone."""
     V, rows = 60_000_001, 37
