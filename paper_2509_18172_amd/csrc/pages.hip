@@ -402,8 +402,12 @@ int launch_fork(const ForkArgs &a, hipStream_t stream)
     const long long items = (long long)a.rows_out * ((a.t.max_pages + threads - 1) / threads);
     const int most = 256 * 1024 / threads;
     const unsigned grid = items < 1 ? 1 : items < most ? (unsigned)items : most;
-    return rows <= 256 ? launch_kernel((const void *)fork_kernel<256, 1>, dim3(grid), dim3(256), 0, stream, argv)
-                       : launch_kernel((const void *)fork_kernel<1024, 4>, dim3(grid), dim3(1024), 0, stream, argv);
+    // as few rows a thread as can be: 512 rows of 40 pages take 4.3 us with one, 5.8 with
+    // four (256 threads of four: 5.3), 1000 rows of 1024 pages 6.5 and 7.8
+    const void *kernel = rows <= 256    ? (const void *)fork_kernel<256, 1>
+                         : rows <= 1024 ? (const void *)fork_kernel<1024, 1>
+                                        : (const void *)fork_kernel<1024, 4>;
+    return launch_kernel(kernel, dim3(grid), dim3(threads), 0, stream, argv);
 }
 
 // ---------------------------------------------------------------------------
@@ -636,7 +640,7 @@ struct CopyArgs {
 
 // A workgroup takes `chunk` tokens of a page, in one cache's keys or values: X lanes
 // for a token's pieces by Y tokens, as in the cache write.  Stores go past the caches
-// (484 MB of forked pages in 8 layers: 129 us, 133 through them); loads do not (copies
+// (484 MB of forked pages in 8 layers: 126 us with the fork, 130 through them); loads do not (copies
 // that fit in the caches 12.8 us, 13.8 past them).  256 rows of 4096 tokens compacted in
 // two layers, 3.0 GB: 606 us together, 4.95 TB/s -- what a plain copy reaches.
 __global__ void __launch_bounds__(COPY_THREADS) page_copy_kernel(CopyArgs a)

@@ -197,6 +197,16 @@ def test_fork_of_most_rows():
     check_fork(lens, rng.integers(0, 9999, (4096, 20)).tolist(), rng.integers(0, 8, (512, 8)).tolist(), 16, list(range(5000)))
 
 
+@pytest.mark.parametrize("rows", [255, 256, 257, 1023, 1024, 1025])
+def test_fork_rows_of_a_kernel(rows):
+    """Up to the rows that a kernel takes, and one more, old and new."""
+    rng = np.random.default_rng(rows)
+    lens, table = rng.integers(0, 70, rows).tolist(), rng.integers(0, 9999, (rows, 5)).tolist()
+    check_fork(lens, table, rng.integers(0, rows, (1, rows)).tolist(), 16, list(range(2000)))
+    check_fork(lens[:3], table[:3], rng.integers(0, 3, (1, rows)).tolist(), 16, list(range(2000)))
+    check_fork(lens, table, rng.integers(0, rows, (1, 3)).tolist(), 16, list(range(2000)))
+
+
 def test_fork_from_no_rows():
     f = sb.page_fork(i32([]), torch.empty(0, 4, dtype=torch.int32, device=DEV), i32([[0, 1]]), 16, i32([3]))
     assert f.page_table.tolist() == [[-1] * 4] * 2 and f.context_lens.tolist() == [0, 0] and f.used.tolist() == [0]
