@@ -191,6 +191,24 @@ def test_many_rows_of_equal_logits():
     assert torch.equal(got.tokens, few.tokens.expand(260, 30)) and torch.equal(got.parents, few.parents.expand(260, 30))
 
 
+@pytest.mark.parametrize("kind", ["equal", "beams", "near", "few"])
+@pytest.mark.parametrize("n", [1, 4, 16, 50])
+def test_equal_lists_of_many_parts(kind, n):
+    """A request whose parts' entries are all as good, or nearly: the join thins them out
+    too.  Score differences are exact in binary64, rows are the same for all beams."""
+    B, V = 8, 70001
+    row = torch.zeros(V, device=DEV)
+    if kind == "near":
+        row += torch.randint(0, 1000, (V,), generator=torch.Generator(device=DEV).manual_seed(n), device=DEV) * 2.0 ** -30
+    if kind == "few":
+        row[[5, 30000, 70000]] = 0.125
+    scores = torch.full((2, B), -1.0, device=DEV)
+    if kind == "beams":
+        scores[0, [2, 7]] = -0.75
+        scores[1, 3] = -INF
+    check(row.expand(2 * B, V).contiguous(), scores, n, ends=(0, 3, 30000, V - 1), exact=True)
+
+
 @pytest.mark.parametrize("V", [100, 2500, 9000])
 def test_masked_rows(V):
     """Rows and beams that leave nothing, or less than is asked for."""
