@@ -314,8 +314,8 @@ __global__ void __launch_bounds__(BEAM_THREADS, 6) beam_part_kernel(sbvr_beam_ar
         if (tile_top > -INFINITY) {  // the same for all
             tile_top = fminf(tile_top, LARGEST);
             // differences instead where c is so large that 2 to its rounding is (2^-25 of
-            // c: 0.04 at a million)
-            const bool huge = fabsf(tile_top) > 1e6f || (fabsf(top) > 1e6f && top > -INFINITY);
+            // c: 0.04 at a million); the largest so far, whose c this tile takes, decides
+            const bool huge = fabsf(fmaxf(tile_top, top)) > 1e6f;
             if (tile_top > top) {
                 const double now = huge ? (double)tile_top : (double)(tile_top * LOG2E) * (1. / (double)LOG2E);
                 total *= exp_of(reference - now);  // (0 before the first)

@@ -342,6 +342,36 @@ def test_equal_best_among_many_close_ones():
         assert got.parents[0].tolist() == [5] * 4
 
 
+def parts_of(R, B, V, n, ends=0):
+    """Parts that the operator cuts a row into: its workspace is a sum of 16 bytes
+    and n + ends entries of 8 for each."""
+    need, each = sb.sbvr_beam_select_workspace_bytes(R, B, V, n, ends), R * B * (16 + 8 * (n + ends))
+    assert need % each == 0
+    return need // each
+
+
+@pytest.mark.parametrize("R,tile", [(1, 2048), (2, 8192)])
+@pytest.mark.parametrize("low", [-1e9, float(np.finfo(np.float32).min), -2e6, 1.0])
+@pytest.mark.parametrize("near", [111.0, 1000.0, 30000.0, 900000.0])
+def test_a_sum_of_several_tiles_refers_to_one_number(R, tile, low, near):
+    """A tile of masked logits, one that has the largest, one that has most of the sum:
+    the last two are of one part, and what rounding the largest's exponent (up to half
+    a unit of its last place: 5e-6 of the sum near 111, 1e-3 near 30000) does to one
+    it has to do to the other."""
+    B, n, V = 32, 64, 3 * tile
+    assert parts_of(R, B, V, n) == 1  # three tiles, or twelve
+    some = np.float32(near) + np.arange(1000, dtype=np.float32) * np.spacing(np.float32(near))
+    exponent = some.astype(np.float64) * float(np.float32(1.44269502))
+    top = some[np.abs(exponent.astype(np.float32) - exponent).argmax()]
+    row = np.full(V, low, np.float32)
+    row[tile:2 * tile] = top - np.float32(20)
+    row[tile + 77] = top
+    row[2 * tile:] = top - np.arange(tile, dtype=np.float32) % 64 / np.float32(16)
+    row[2 * tile::64] = top - np.float32(1 / 16)  # (the largest is in the tile before)
+    logits = torch.from_numpy(row).to(DEV).expand(R * B, V).contiguous()
+    check(logits, torch.zeros(R, B, device=DEV), n)
+
+
 @pytest.mark.parametrize("R,B,V", [(1, 4, 1000), (40, 8, 5001), (2047, 32, 100), (3, 32, 60000)])
 def test_scores_in_place(R, B, V):
     logits = torch.randn(R * B, V, device=DEV, generator=torch.Generator(device=DEV).manual_seed(R))
