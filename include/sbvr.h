@@ -722,7 +722,7 @@ int sbvr_page_usage(int R, int page_size, int n_pages, const int32_t *context_le
  *   src, dst, tokens  [rows_out] (output): the copies: page, page, and the number
  *               of tokens; -1, -1 and 0 for a row that needs none or found no page.
  *   used        [1] (output): pages that were needed.
- * Inputs and outputs must not overlap.
+ * Inputs and outputs must not overlap (an output that is an input is refused).
  */
 int sbvr_page_fork(int groups, int rows_in, int rows_out, int page_size, const int32_t *context_lens,
                    const int32_t *page_table, int max_pages, int64_t table_stride, const int32_t *parents,

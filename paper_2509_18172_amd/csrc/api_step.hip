@@ -407,14 +407,24 @@ int sbvr_page_fork(int groups, int rows_in, int rows_out, int page_size, const i
     if (st != SBVR_OK || (st = check_table_shape(rows_out, max_pages, out_stride, page_size)) != SBVR_OK)
         return st;
     if ((rows_in && (!context_lens || !page_table)) || (n_free && !free_pages) || !used ||
-        (rows_out && (!parents || !out_table || !out_lens || !src || !dst || !tokens)) ||
-        (rows_out && out_table == page_table))
+        (rows_out && (!parents || !out_table || !out_lens || !src || !dst || !tokens)))
         return SBVR_E_INVALID_ARG;
     const void *words[] = {context_lens, page_table, parents, free_pages, taken, out_table, out_lens, src, dst, tokens,
                            used};
     for (const void *p : words)
         if (!aligned(p, 4))
             return SBVR_E_ALIGNMENT;
+    // one workgroup writes the lengths and lists while others read what they come from
+    const void *read[] = {rows_in ? context_lens : nullptr, rows_in ? page_table : nullptr, rows_out ? parents : nullptr,
+                          n_free ? free_pages : nullptr, taken};
+    const void *written[] = {out_table, out_lens, src, dst, tokens};
+    for (const void *p : read) {
+        if (p && p == used)
+            return SBVR_E_INVALID_ARG;
+        for (const void *q : written)
+            if (p && p == q && rows_out)
+                return SBVR_E_INVALID_ARG;
+    }
     const PageTable t{rows_in, __builtin_ctz(page_size), max_pages, context_lens, page_table, table_stride};
     const ForkArgs a{t, rows_out, rows_in / groups, rows_out / groups > 0 ? rows_out / groups : 1, n_free, parents,
                      free_pages, taken, out_table, out_stride, out_lens, src, dst, tokens, used};

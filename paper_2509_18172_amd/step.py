@@ -237,8 +237,8 @@ def page_fork(context_lens, page_table, parents, page_size: int, free_pages, tak
     the groups); any other number makes an empty row.  Full pages are shared, a
     partly filled one is copied into one of free_pages for all but the first of
     a parent's rows; taken (int32, its first element counts): how many of
-    free_pages are gone.  out: a PageFork of the same sizes to fill, with a
-    page_table that is not the old one."""
+    free_pages are gone.  out: a PageFork of the same sizes to fill, of which
+    nothing may be an input (a captured step forks from one into another)."""
     given = None if out is None else [getattr(out, name) for name in PageFork.__slots__]
     made = _native.page_fork(context_lens, page_table, parents, page_size, free_pages, taken, given, stream)
     return PageFork(*made) if out is None else out

@@ -164,6 +164,17 @@ def test_fork_refusals(bad, status):
     assert fork(**bad) == status
 
 
+FORK_INPUTS, FORK_OUTPUTS = ("lens", "table", "parents", "free", "taken"), ("out", "out_lens", "src", "dst", "tokens", "used")
+
+
+@pytest.mark.parametrize("output", FORK_OUTPUTS)
+@pytest.mark.parametrize("given", FORK_INPUTS)
+def test_fork_in_place_is_refused(given, output):
+    """Every workgroup reads the inputs while the first one writes lengths and lists."""
+    apart = {name: FAKE + 4096 * i for i, name in enumerate(FORK_INPUTS + FORK_OUTPUTS)}
+    assert fork(**{**apart, output: apart[given]}) == INVALID
+
+
 @pytest.mark.parametrize("caches,more,status", [
     (None, {}, INVALID), ([], {}, INVALID), ([cache()], dict(n=-1), INVALID), ([cache()], dict(src=None), INVALID),
     ([cache()], dict(dst=None), INVALID), ([cache(), cache(n_pages=5)], {}, INVALID),
