@@ -661,8 +661,8 @@ int sbvr_rotary_write(const sbvr_rotary_args *args, const sbvr_kv_cache *cache, 
  *   end_tokens  int32 [n_end], n_end >= 0 (0: none, and not read).
  *   workspace   sbvr_beam_select_workspace_bytes, 16-byte aligned; its content
  *            needs no preparation and is not kept.
- * scores_out may be scores where n = B; apart from that inputs and outputs must not
- * overlap.  The struct is read during the call.
+ * scores_out may be scores where n = B (else that is refused); apart from that inputs
+ * and outputs must not overlap.  The struct is read during the call.
  */
 typedef struct sbvr_beam_args {
     int32_t R, B, V, n, n_end, dtype;

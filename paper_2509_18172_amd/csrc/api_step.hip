@@ -367,6 +367,8 @@ int sbvr_beam_select(const sbvr_beam_args *a, void *workspace, size_t ws_bytes, 
             return SBVR_E_ALIGNMENT;
     if (!aligned(a->logits, a->dtype == SBVR_F32 ? 4 : 2) || !aligned(workspace, 16))
         return SBVR_E_ALIGNMENT;
+    if (a->scores_out == a->scores && a->n != a->B)  // in place, one request's would lie on another's
+        return SBVR_E_INVALID_ARG;
     return launch_beam(*a, workspace, stream);
 }
 

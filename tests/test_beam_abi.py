@@ -94,6 +94,14 @@ def test_beam_refusals(bad, status):
     assert beams(**bad) == status
 
 
+@pytest.mark.parametrize("B,n", [(4, 3), (4, 5), (1, 2)])
+def test_beam_scores_in_place_of_another_width_are_refused(B, n):
+    """Request r's new scores lie where another request's old ones are read."""
+    outs = dict(zip(("tokens", "parents", "ended", "ended_tokens"), range(FAKE + 4096, FAKE + 5 * 4096, 4096)))
+    assert beams(B=B, n=n, **outs) == INVALID
+    assert beams(R=1, B=B, n=n, **outs) == INVALID
+
+
 @pytest.mark.parametrize("R,B,V,n,ends", [(1, 1, 1, 1, 0), (1, 32, 1 << 30, 64, 0), (2047, 32, 1 << 30, 1, 63), (65535, 1, 50000, 8, 2),
                                           (32, 8, 131072, 8, 2)])
 def test_beam_workspace(R, B, V, n, ends):
