@@ -712,7 +712,7 @@ int sbvr_page_usage(int R, int page_size, int n_pages, const int32_t *context_le
  * partly filled one goes to the first row that continues the parent; each further row
  * takes the next free page, into which its content has to be copied (sbvr_page_copy
  * with the lists given here, before the next tokens are written).
- *   groups      >= 1, a divisor of rows_in and of rows_out.
+ *   groups      >= 1, a divisor of rows_in and of rows_out; 0 where both are 0.
  *   free_pages  [n_free]: unused pages, taken in order from number *taken on
  *               (int32 on the device, such as the first of sbvr_batch_plan's used; NULL:
  *               0); -1 in the list, or its end: there is none.

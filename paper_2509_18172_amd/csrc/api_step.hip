@@ -403,7 +403,10 @@ int sbvr_page_fork(int groups, int rows_in, int rows_out, int page_size, const i
                    int64_t out_stride, int32_t *out_lens, int32_t *src, int32_t *dst, int32_t *tokens, int32_t *used,
                    hipStream_t stream)
 {
-    if (groups < 1 || rows_in < 0 || rows_out < 0 || rows_in % groups || rows_out % groups || n_free < 0)
+    if (groups < 0 || rows_in < 0 || rows_out < 0 || n_free < 0 || (groups == 0 && (rows_in || rows_out)))
+        return SBVR_E_INVALID_ARG;
+    groups = groups > 0 ? groups : 1;  // no groups: no rows
+    if (rows_in % groups || rows_out % groups)
         return SBVR_E_INVALID_ARG;
     int st = check_table_shape(rows_in, max_pages, table_stride, page_size);
     if (st != SBVR_OK || (st = check_table_shape(rows_out, max_pages, out_stride, page_size)) != SBVR_OK)

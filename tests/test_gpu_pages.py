@@ -214,6 +214,20 @@ def test_fork_from_no_rows():
     assert f.page_table.shape == (0, 2) and f.used.tolist() == [0]
 
 
+def test_no_requests():
+    """What a selection of no requests gives is forked and moved too."""
+    lens, table, made = i32([]), torch.empty(0, 4, dtype=torch.int32, device=DEV), caches(1, 10, 16, 2, 64)
+    usage = sb.page_usage(lens, table, 16, 10)
+    choice = sb.beam_select(torch.empty(0, 100, device=DEV), torch.empty(0, 3, device=DEV))
+    assert choice.parents.shape == (0, 3)
+    fork = sb.page_fork(lens, table, choice.parents, 16, usage.free_pages, taken=usage.counts)
+    assert fork.page_table.shape == (0, 4) and fork.context_lens.shape == fork.src.shape == (0,) and fork.used.tolist() == [0]
+    sb.page_copy(made, fork.src, fork.dst, fork.tokens)
+    assert sb.page_compact(fork.context_lens, fork.page_table, 16, 10).counts.tolist() == [0, 0]
+    with pytest.raises(sb.SBVRError):  # rows of no group
+        sb.page_fork(i32([20]), i32([[1, 2]]), choice.parents, 16, usage.free_pages)
+
+
 # ---------------------------------------------------------------------------
 # compaction
 # ---------------------------------------------------------------------------
