@@ -593,7 +593,8 @@ int sbvr_adjust_logits(const sbvr_logits_args *args, hipStream_t stream);
  *             (elements, multiples of 8, not negative), 16-byte aligned.  Rows of an
  *             output must not overlap.  q_out may be q itself, k_out k, with the
  *             same strides; apart from that inputs and outputs must not overlap.
- *   positions int32 [axes][T], row stride position_stride; any value.
+ *   positions int32 [axes][T], row stride position_stride (at least T, or 0: one row
+ *             for all axes); any value.
  *   pair_axis int32 [pairs], or NULL: axis 0 for all.  A pair whose axis is outside
  *             0 .. axes - 1 is not turned.
  *   frequencies  binary32 [pairs].

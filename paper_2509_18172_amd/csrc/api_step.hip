@@ -116,7 +116,7 @@ int check_rotary(const sbvr_rotary_args *a, const sbvr_kv_cache *cache)
     if (!a || a->T < 0 || a->heads < 0 || a->kv_heads < 0 || a->heads + (int64_t)a->kv_heads < 1 || a->head_dim < 8 ||
         a->head_dim % 8 != 0 || a->pairs < 1 || a->pairs > a->head_dim / 2 || a->axes < 1 || a->dtype < SBVR_F16 ||
         a->dtype > SBVR_F32 || (a->interleaved & ~1) || (a->inverse & ~1) || !stride_ok(a->position_stride) ||
-        (a->axes > 1 && a->position_stride < a->T))
+        (a->axes > 1 && a->position_stride != 0 && a->position_stride < a->T))
         return SBVR_E_INVALID_ARG;
     if (cache && (a->kv_heads != cache->kv_heads || a->head_dim != cache->head_dim || a->dtype != cache->dtype || a->k_out))
         return SBVR_E_INVALID_ARG;

@@ -160,10 +160,11 @@ def rotary(q, k, positions, frequencies, axes=None, interleaved: bool = False, i
            k_out=None, stream=None):
     """Queries and keys [T][heads][head_dim] (fp16, bf16 or fp32, views with
     contiguous heads; either may be None) turned by their positions: int32 [T],
-    or [axes][T] with axes (int32 [pairs]) naming each pair's.  frequencies:
-    fp32 [pairs], the angle per position; the elements behind the pairs are
-    copied.  Pairs are element i and i + pairs, or neighbours (interleaved);
-    inverse turns back.  Returns (q, k); q_out may be q, k_out k."""
+    or [axes][T] (one row expanded among them) with axes (int32 [pairs]) naming
+    each pair's.  frequencies: fp32 [pairs], the angle per position; the
+    elements behind the pairs are copied.  Pairs are element i and i + pairs, or
+    neighbours (interleaved); inverse turns back.  Returns (q, k); q_out may be
+    q, k_out k."""
     return _native.rotary(q, k, positions, frequencies, axes, interleaved, inverse, q_out, k_out, stream)
 
 

@@ -109,6 +109,20 @@ def test_several_axes(axes):
     assert torch.equal(a, b)
 
 
+@pytest.mark.parametrize("T", [1, 50])
+def test_expanded_positions(T):
+    """A text's positions are the same on all axes: one row, expanded."""
+    n = 32
+    q, k, v = qkv(T, 4, 2, 64, F16)
+    pos, which = i32(list(range(7, 7 + T))), i32([i % 3 for i in range(n)])
+    want = sb.rotary(q, k, pos, frequencies(n))
+    for g, w in zip(sb.rotary(q, k, pos.expand(3, T), frequencies(n), axes=which), want):
+        assert torch.equal(g, w)
+    cache, slots = caches(-(-T // 16), 16, 2, 64, F16, "token"), torch.arange(T, device=DEV)
+    assert torch.equal(sb.rotary_write(q, cache, k, v, slots, pos.expand(3, T), frequencies(n), axes=which), want[0])
+    assert torch.equal(cache.k.reshape(-1, 2, 64)[:T], want[1])
+
+
 def test_one_of_the_two():
     q, k, _ = qkv(5, 4, 2, 64, F16)
     pos, freq = i32([3, 1, 4, 1, 5]), frequencies(32)
