@@ -596,7 +596,7 @@ int sbvr_adjust_logits(const sbvr_logits_args *args, hipStream_t stream);
  *   positions int32 [axes][T], row stride position_stride (at least T, or 0: one row
  *             for all axes); any value.
  *   pair_axis int32 [pairs], or NULL: axis 0 for all.  A pair whose axis is outside
- *             0 .. axes - 1 is not turned.
+ *             0 .. axes - 1 is not turned: its elements are copied.
  *   frequencies  binary32 [pairs].
  * The struct is read during the call.
  */

@@ -24,6 +24,7 @@
 namespace sbvr {
 
 constexpr int ROTARY_THREADS = 256;
+constexpr float STILL = 2.f;  // as a cosine: a pair of no axis, whose elements are copied (a sum with 0 times an infinity is none)
 
 struct RotaryShape {
     int turned, per_head, valued;  // pieces of a head that are turned, all of it, and of its values
@@ -56,6 +57,9 @@ __global__ void __launch_bounds__(ROTARY_THREADS) rotary_kernel(RotaryArgs args,
 {
     extern __shared__ __attribute__((aligned(16))) float turn[];  // cosines, then sines, of [tokens][width]
     const sbvr_rotary_args &a = args.r;
+    __shared__ int some_still;  // (the same for all tokens)
+    if (threadIdx.x == 0)
+        some_still = 0;
     const int n = a.pairs, heads = a.heads + a.kv_heads;
     float *cosine = turn, *sine = turn + s.tokens * s.width;
     for (long long t0 = (long long)blockIdx.x * s.tokens; t0 < a.T; t0 += (long long)gridDim.x * s.tokens) {
@@ -68,13 +72,16 @@ __global__ void __launch_bounds__(ROTARY_THREADS) rotary_kernel(RotaryArgs args,
             const int position = a.positions[(turns ? axis : 0) * a.position_stride + t0 + t];
             double angle = (double)position * (double)a.frequencies[p] * 0.15915494309189535;  // in turns
             angle -= rint(angle);
-            float c = 1.f, sn = 0.f;
+            float c = STILL, sn = 0.f;
             if (turns)
                 sincospif(2.f * (float)angle, &sn, &c);
+            else
+                some_still = 1;
             cosine[i] = c;
             sine[i] = a.inverse ? -sn : sn;
         }
         __syncthreads();
+        const bool still = __builtin_amdgcn_readfirstlane(some_still);
 
         const int first = blockIdx.y * s.split, last = min(first + s.split, tokens * s.units);
         for (int i = first + (int)threadIdx.x; i < last; i += ROTARY_THREADS) {
@@ -130,6 +137,12 @@ __global__ void __launch_bounds__(ROTARY_THREADS) rotary_kernel(RotaryArgs args,
                         yo.e[2 * e] = (T)turned_first(w, z, c[e + 4], sn[e + 4]);
                         yo.e[2 * e + 1] = (T)turned_second(w, z, c[e + 4], sn[e + 4]);
                     }
+                    if (still)
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            xo.e[e] = c[e / 2] == STILL ? x.e[e] : xo.e[e];
+                            yo.e[e] = c[e / 2 + 4] == STILL ? y.e[e] : yo.e[e];
+                        }
                 } else {
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
@@ -137,15 +150,22 @@ __global__ void __launch_bounds__(ROTARY_THREADS) rotary_kernel(RotaryArgs args,
                         xo.e[e] = (T)turned_first(u, v, c[e], sn[e]);
                         yo.e[e] = (T)turned_second(u, v, c[e], sn[e]);
                     }
+                    if (still)
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            xo.e[e] = c[e] == STILL ? x.e[e] : xo.e[e];
+                            yo.e[e] = c[e] == STILL ? y.e[e] : yo.e[e];
+                        }
                 }
                 store_words(out + a0, turns ? to_words(xo) : wx);
                 store_words(out + b0, turns ? to_words(yo) : wy);
             } else if (turns) {
                 for (int p = p0; p < min(p0 + 8, n); ++p) {
                     const int ia = a.interleaved ? 2 * p : p, ib = a.interleaved ? 2 * p + 1 : n + p;
-                    const float u = (float)in[ia], v = (float)in[ib];
-                    out[ia] = (T)turned_first(u, v, c[p - p0], sn[p - p0]);
-                    out[ib] = (T)turned_second(u, v, c[p - p0], sn[p - p0]);
+                    const T u = in[ia], v = in[ib];
+                    const bool turn_it = c[p - p0] != STILL;
+                    out[ia] = turn_it ? (T)turned_first((float)u, (float)v, c[p - p0], sn[p - p0]) : u;
+                    out[ib] = turn_it ? (T)turned_second((float)u, (float)v, c[p - p0], sn[p - p0]) : v;
                 }
             } else {
                 int e = at;

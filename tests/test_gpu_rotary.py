@@ -11,6 +11,7 @@ pytestmark = pytest.mark.gpu
 DEV = "cuda"
 F16, BF16, F32 = torch.float16, torch.bfloat16, torch.float32
 HALF = {F16: 2.0 ** -11, BF16: 2.0 ** -8, F32: 2.0 ** -24}  # one rounding, relative
+INF, NAN = float("inf"), float("nan")
 LEAST = {F16: 2.0 ** -25, BF16: 2.0 ** -134, F32: 2.0 ** -150}  # and below the normal numbers
 
 
@@ -196,6 +197,32 @@ def test_infinite_and_nan_elements_stay_theirs():
     bad = torch.zeros_like(want, dtype=torch.bool)
     bad[1, 0, 5] = bad[1, 0, 21] = bad[1, 1, 40] = True
     assert torch.equal(got[~bad], want[~bad]) and not bool(got[bad].isfinite().any())
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16, F32])
+@pytest.mark.parametrize("D,n", [(64, 32), (64, 27), (8, 3)])
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("in_place", [False, True])
+def test_pairs_of_no_axis_keep_their_bits(dtype, D, n, interleaved, in_place):
+    """Each of a pair that is not turned stays what it is, whatever the other one is:
+    infinite, no number, a zero of either sign."""
+    T = 4 * 36
+    odd = torch.tensor([INF, -INF, NAN, 0.0, -0.0, 1.5], device=DEV)
+    x = torch.randn(T, 3, D, device=DEV, generator=torch.Generator(device=DEV).manual_seed(0)).to(dtype)
+    still = [i for i in range(n) if i % 3 == 1 or i == n - 1]
+    at = [(2 * i, 2 * i + 1) if interleaved else (i, i + n) for i in still]
+    for t in range(T):
+        for a, b in at:
+            x[t, :, a], x[t, :, b] = odd[t % 36 // 6], odd[t % 6]
+    pos, axes = i32(list(range(T))), i32([[-1, 1, 7][i % 3] if i in still else 0 for i in range(n)])
+    x0 = x.clone()
+    got = sb.rotary(x, None, pos, frequencies(n), axes=axes, interleaved=interleaved, q_out=x if in_place else None)[0]
+    keep = sum(at, ())
+    bits = torch.int32 if dtype == F32 else torch.int16
+    assert torch.equal(got[..., keep].view(bits), x0[..., keep].view(bits))
+    turned = [e for e in range(D) if e not in keep]
+    want = sb.rotary(torch.where(x0.isfinite(), x0, 0), None, pos, frequencies(n), axes=axes, interleaved=interleaved)[0]
+    assert torch.equal(got[..., turned], want[..., turned])
 
 
 @pytest.mark.parametrize("T", [1, 8, 300, 5000])
