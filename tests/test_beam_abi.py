@@ -114,6 +114,16 @@ def test_beam_workspace(R, B, V, n, ends):
     assert beams(R=R, B=B, V=V, n=n, n_end=ends, logits_stride=V, ws_bytes=need, ws=FAKE + 8) == ALIGNMENT
 
 
+def test_beam_workspace_is_a_requests():
+    """The join holds 2816 entries of all beams of a request together, of 8 bytes, each
+    part of a row has one of them at least, and a sum of 16 bytes."""
+    for R, B, V, n, ends in ((1, 1, 1, 1, 0), (1, 32, 1 << 30, 64, 0), (2047, 32, 1 << 30, 1, 63), (65535, 1, 50000, 8, 2),
+                             (32, 8, 131072, 8, 2), (3, 32, 1 << 30, 1, 0), (1, 1, 1 << 30, 1, 0)):
+        need, keep = sb.sbvr_beam_select_workspace_bytes(R, B, V, n, ends), n + ends
+        parts, rest = divmod(need, R * B * (16 + 8 * keep))
+        assert rest == 0 and 1 <= parts and B * parts * keep <= max(2816, B * keep) and need <= R * 2816 * (8 + 16)
+
+
 def test_workspaces_of_bad_shapes():
     for bad in ((-1, 1, 1, 1, 0), (1, 0, 1, 1, 0), (1, 33, 1, 1, 0), (1, 1, 0, 1, 0), (1, 1, 1, 0, 0), (1, 1, 1, 60, 5)):
         assert sb.sbvr_beam_select_workspace_bytes(*bad) == 0

@@ -265,6 +265,53 @@ def test_extreme_logits():
         check(wide, torch.zeros(1, 32, device=DEV), 3)
 
 
+def parts_of(R, B, V, n, ends=0):
+    """Parts that the operator cuts a row into: its workspace is a sum of 16 bytes
+    and n + ends entries of 8 for each."""
+    need, each = sb.sbvr_beam_select_workspace_bytes(R, B, V, n, ends), R * B * (16 + 8 * (n + ends))
+    assert need % each == 0
+    return need // each
+
+
+# Rows of three tiles of 2048 or 8192 logits in one part: one request of 32 beams has too
+# few rows for the large ones, and 64 entries a row leave no more parts (a part has a
+# tile at least, so this stays what it is when a rule for tiles or parts moves).
+IN_TURN = [(1, 2048), (2, 8192)]
+
+
+def in_turn(R, tile, rows, n, ends=()):
+    """check() of R requests of 32 beams, every row [three tiles]."""
+    V = len(rows)
+    assert parts_of(R, 32, V, n, len(ends)) == 1 and V > 2 * tile
+    logits = torch.from_numpy(np.asarray(rows, np.float32)).to(DEV).expand(32 * R, V).contiguous()
+    return check(logits, torch.zeros(R, 32, device=DEV), n, ends=ends, exact=True)
+
+
+@pytest.mark.parametrize("R,tile", IN_TURN)
+@pytest.mark.parametrize("levels", [
+    (-1e38, 5.0, 7.0), (5.0, 1e38, -3e38), (3e38, 1.0, 3.2e38), (-3e38, -2e38, 3.0), (30.0, 2e37, 2.0), (-1e9, 111.3, 110.0),
+    (2e6, -2e6, 1.9e6), (-INF, 3e38, 3e38), (INF, -INF, 1.0), (1e6, 1000001.0, 999999.0), (-1e9, -1e9, 0.0), (0.0, -1e9, -1e9)])
+def test_extreme_tiles_in_turn(R, tile, levels):
+    """The sum follows a largest logit that rises, or does not, by more than binary32
+    can tell apart."""
+    row = np.concatenate([np.float32(v) + np.arange(tile, dtype=np.float32) % 5 for v in levels])
+    in_turn(R, tile, row, 64)
+
+
+@pytest.mark.parametrize("R,tile", IN_TURN)
+@pytest.mark.parametrize("kind", ["equal", "rising", "falling", "two", "steps", "stairs", "some", "plateau"])
+def test_ordered_tiles_in_turn(R, tile, kind):
+    """Equal logits, and lists that are too long, beside what earlier tiles have left
+    (multiples of 1/8, so that equal scores are equal in every form)."""
+    v = np.arange(3 * tile - 5)  # (the last piece is moved back)
+    row = {"equal": 0 * v, "rising": v // 16, "falling": -(v // 16), "two": v % 2, "steps": v // tile, "stairs": -(v // tile),
+           # 30 of the first tile are better than the next one's equal ones, 34 are not
+           "some": np.where(v < tile, 2.0 * (v % 61 == 7) * (v < 61 * 30), 1.0),
+           # the best are of the last tile, as many as are kept, behind as good ones of the first
+           "plateau": 3.0 * ((v < 40) | (v > 3 * tile - 70)) + (v // tile == 1)}[kind] / 8.0
+    in_turn(R, tile, row, 60, ends=(1, 7, tile, 2 * tile + 3))
+
+
 def test_zeros_of_either_sign_are_equal():
     for V in (300, 9000, 70000):
         logits = torch.zeros(2, V, dtype=F32, device=DEV)
@@ -342,15 +389,7 @@ def test_equal_best_among_many_close_ones():
         assert got.parents[0].tolist() == [5] * 4
 
 
-def parts_of(R, B, V, n, ends=0):
-    """Parts that the operator cuts a row into: its workspace is a sum of 16 bytes
-    and n + ends entries of 8 for each."""
-    need, each = sb.sbvr_beam_select_workspace_bytes(R, B, V, n, ends), R * B * (16 + 8 * (n + ends))
-    assert need % each == 0
-    return need // each
-
-
-@pytest.mark.parametrize("R,tile", [(1, 2048), (2, 8192)])
+@pytest.mark.parametrize("R,tile", IN_TURN)
 @pytest.mark.parametrize("low", [-1e9, float(np.finfo(np.float32).min), -2e6, 1.0])
 @pytest.mark.parametrize("near", [111.0, 1000.0, 30000.0, 900000.0])
 def test_a_sum_of_several_tiles_refers_to_one_number(R, tile, low, near):
@@ -370,6 +409,28 @@ def test_a_sum_of_several_tiles_refers_to_one_number(R, tile, low, near):
     row[2 * tile::64] = top - np.float32(1 / 16)  # (the largest is in the tile before)
     logits = torch.from_numpy(row).to(DEV).expand(R * B, V).contiguous()
     check(logits, torch.zeros(R, B, device=DEV), n)
+
+
+def test_equal_best_in_a_thinned_list():
+    """A tile's four best are equal and alone above some hundred that are listed with
+    them, behind tiles that have filled the list of the kept: where they lie in four
+    wavefronts' shares of the list (3 of 32 times, by the order of the additions to
+    it), thinning leaves exactly them, and they have to be put in order all the same."""
+    B, n, tile, V = 32, 4, 8192, 8192 * 45
+    assert V >= 3 * tile * parts_of(1, B, V, n)
+    rng = np.random.default_rng(0)
+    scores = torch.full((1, B), -100.0, device=DEV)
+    scores[0, 5] = 0
+    for trial in range(100):
+        row = np.full(V, -3.0, np.float32)
+        for t in range(V // tile):  # a thousand that share their upper 16 bits, each tile's above the last one's
+            at = t * tile + rng.permutation(tile)[:1000]
+            row[at] = 1 + (t * 1000 + rng.integers(0, 999, 1000)) * 2.0 ** -23
+        best = V - tile + rng.permutation(tile)[:4]
+        row[best] = 1 + 60 * 1000 * 2.0 ** -23
+        got = sb.beam_select(torch.from_numpy(row).to(DEV).expand(B, V).contiguous(), scores, n=n)
+        assert got.tokens[0].tolist() == sorted(best.tolist()), trial
+        assert got.parents[0].tolist() == [5] * 4
 
 
 @pytest.mark.parametrize("R,B,V", [(1, 4, 1000), (40, 8, 5001), (2047, 32, 100), (3, 32, 60000)])

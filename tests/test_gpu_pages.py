@@ -91,6 +91,29 @@ def test_usage_of_many_rows_and_pages(R, width, pages):
     check_usage(lens.tolist(), table, 16, pages, stride=width + 1)
 
 
+@pytest.mark.parametrize("pages", [703, 704, 705, 11263, 11264, 11265, 11264 + 704, 11264 + 705, 2 * 11264, 2 * 11264 + 1])
+@pytest.mark.parametrize("R,width", [(20, 300), (600, 65)])
+def test_usage_at_the_edges_of_owners_and_shares(pages, R, width):
+    """A workgroup owns 11264 pages, a wavefront or a later launch's workgroup has 704
+    of them; the entries whole and split."""
+    rng = np.random.default_rng(pages)
+    table = rng.integers(0, pages, (R, width))
+    table[0, :4] = [0, pages - 1, pages, -1]
+    check_usage(rng.integers(64, width * 16, R).tolist(), table.tolist(), 16, pages)
+
+
+@pytest.mark.parametrize("R,width,pages", [
+    (511, 64, 300), (512, 64, 300), (4095, 64, 5000), (4096, 64, 5000),        # chunks of 64 entries: two and sixteen splits
+    (2000, 100, 400001), (4096, 65, 17 * 11264), (600, 64, 129 * 11264)])     # as many as 256 workgroups leave: 7, 15 and 1
+def test_usage_at_the_edges_of_splits(R, width, pages):
+    rng = np.random.default_rng(R)
+    lens = rng.integers(0, width * 16 + 40, R)
+    lens[-1] = width * 16
+    table = rng.integers(0, pages, (R, width))
+    table[-1, -1] = pages - 1
+    check_usage(lens.tolist(), table.tolist(), 16, pages)
+
+
 def test_usage_of_one_page_by_all():
     check_usage([160] * 500, [[5] * 10] * 500, 16, 9)
 
@@ -288,6 +311,18 @@ def test_compact_many_entries(R, width, pages):
     lens = rng.integers(0, width * 16 + 30, R)
     lens[rng.random(R) < 0.7] //= 20
     check_compact(lens.tolist(), rng.integers(-1, pages + 1, (R, width)).tolist(), 16, pages, stride=width + 2)
+
+
+@pytest.mark.parametrize("R,width,pages", [
+    (2, 1024, 2500), (1, 2047, 3000), (1, 2048, 3000), (1, 2049, 3000), (2049, 1, 4100),  # with the tables, and without
+    (2048, 64, 70000), (2048, 64, 131073), (1, 131073, 131072), (131, 1001, 131072)])     # one workgroup, and many
+def test_compact_at_the_edges_of_its_forms(R, width, pages):
+    rng = np.random.default_rng(R + width)
+    lens = rng.integers(0, width * 16 + 40, R)
+    lens[-1] = width * 16
+    table = rng.integers(0, pages, (R, width))
+    table[-1, -1], table[0, 0] = pages - 1, -1
+    check_compact(lens.tolist(), table.tolist(), 16, pages, stride=width + 1)
 
 
 def test_compact_without_rows():
