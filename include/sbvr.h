@@ -653,7 +653,9 @@ int sbvr_rotary_write(const sbvr_rotary_args *args, const sbvr_kv_cache *cache, 
  * Exponentials are summed in binary32 within a lane and in binary64 from there on,
  * scores are binary64 -- in which they are compared, so that the continuations of one
  * beam are ordered by their logits wherever these differ by more than 2^-52 of the
- * score -- and rounded to binary32 at the end.
+ * score (nearer ones, such as ordinary logits beside a score of -1e30, come in an order
+ * that is neither the logits' nor the tokens', the same in every call) -- and rounded to
+ * binary32 at the end.
  *   R, B, V  R >= 0 requests of 1 <= B <= SBVR_BEAMS_MAX beams, V tokens (at most
  *            2^30; R * B at most 65535), else SBVR_E_UNSUPPORTED.
  *   n        >= 1, n + n_end at most SBVR_BEAM_KEEP_MAX (else SBVR_E_UNSUPPORTED).

@@ -289,8 +289,8 @@ __global__ void __launch_bounds__(BEAM_THREADS, 6) beam_part_kernel(sbvr_beam_ar
         if ((tid & 3) == 0)
             groups[tid >> 2] = in_group;
         // many to keep: the 64 groups' maxima are no close bound, the lanes' of each
-        // wavefront are (128 rows of 131072 in binary16: 64 kept 57.7 us, by the groups
-        // 59.9; 48 alike; 32 29.3 by the groups, 30.4)
+        // wavefront are (128 rows of 131072 in binary16: 64 kept 68.3 us, by the groups
+        // 70.4; 48 34.0 both ways; 32 29.4 by the groups, 30.1)
         const bool many = s.keep > 32;
         if (many) {
             const uint32_t reached = reached_by(ordered(best), (s.keep + WAVES - 1) / WAVES, 16);
@@ -688,9 +688,10 @@ __global__ void __launch_bounds__(THREADS) beam_join_kernel(sbvr_beam_args a, Be
 
 namespace {
 
-// pieces of a thread: large tiles unless that leaves half of the chip empty (binary16,
-// 8 beams: 8 rows of 131072 take 10.5 us with four, 12.2 with one; 256 rows 26 and 47;
-// 16 of 32000 10.7 and 10.1)
+// pieces of a thread: large tiles unless the rows have too few of them for half of the chip
+// (binary16, 8 beams: 8 rows of 131072 take 10.5 us with four, 12.2 with one; 256 rows 26
+// and 47; 16 of 32000 10.7 and 10.1).  Where BEAM_ENTRIES leaves fewer parts than that a
+// part has several tiles (8 rows of 131072, 64 continuations: 32 workgroups, 65 us).
 int beam_pieces(long long rows, int V)
 {
     return rows * ((V + 8191ll) / 8192) >= 128 ? 4 : 1;

@@ -64,9 +64,10 @@ __device__ __forceinline__ void store_words(T *p, const Words<T> &w)
     *(LooseWords<T> *)p = w;
 }
 
-// A value whose address is the same in every lane and that no kernel of these
-// operators writes, read on the scalar side: a vector load would take a lane's
-// worth of work per wavefront and have its wait among those of the data.
+// A value whose address is the same in every lane and that the kernel that reads it
+// does not write (an earlier one may have: a kernel's start drops what the scalar
+// cache holds), read on the scalar side: a vector load would take a lane's worth of
+// work per wavefront and have its wait among those of the data.
 template <typename T>
 __device__ __forceinline__ T uniform_load(const T *p)
 {
