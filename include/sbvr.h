@@ -640,7 +640,7 @@ int sbvr_rotary_write(const sbvr_rotary_args *args, const sbvr_kv_cache *cache, 
  * A continuation (b, v) has the score
  *     s(b, v) = scores[r][b] + logits[v] - log(sum_u exp(logits[u]))      (row r * B + b)
  * and one is better than another if its score is higher or, of equal ones, its beam
- * is lower, or its token in the same beam.
+ * is lower, or in the same beam its logit is higher, or, of equal logits, its token lower.
  *     tokens, parents, scores_out [R][n]: the n best continuations whose token is
  *         no end token, best first: token, beam and score; -1, -1 and -infinity
  *         past the last one there is.
@@ -651,11 +651,9 @@ int sbvr_rotary_write(const sbvr_rotary_args *args, const sbvr_kv_cache *cache, 
  * their logits are not read; nor has a token whose logit is -infinity or NaN, which
  * adds nothing to the sum.  A logit of +infinity counts as the largest binary32 number.
  * Exponentials are summed in binary32 within a lane and in binary64 from there on,
- * scores are binary64 -- in which they are compared, so that the continuations of one
- * beam are ordered by their logits wherever these differ by more than 2^-52 of the
- * score (nearer ones, such as ordinary logits beside a score of -1e30, come in an order
- * that is neither the logits' nor the tokens', the same in every call) -- and rounded to
- * binary32 at the end.
+ * scores are binary64 -- in which they are compared, and which may be equal where the
+ * logits differ by less than 2^-52 of the score, as beside a score of -1e30: of one beam
+ * the logits decide then -- and rounded to binary32 at the end.
  *   R, B, V  R >= 0 requests of 1 <= B <= SBVR_BEAMS_MAX beams, V tokens (at most
  *            2^30; R * B at most 65535), else SBVR_E_UNSUPPORTED.
  *   n        >= 1, n + n_end at most SBVR_BEAM_KEEP_MAX (else SBVR_E_UNSUPPORTED).

@@ -478,32 +478,42 @@ __global__ void __launch_bounds__(BEAM_THREADS, 6) beam_part_kernel(sbvr_beam_ar
 // instead of 40; n = 16 394 instead of 53.
 constexpr int JOIN_RANKED = 256;
 
+// Of equal scores the lower beam is the better, in a beam the higher logit -- a score of
+// -1e30 has no room for them --, and of equal logits the lower place: entries are in the
+// order of beam, part and rank, and those of a part in that of their keys.  So the place
+// decides unless two of a beam have one score and different logits, which the next number
+// behind the lower one's logit shows: it then has that score too.
 struct Candidate {
     double score;
-    int place;  // number of the entry; of equal scores the lower place is better
+    int place;  // number of the entry
 };
 __device__ __forceinline__ bool better_than(const Candidate &a, const Candidate &b)
 {
     return (a.score > b.score) | ((a.score == b.score) & (a.place < b.place));  // (no branch: LDS reads stay in flight)
 }
-// One request.  Entries are in the order of beam, part and rank, so of those with
-// equal scores the lower place has the lower beam, or token.  A chain of latencies:
-// the entries are loaded beside the sums.
+// The whole order of equal scores as one number of 49 bits, more than 0.
+constexpr int ORDER_BITS = 49;
+__device__ __forceinline__ uint64_t order_of(uint32_t logit, int beam, int place)
+{
+    return (uint64_t)(SBVR_BEAMS_MAX - 1 - beam) << 44 | (uint64_t)logit << 12 | (uint64_t)(4095 - place);
+}
+
+// One request.  A chain of latencies: the entries are loaded beside the sums.
 template <int THREADS>
 __global__ void __launch_bounds__(THREADS) beam_join_kernel(sbvr_beam_args a, BeamShape s, const PartSum *sums,
                                                             const uint64_t *entries)
 {
     constexpr int PER = THREADS == 1024 ? (BEAM_ENTRIES + 1023) / 1024 : 4, WAVES = THREADS / 64;
     constexpr uint32_t END = 1u << 31;
-    extern __shared__ double list_score[];  // and behind them, each entry's place, beam and whether it is an end, and its token
+    extern __shared__ double list_score[];  // and behind them, each entry's place, beam and whether it is an end, its token and logit
     __shared__ double add[SBVR_BEAMS_MAX], beam_reference[SBVR_BEAMS_MAX];
     __shared__ __attribute__((aligned(16))) uint32_t group[256];
-    __shared__ int rank[256], count;
+    __shared__ int rank[256], count, hides;  // hides: a score may be that of another logit of its beam too
     __shared__ float score_out[SBVR_BEAM_KEEP_MAX], ended[SBVR_BEAMS_MAX];
     __shared__ int token_out[SBVR_BEAM_KEEP_MAX], parent_out[SBVR_BEAM_KEEP_MAX], ended_token[SBVR_BEAMS_MAX];
     const int tid = threadIdx.x, lane = tid & 63, per_beam = s.parts * s.keep, all = a.B * per_beam;
     const long long request = blockIdx.x;
-    uint32_t *list_what = (uint32_t *)(list_score + all), *list_token = list_what + all;
+    uint32_t *list_what = (uint32_t *)(list_score + all), *list_token = list_what + all, *list_logit = list_token + all;
     entries += request * all;
     sums += request * a.B * s.parts;
 
@@ -550,7 +560,7 @@ __global__ void __launch_bounds__(THREADS) beam_join_kernel(sbvr_beam_args a, Be
         ended_token[tid] = -1;
     }
     if (tid == 0)
-        count = 0;
+        count = hides = 0;
     __syncthreads();
 
     // As in a tile: the n-th largest of 64 groups' best scores that go on (256 where n
@@ -559,13 +569,16 @@ __global__ void __launch_bounds__(THREADS) beam_join_kernel(sbvr_beam_args a, Be
     float mine = -INFINITY;
     double score[PER];
     int beam[PER];
+    bool same_as_next = false;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
         const int place = i * THREADS + tid;
         beam[i] = small_div(min(place, all - 1), per_beam, 1.f / (float)per_beam);
         // (the score of a beam that is none is -infinity)
         const double value = add[beam[i]] + ((double)unordered((uint32_t)(key[i] >> 32)) - beam_reference[beam[i]]);
+        const double next = add[beam[i]] + ((double)unordered((uint32_t)(key[i] >> 32) + 1) - beam_reference[beam[i]]);
         score[i] = (place < all) & (key[i] != 0) & (add[beam[i]] > -INFINITY) ? value : -INFINITY;
+        same_as_next |= (next == score[i]) & (score[i] > -INFINITY);
         mine = fmaxf(mine, key[i] & END_ENTRY ? (float)score[i] : -INFINITY);
     }
     // A group is every 64th or 256th thread: neighbours are of one list, in order.
@@ -601,11 +614,14 @@ __global__ void __launch_bounds__(THREADS) beam_join_kernel(sbvr_beam_args a, Be
             mine_listed += listed[i];
         if (mine_listed) {
             int k = atomicAdd(&count, mine_listed);
+            if (same_as_next)
+                hides = 1;
 #pragma unroll
             for (int i = 0; i < PER; ++i)
                 if (listed[i]) {
                     list_score[k] = score[i];
                     list_what[k] = (uint32_t)beam[i] << 16 | (i * THREADS + tid) | (key[i] & END_ENTRY ? 0 : END);
+                    list_logit[k] = (uint32_t)(key[i] >> 32);
                     list_token[k++] = ~(uint32_t)(key[i] | END_ENTRY);
                 }
         }
@@ -615,8 +631,9 @@ __global__ void __launch_bounds__(THREADS) beam_join_kernel(sbvr_beam_args a, Be
     int c = list_them();
     if (c > JOIN_RANKED) {
         // Equal or nearly so: only what is no worse than the n-th best that goes on, found
-        // bit by bit -- its score, and of those that have it the places that are left.
-        // Each step counts in a word of its own.
+        // bit by bit -- its score, and of those that have it the places that are left, or,
+        // where their logits are not all alike, the orders.  Each step counts in a word of
+        // its own.
         __syncthreads();
         if (tid < 256)
             group[tid] = 0;
@@ -639,15 +656,40 @@ __global__ void __launch_bounds__(THREADS) beam_join_kernel(sbvr_beam_args a, Be
             bound = reach(bit, [&](int i) { return ordered(score[i]) >= candidate; }) >= a.n ? candidate : bound;
         }
         const int equal = a.n - reach(64, [&](int i) { return ordered(score[i]) > bound; });
+#pragma unroll
+        for (int i = 0; i < PER; ++i)
+            if (listed[i] && ordered(score[i]) == bound)
+                group[65] = (uint32_t)(key[i] >> 32);  // any one's
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < PER; ++i)
+            if (listed[i] && ordered(score[i]) == bound && group[65] != (uint32_t)(key[i] >> 32))
+                group[66] = 1;
+        __syncthreads();
         int places = 0;  // as many as still leave `equal` of them, or fewer
-        for (int bit = 11; bit >= 0; --bit) {
-            const int candidate = places | 1 << bit;
-            const int n = reach(65 + bit, [&](int i) { return ordered(score[i]) == bound && i * THREADS + tid < candidate; });
-            places = n <= equal ? candidate : places;
+        uint64_t last = 0;
+        if (!group[66]) {
+            for (int bit = 11; bit >= 0; --bit) {
+                const int candidate = places | 1 << bit;
+                const int n = reach(67 + bit, [&](int i) { return ordered(score[i]) == bound && i * THREADS + tid < candidate; });
+                places = n <= equal ? candidate : places;
+            }
+        } else {
+            places = 4096;
+            for (int bit = ORDER_BITS - 1; bit >= 0; --bit) {
+                const uint64_t candidate = last | 1ull << bit;
+                const int n = reach(67 + bit, [&](int i) {
+                    return ordered(score[i]) == bound &&
+                           order_of((uint32_t)(key[i] >> 32), beam[i], i * THREADS + tid) >= candidate;
+                });
+                last = n >= equal ? candidate : last;
+            }
         }
 #pragma unroll
         for (int i = 0; i < PER; ++i)
-            listed[i] &= (ordered(score[i]) > bound) | ((ordered(score[i]) == bound) & (i * THREADS + tid < places));
+            listed[i] &= (ordered(score[i]) > bound) |
+                         ((ordered(score[i]) == bound) & (i * THREADS + tid < places) &
+                          (order_of((uint32_t)(key[i] >> 32), beam[i], i * THREADS + tid) >= last));
         c = list_them();
     }
     for (int i = tid; i < c; i += THREADS) {
@@ -655,13 +697,26 @@ __global__ void __launch_bounds__(THREADS) beam_join_kernel(sbvr_beam_args a, Be
         const Candidate me = {list_score[i], (int)(w & 0xffff)};
         const uint32_t beam = (w >> 16) & 0x7fff;
         int better = 0, going = 0, same = 0;  // all, those that go on, and ends of the beam
+        if (!hides) {
 #pragma unroll 4
-        for (int j = 0; j < c; ++j) {
-            const uint32_t u = list_what[j];
-            const int b = better_than(Candidate{list_score[j], (int)(u & 0xffff)}, me), end = u >> 31;
-            better += b;
-            going += b & ~end;
-            same += b & end & (int)(((u >> 16) & 0x7fff) == beam);
+            for (int j = 0; j < c; ++j) {
+                const uint32_t u = list_what[j];
+                const int b = better_than(Candidate{list_score[j], (int)(u & 0xffff)}, me), end = u >> 31;
+                better += b;
+                going += b & ~end;
+                same += b & end & (int)(((u >> 16) & 0x7fff) == beam);
+            }
+        } else {
+            const uint64_t order = order_of(list_logit[i], beam, me.place);
+            for (int j = 0; j < c; ++j) {
+                const uint32_t u = list_what[j], of = (u >> 16) & 0x7fff;
+                const int b = (list_score[j] > me.score) |
+                              ((list_score[j] == me.score) & (order_of(list_logit[j], of, u & 0xffff) > order));
+                const int end = u >> 31;
+                better += b;
+                going += b & ~end;
+                same += b & end & (int)(of == beam);
+            }
         }
         if (!(w & END)) {
             if (going < a.n) {
@@ -754,7 +809,7 @@ int launch_beam(const sbvr_beam_args &a, void *workspace, hipStream_t stream)
     const uint64_t *entries_in = entries;
     void *argv[] = {&args, &shape, &sums_in, &entries_in};
     const int all = a.B * s.parts * s.keep;
-    const size_t lds = (size_t)all * (sizeof(double) + 2 * sizeof(uint32_t));
+    const size_t lds = (size_t)all * (sizeof(double) + 3 * sizeof(uint32_t));
     return all <= 1024 ? launch_kernel((const void *)beam_join_kernel<256>, dim3(a.R), dim3(256), lds, stream, argv)
                        : launch_kernel((const void *)beam_join_kernel<1024>, dim3(a.R), dim3(1024), lds, stream, argv);
 }

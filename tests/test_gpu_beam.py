@@ -312,6 +312,52 @@ def test_ordered_tiles_in_turn(R, tile, kind):
     in_turn(R, tile, row, 60, ends=(1, 7, tile, 2 * tile + 3))
 
 
+def first_of(row, n, without=()):
+    """The n best tokens of a beam whose scores are all the same number: by logit, and
+    equal ones by number."""
+    row = cleaned(row)
+    order = np.argsort(-row, kind="stable")[:n + len(without)].tolist()
+    return [v for v in order if v not in without and row[v] > -INF][:n]
+
+
+@pytest.mark.parametrize("dtype", [F16, F32])
+@pytest.mark.parametrize("V", [40, 5000, 70001, 300007])
+@pytest.mark.parametrize("n,ends", [(1, 0), (4, 0), (8, 3), (40, 2), (64, 0)])
+@pytest.mark.parametrize("low", [-1e30, float(np.finfo(np.float32).min)])
+def test_logits_decide_where_a_score_hides_them(dtype, V, n, ends, low):
+    """Beams as good as dead, whose score has no room for a logit: of one beam the
+    higher logit is the better, in whatever parts of the row the two lie."""
+    B = 3
+    logits, _ = make(2, B, V, dtype, seed=V + n)
+    logits[:, ::3] = logits[:, :1]  # many alike, too
+    scores = torch.tensor([[low, low, low], [-INF, low, 0.0]], device=DEV)
+    logits[5, 2:] = -INF  # two continuations of the one that lives
+    host = logits.float().cpu().numpy()
+    end = [int(host[b].argmax()) for b in (0, 1, 4)][:ends]
+    got = sb.beam_select(logits, scores, n=n, end_tokens=torch.tensor(end, dtype=torch.int32, device=DEV))
+    want = [(0, v) for v in first_of(host[0], n, end)]
+    want = (want + [(1, v) for v in first_of(host[1], n, end)] + [(2, v) for v in first_of(host[2], n, end)])[:n]
+    pairs = list(zip(got.parents[0].tolist(), got.tokens[0].tolist()))
+    assert pairs[:len(want)] == want and pairs[len(want):] == [(-1, -1)] * (n - len(want))
+    best = first_of(host[0], n)
+    assert got.ended_tokens[0, 0].item() == next((v for v in best if v in end), -1)
+    alive = sorted([0, 1], key=lambda v: (-host[5][v], v))
+    want = ([(2, v) for v in alive if v not in end] + [(1, v) for v in first_of(host[4], n, end)])[:n]
+    pairs = list(zip(got.parents[1].tolist(), got.tokens[1].tolist()))
+    assert pairs[:len(want)] == want and pairs[len(want):] == [(-1, -1)] * (n - len(want))
+
+
+@pytest.mark.parametrize("V", [300, 70001])
+@pytest.mark.parametrize("n", [1, 5, 64])
+def test_logits_decide_where_they_are_small_beside_the_sum(V, n):
+    """Logits around 1e-25: exp(logit) is 1, and every score the sum's logarithm."""
+    rng = np.random.default_rng(V + n)
+    rows = (rng.integers(-V, V, (4, V)) * 1e-25).astype(np.float32)
+    got = sb.beam_select(torch.from_numpy(rows).to(DEV), torch.full((2, 2), -2.0, device=DEV), n=n)
+    for r in range(2):
+        assert got.parents[r].tolist() == [0] * n and got.tokens[r].tolist() == first_of(rows[2 * r], n)
+
+
 def test_zeros_of_either_sign_are_equal():
     for V in (300, 9000, 70000):
         logits = torch.zeros(2, V, dtype=F32, device=DEV)
