@@ -133,7 +133,9 @@ def search(model, prompts, beams, n, end, store=SharedPages, **more):
         ended.append((choice.ended, history))
         store.lens = store.lens + new
         store.follow(choice.parents)
-        kept = history.gather(1, choice.parents.long()[:, :, None].expand(-1, -1, history.shape[2]))
+        # (a row that found no continuation has the parent -1 and the score -infinity; its history is not used)
+        parents = choice.parents.long().clamp(min=0)
+        kept = history.gather(1, parents[:, :, None].expand(-1, -1, history.shape[2]))
         history = torch.cat([kept, choice.tokens[:, :, None]], dim=2)
         tokens, scores = choice.tokens, choice.scores
     return history, scores, ended

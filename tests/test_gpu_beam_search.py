@@ -39,6 +39,26 @@ def test_shared_pages_change_nothing(example, lengths, beams, n, page, every):
     assert bool((tokens >= 0).all()) and bool((scores[:, :-1] >= scores[:, 1:]).all())
 
 
+def test_fewer_continuations_than_beams(example, monkeypatch):
+    """Two tokens allowed and four beams: two rows of the first step have no parent, and
+    the second step fills them."""
+    plain, allowed = example.forward, [3, 500]
+
+    def masked(*args):
+        logits = plain(*args).float()
+        only = torch.full_like(logits, -float("inf"))
+        only[:, allowed] = logits[:, allowed]
+        return only
+    monkeypatch.setattr(example, "forward", masked)
+    for n in (1, 2, 6):
+        runs = [example.search(example.Decoder(pages=256, seed=4), prompts(20, 33), 4, n, end=7, store=store)
+                for store in (example.SharedPages, example.OwnPages)]
+        (tokens, scores, _), (want_tokens, want_scores, _) = runs
+        assert torch.equal(tokens, want_tokens) and torch.equal(scores, want_scores)
+        assert scores.isfinite().sum(1).tolist() == [min(2 ** n, 4)] * 2
+        assert set(tokens[scores.isfinite()].flatten().tolist()) <= set(allowed)
+
+
 def test_scores_are_the_tokens_own(example):
     """A beam's score is the sum of its tokens' log probabilities, as plain steps on
     its own tokens give them: logits of other products and other attention kernels,
